@@ -24,7 +24,8 @@ OBJ_DIR = os.path.join(HERE, "_build")
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(HERE, "csrc", "*.hip")))
+    """The decode path's translation units, then the cache operators' (their names differ)."""
+    return [s for d in ("csrc", "csrc_cache") for s in sorted(glob.glob(os.path.join(HERE, d, "*.hip")))]
 
 
 def _run(cmd):
@@ -38,7 +39,7 @@ def build(verbose=False, jobs=None):
     """Compile every translation unit (in parallel), then link libcobs.so."""
     from concurrent.futures import ThreadPoolExecutor
     os.makedirs(OBJ_DIR, exist_ok=True)
-    inc = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
+    inc = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"), "-I", os.path.join(HERE, "csrc_cache")]
     srcs = sources()
     objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-4] + ".o") for s in srcs]
     cmds = [[HIPCC, *FLAGS, *inc, "-c", s, "-o", o] for s, o in zip(srcs, objs)]

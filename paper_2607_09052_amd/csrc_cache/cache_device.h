@@ -1,0 +1,97 @@
+// Device helpers of the cache operators.
+#pragma once
+
+#include "cache_kernels.h"
+
+namespace cobs {
+
+// The tokens of one (batch row, KV head) that queries attend to, as frames:
+// aligned runs of 32 positions a .. a + 31, of which lo .. hi - 1 take part.
+// First the frames of the valid selected blocks (tokens before the window start
+// ws), then those from ws to the end E = C + n of the context and the draft
+// (with the whole cache attended, ws = 0 and there are no blocks).  A frame
+// lies within one block, so within one page, and wholly inside the cache (whose
+// capacity is a multiple of 32).  Its tokens at positions below C are attended to
+// by every query, those from C on by the queries with their bit set.
+struct Attended {
+  int C, n, E, ws;       // context, drafted tokens, their sum, window start
+  int nq;                // live queries
+  int nsel, fpb;         // valid selected blocks, frames of a block
+  int lsh;
+  const int32_t* sel;
+  __device__ __forceinline__ int sel_frames() const { return nsel * fpb; }
+  __device__ __forceinline__ int frames() const {
+    return sel_frames() + (E > ws ? ((E + kFrame - 1) / kFrame - ws / kFrame) : 0);
+  }
+  __device__ __forceinline__ void frame(int f, int& a, int& lo, int& hi) const {
+    const int ns = sel_frames();
+    if (f < ns) {
+      a = (sel[f / fpb] << lsh) + kFrame * (f % fpb);
+      lo = a;
+      hi = min(a + kFrame, ws);
+    } else {
+      a = (ws / kFrame + (f - ns)) * kFrame;
+      lo = max(a, ws);
+      hi = min(a + kFrame, E);
+    }
+  }
+};
+
+// Called by every thread of a workgroup of NT threads (with a barrier inside
+// when there is a selection); `red`: NT / 64 ints of LDS.
+template <int NT>
+__device__ __forceinline__ Attended attended(const AttendParams& p, int b, int h, int* red) {
+  Attended x;
+  x.C = clamp_len(p.seq_lens[b], p.tmax);
+  x.n = 0;
+  x.nq = p.N;
+  if (p.mask) {
+    x.n = clamp_len(p.draft_lens[b], min(p.N, p.tmax - x.C));
+    x.nq = x.n;
+  }
+  x.E = x.C + x.n;
+  x.ws = p.sparse ? max(0, x.C - p.w) : 0;
+  x.lsh = p.lsh;
+  x.fpb = (1 << p.lsh) / kFrame;
+  x.nsel = 0;
+  x.sel = p.sel + ((int64_t)b * p.hkv + h) * p.s;
+  if (p.sparse && p.s > 0) {
+    const int nc = blocks_of(x.ws, p.lsh);
+    int valid = p.s;                      // first entry that breaks the ascending run of candidates
+    for (int i = threadIdx.x; i < p.s; i += NT) {
+      const int bi = x.sel[i], prev = x.sel[i > 0 ? i - 1 : 0];
+      if (bi < 0 || bi >= nc || (i > 0 && bi <= prev)) valid = min(valid, i);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) valid = min(valid, __shfl_xor(valid, o, 64));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = valid;
+    __syncthreads();
+    valid = red[0];
+#pragma unroll
+    for (int i = 1; i < NT / 64; ++i) valid = min(valid, red[i]);
+    x.nsel = valid;
+  }
+  return x;
+}
+
+// Position of the first selected block >= blk among the nsel valid ones.
+__device__ __forceinline__ int sel_lower_bound(const Attended& x, int blk) {
+  int lo = 0, hi = x.nsel;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (x.sel[mid] < blk) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ float load_elem(const void* p, int64_t i, bool f32) {
+  if (f32) return static_cast<const float*>(p)[i];
+  return bf16_lo((uint32_t) static_cast<const uint16_t*>(p)[i]);
+}
+
+__device__ __forceinline__ void store_elem(void* p, int64_t i, float v, bool f32) {
+  if (f32) static_cast<float*>(p)[i] = v;
+  else static_cast<uint16_t*>(p)[i] = (uint16_t)f32_to_bf16_rne(v);
+}
+
+}  // namespace cobs

@@ -1,0 +1,63 @@
+// Launch interface between the host side of the cache operators and their kernels.
+#pragma once
+
+#include "cobs_device.h"
+
+namespace cobs {
+
+constexpr int kMaxQueries = 64;      // query tokens per row: the bits of a tree mask word
+constexpr int kFrame = 32;           // tokens of a frame (see Attended)
+
+// What the query tokens of a call attend to (include/cobs_cache.h), and the sizes.
+struct AttendParams {
+  KvView kv;
+  const void* q;                // [B, N, Hq, d], fp32 or bf16
+  const int32_t* seq_lens;
+  const int32_t* draft_lens;    // null: no draft
+  const uint64_t* mask;
+  const int32_t* sel;
+  int sparse;
+  int B, hkv, hq, G, N, d, tmax, s, w, lsh;
+  int kv_f32, io_bf16;
+  float c;
+};
+
+struct TreeParams {
+  AttendParams a;
+  void* out;
+  float* lse;
+  float* part;                  // split partials (tree_workspace)
+};
+
+struct WeightsParams {
+  AttendParams a;
+  const float* lse;
+  const float* prev;
+  float* weights;
+};
+
+struct EvictParams {
+  const float* weights;
+  const int32_t* seq_lens;
+  int32_t* kept;
+  int32_t* new_lens;
+  int B, hkv, tmax, keep, sinks, recent;
+};
+
+struct CompactParams {
+  KvView src, dst;
+  const int32_t* kept;
+  const int32_t* seq_lens;
+  const int32_t* first;
+  const float* weights;
+  float* weights_out;
+  int per_head, num_kept, B, hkv, d, tmax, dst_max, kv_f32, in_place;
+};
+
+size_t tree_workspace(const AttendParams& a);
+hipError_t launch_tree(const TreeParams& p, hipStream_t st);
+hipError_t launch_weights(const WeightsParams& p, hipStream_t st);
+hipError_t launch_evict(const EvictParams& p, hipStream_t st);
+hipError_t launch_compact(const CompactParams& p, hipStream_t st);
+
+}  // namespace cobs

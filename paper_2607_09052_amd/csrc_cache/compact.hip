@@ -1,0 +1,142 @@
+// The kept tokens of a cache moved together (cobs_compact_cache): a copy of
+// rows, bound by HBM.
+//
+// To another cache every (destination position, K or V) is independent.  In place
+// a row may land where another row still has to be read from.  With entries
+// that ascend strictly and kept[j] >= first + j, a position below first + j1 is the
+// source of no entry from j1 on, so a workgroup that owns a column slice of one
+// (batch row, KV head) walks the entries in order, reads a batch of rows into
+// registers, waits, and writes it: no write meets a later read.
+#include "cache_device.h"
+
+namespace cobs {
+
+constexpr int kCompactThreads = 256;
+
+__device__ __forceinline__ int kept_at(const CompactParams& p, int b, int h, int j) {
+  return p.kept[(p.per_head ? ((int64_t)b * p.hkv + h) : (int64_t)b) * p.num_kept + j];
+}
+
+// Destination of entry j and its source; false when the entry moves nothing.
+__device__ __forceinline__ bool move_of(const CompactParams& p, int b, int h, int T, int first, int j, int64_t& from,
+                                        int64_t& to) {
+  const int t = kept_at(p, b, h, j);
+  if (t < 0 || t >= T || j >= p.dst_max - first) return false;
+  from = kv_offset(p.src, b, h, t);
+  to = kv_offset(p.dst, b, h, first + j);
+  return from >= 0 && to >= 0;
+}
+
+// out of place: one thread per 16 bytes of a row, K and V both
+template <int CPR>
+__global__ __launch_bounds__(kCompactThreads) void compact_copy_kernel(CompactParams p) {
+  const int h = blockIdx.y, b = blockIdx.z, es = p.kv_f32 ? 4 : 2;
+  const int T = clamp_len(p.seq_lens[b], p.tmax);
+  const int first = p.first ? clamp_len(p.first[b], p.dst_max) : 0;
+  const int row = (blockIdx.x * kCompactThreads + threadIdx.x) / CPR, ch = threadIdx.x % CPR;
+  if (row < p.num_kept) {
+    int64_t from, to;
+    const bool ok = move_of(p, b, h, T, first, row, from, to);
+    if (ok) {
+      const uint4 k = reinterpret_cast<const uint4*>(static_cast<const char*>(p.src.k) + from * es)[ch];
+      const uint4 v = reinterpret_cast<const uint4*>(static_cast<const char*>(p.src.v) + from * es)[ch];
+      reinterpret_cast<uint4*>(static_cast<char*>(const_cast<void*>(p.dst.k)) + to * es)[ch] = k;
+      reinterpret_cast<uint4*>(static_cast<char*>(const_cast<void*>(p.dst.v)) + to * es)[ch] = v;
+    }
+  }
+}
+
+__global__ __launch_bounds__(kCompactThreads) void compact_weights_kernel(CompactParams p) {
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int T = clamp_len(p.seq_lens[b], p.tmax);
+  const int first = p.first ? clamp_len(p.first[b], p.dst_max) : 0;
+  const int64_t u = (int64_t)b * p.hkv + h;
+  const int end = p.num_kept > T - first ? p.num_kept : T - first;     // entries, then the tail to T
+  const int j = blockIdx.x * kCompactThreads + threadIdx.x;
+  if (j >= end || j >= p.dst_max - first) return;
+  int64_t from, to;
+  float w = 0.0f;
+  if (j < p.num_kept && move_of(p, b, h, T, first, j, from, to)) w = p.weights[u * p.tmax + kept_at(p, b, h, j)];
+  p.weights_out[u * p.dst_max + first + j] = w;
+}
+
+// in place: blockIdx.x = slice of a row's 16-byte chunks (SC of them, K then V),
+// and one more for the weights
+template <int CPR, int SC>
+__global__ __launch_bounds__(kCompactThreads) void compact_in_place_kernel(CompactParams p) {
+  constexpr int NS = CPR / SC, RPP = kCompactThreads / SC, U = 8;
+  const int h = blockIdx.y, b = blockIdx.z, es = p.kv_f32 ? 4 : 2, tid = threadIdx.x;
+  const int T = clamp_len(p.seq_lens[b], p.tmax);
+  const int first = p.first ? clamp_len(p.first[b], p.dst_max) : 0;
+  const int slice = blockIdx.x;
+  if (slice == 2 * NS) {
+    const int64_t u = ((int64_t)b * p.hkv + h) * p.tmax;
+    const int end = p.num_kept > T - first ? p.num_kept : T - first;
+    for (int j0 = 0; j0 < end; j0 += kCompactThreads * U) {
+      float w[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int j = j0 + i * kCompactThreads + tid;
+        int64_t from, to;
+        w[i] = 0.0f;
+        if (j < p.num_kept && move_of(p, b, h, T, first, j, from, to)) w[i] = p.weights[u + kept_at(p, b, h, j)];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int j = j0 + i * kCompactThreads + tid;
+        if (j < end && j < p.dst_max - first) p.weights_out[u + first + j] = w[i];
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  char* base = static_cast<char*>(const_cast<void*>(slice < NS ? p.src.k : p.src.v));
+  const int ch = (slice % NS) * SC + tid % SC;
+  for (int j0 = 0; j0 < p.num_kept; j0 += RPP * U) {
+    uint4 x[U];
+    int64_t to[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int j = j0 + i * RPP + tid / SC;
+      int64_t from;
+      if (j < p.num_kept && move_of(p, b, h, T, first, j, from, to[i]))
+        x[i] = reinterpret_cast<const uint4*>(base + from * es)[ch];
+      else to[i] = -1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (to[i] >= 0) reinterpret_cast<uint4*>(base + to[i] * es)[ch] = x[i];
+    __syncthreads();
+  }
+}
+
+template <int CPR>
+static hipError_t launch_compact_rows(const CompactParams& p, hipStream_t st) {
+  if (p.in_place) {
+    const int slices = 2 * CPR / 4 + (p.weights ? 1 : 0);
+    hipLaunchKernelGGL((compact_in_place_kernel<CPR, 4>), dim3(slices, p.hkv, p.B), dim3(kCompactThreads), 0, st, p);
+    return hipGetLastError();
+  }
+  const int rpw = kCompactThreads / CPR;
+  if (p.num_kept > 0)
+    hipLaunchKernelGGL(compact_copy_kernel<CPR>, dim3((p.num_kept + rpw - 1) / rpw, p.hkv, p.B), dim3(kCompactThreads),
+                       0, st, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.weights) return e;
+  const int64_t span = p.num_kept > p.tmax ? p.num_kept : p.tmax;
+  hipLaunchKernelGGL(compact_weights_kernel, dim3((unsigned)((span + kCompactThreads - 1) / kCompactThreads), p.hkv, p.B),
+                     dim3(kCompactThreads), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact(const CompactParams& p, hipStream_t st) {
+  if (p.num_kept == 0 && !p.weights) return hipSuccess;
+  switch (p.d * (p.kv_f32 ? 4 : 2) / 16) {
+    case 8: return launch_compact_rows<8>(p, st);
+    case 16: return launch_compact_rows<16>(p, st);
+    default: return launch_compact_rows<32>(p, st);
+  }
+}
+
+}  // namespace cobs
