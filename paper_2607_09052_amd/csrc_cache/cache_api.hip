@@ -126,7 +126,7 @@ cobs_status_t cobs_tree_decode(const cobs_config_t* cfg, const void* q, cobs_dty
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 256))) return COBS_ERR_WORKSPACE;
   p.out = out;
   p.lse = lse;
-  p.part = static_cast<float*>(ws);
+  p.part_ml = static_cast<float*>(ws);
   return hip_status(launch_tree(p, static_cast<hipStream_t>(stream)));
 }
 

@@ -84,6 +84,36 @@ __device__ __forceinline__ int sel_lower_bound(const Attended& x, int blk) {
   return lo;
 }
 
+__device__ __forceinline__ int wave_uniform32(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The value that the lane of the other half of the wave (l ^ 32) holds.
+__device__ __forceinline__ float other_half(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float((threadIdx.x & 32) ? s[0] : s[1]);
+}
+
+// Transposing LDS read of bf16: the 16 lanes of a group give the addresses of 4
+// rows by four 8-byte pieces; lane i gets column i of the 4 rows.
+__device__ __forceinline__ auto tr_read(const char* p) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) s16x4*)(const_cast<char*>(p)));
+}
+
+// Four outputs sum / total at element `i` (a multiple of 4) in the outputs' type; 0 for a total of 0.
+__device__ __forceinline__ void store_row4(void* out, int64_t i, float4 sum, float total, int bf16) {
+  const float f = total != 0.0f ? 1.0f / total : 0.0f;
+  if (total == 0.0f) sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const float4 y = make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f);
+  if (bf16) {
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + i) =
+        make_uint2(f32x2_to_bf16x2_rne(y.x, y.y), f32x2_to_bf16x2_rne(y.z, y.w));
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(out) + i) = y;
+  }
+}
+
 __device__ __forceinline__ float load_elem(const void* p, int64_t i, bool f32) {
   if (f32) return static_cast<const float*>(p)[i];
   return bf16_lo((uint32_t) static_cast<const uint16_t*>(p)[i]);

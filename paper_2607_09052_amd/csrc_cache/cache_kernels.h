@@ -26,7 +26,11 @@ struct TreeParams {
   AttendParams a;
   void* out;
   float* lse;
-  float* part;                  // split partials (tree_workspace)
+  // parts of a context that is split over workgroups (tree_workspace): per (unit, split,
+  // query row) the log2-domain maximum and sum, and D unnormalised outputs
+  float* part_ml;
+  float* part_o;
+  int units, mtiles, nsplit;    // (row, KV head) pairs, query row tiles, splits
 };
 
 struct WeightsParams {
@@ -54,6 +58,9 @@ struct CompactParams {
   int per_head, num_kept, B, hkv, d, tmax, dst_max, kv_f32, in_place;
 };
 
+// Row tiles and splits of a call, from its shape alone (so that a workspace's size
+// and a result's bits depend on nothing else).
+void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit);
 size_t tree_workspace(const AttendParams& a);
 hipError_t launch_tree(const TreeParams& p, hipStream_t st);
 hipError_t launch_weights(const WeightsParams& p, hipStream_t st);

@@ -1,85 +1,96 @@
-// Attention of several query tokens a row over the cache and their draft
-// (cobs_tree_decode).  One workgroup per (query, query head); its four waves
-// take the frames of the attended tokens round-robin, each with a running
-// maximum, sum and output, which they merge through LDS at the end.  Per frame
-// lane l scores token l & 31 over half l >> 5 of the head dimension.
+// cobs_tree_decode: the plan of a call, its launches, and the kernel that joins
+// the parts of a split context.  The attention itself is in tree_kernel.h.
 #include "cache_device.h"
 
 namespace cobs {
 
+constexpr int kMergeThreads = 256;
+
+// One thread per 4 outputs of a query row: the parts' weights 2^(m_k - max m) and
+// sums in split order.
 template <int D>
-__global__ __launch_bounds__(256) void tree_plain_kernel(TreeParams p) {
-  constexpr int CPL = D / 64;
-  __shared__ float qs[D];
-  __shared__ float wm[4], wl[4], wo[4][D];
-  __shared__ int red[4];
+__global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeParams p) {
+  constexpr int TPR = D / 4;
   const AttendParams& a = p.a;
-  const int hq = blockIdx.x, i = blockIdx.y, b = blockIdx.z;
-  const int h = hq / a.G, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const Attended x = attended<256>(a, b, h, red);
-  const int64_t row = ((int64_t)b * a.N + i) * a.hq + hq;
-  for (int e = tid; e < D; e += 256) qs[e] = load_elem(a.q, row * D + e, !a.io_bf16) * a.c;
-  __syncthreads();
-  float m = -INFINITY, l = 0.0f, o[CPL];
-#pragma unroll
-  for (int j = 0; j < CPL; ++j) o[j] = 0.0f;
-  const uint64_t bits = a.mask ? a.mask[(int64_t)b * a.N + i] : 0;
-  const int64_t rs = a.kv.table ? a.kv.d : a.kv.st;
-  const bool f32 = a.kv_f32 != 0;
-  const int nf = i < x.nq ? x.frames() : 0;
-  for (int f = wave; f < nf; f += 4) {
-    int t0, lo, hi;
-    x.frame(f, t0, lo, hi);
-    const int64_t base = hi > lo ? kv_offset(a.kv, b, h, t0) : -1;
-    if (base < 0) continue;
-    const int t = t0 + (lane & 31), half = lane >> 5;
-    const bool seen = t >= lo && t < hi && (t < x.C || ((bits >> (t - x.C)) & 1));
-    float sc = 0.0f;
-    if (seen)
-      for (int e = half * (D / 2); e < (half + 1) * (D / 2); ++e)
-        sc += qs[e] * load_elem(a.kv.k, base + (t - t0) * rs + e, f32);
-    sc += __shfl_xor(sc, 32, 64);
-    if (!seen) sc = -INFINITY;
-    const float mn = fmaxf(m, wave_max(sc));
-    const float ref = mn == -INFINITY ? 0.0f : mn;
-    const float alpha = __expf(m - ref), pr = seen ? __expf(sc - ref) : 0.0f;
-    l = l * alpha + 0.5f * wave_sum(pr);
-    m = mn;
-#pragma unroll
-    for (int j = 0; j < CPL; ++j) o[j] *= alpha;
-    for (int r = 0; r < kFrame; ++r) {
-      if (!__shfl((int)seen, r, 64)) continue;
-      const float pt = __shfl(pr, r, 64);
-#pragma unroll
-      for (int j = 0; j < CPL; ++j) o[j] += pt * load_elem(a.kv.v, base + r * rs + j * 64 + lane, f32);
+  const int M = a.N * a.G;
+  const int64_t idx = (int64_t)blockIdx.x * (kMergeThreads / TPR) + threadIdx.x / TPR;
+  const int d4 = threadIdx.x % TPR;
+  if (idx >= (int64_t)p.units * M) return;
+  const int unit = (int)(idx / M), row = (int)(idx % M), b = unit / a.hkv, h = unit % a.hkv;
+  const int i = row / a.G;
+  const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
+  const int C = clamp_len(a.seq_lens[b], a.tmax);
+  const int nq = a.mask ? clamp_len(a.draft_lens[b], min(a.N, a.tmax - C)) : a.N;
+  float top = -INFINITY, total = 0.0f;
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (i < nq) {
+    const int64_t first = (int64_t)unit * p.nsplit * M + row;
+    for (int k = 0; k < p.nsplit; ++k) top = fmaxf(top, p.part_ml[2 * (first + (int64_t)k * M)]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    for (int k = 0; k < p.nsplit; ++k) {
+      const int64_t r = first + (int64_t)k * M;
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * r);
+      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+      const float4 o = *reinterpret_cast<const float4*>(p.part_o + r * D + 4 * d4);
+      total += f * ml.y;
+      sum.x += f * o.x; sum.y += f * o.y; sum.z += f * o.z; sum.w += f * o.w;
     }
+    top = ref;
   }
-  if (lane == 0) { wm[wave] = m; wl[wave] = l; }
-#pragma unroll
-  for (int j = 0; j < CPL; ++j) wo[wave][j * 64 + lane] = o[j];
-  __syncthreads();
-  const float top = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3])), M = top == -INFINITY ? 0.0f : top;
-  float L = 0.0f, f[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    f[k] = __expf(wm[k] - M);
-    L += f[k] * wl[k];
-  }
-  for (int e = tid; e < D; e += 256) {
-    float s = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s += f[k] * wo[k][e];
-    store_elem(p.out, row * D + e, L != 0.0f ? s / L : 0.0f, !a.io_bf16);
-  }
-  if (p.lse && tid == 0) p.lse[row] = L != 0.0f ? M + logf(L) : -INFINITY;
+  store_row4(p.out, at * D + 4 * d4, sum, total, a.io_bf16);
+  if (d4 == 0 && p.lse) p.lse[at] = total != 0.0f ? top * 0.6931471805599453f + logf(total) : -INFINITY;
 }
 
-size_t tree_workspace(const AttendParams&) { return 256; }
+hipError_t launch_tree_bf16_d64(const TreeParams& p, int wq, int grid, hipStream_t st);
+hipError_t launch_tree_bf16_d128(const TreeParams& p, int wq, int grid, hipStream_t st);
+hipError_t launch_tree_f32_d64(const TreeParams& p, int wq, int grid, hipStream_t st);
+hipError_t launch_tree_f32_d128(const TreeParams& p, int wq, int grid, hipStream_t st);
 
-hipError_t launch_tree(const TreeParams& p, hipStream_t st) {
-  const dim3 grid(p.a.hq, p.a.N, p.a.B);
-  if (p.a.d == 128) hipLaunchKernelGGL(tree_plain_kernel<128>, grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL(tree_plain_kernel<64>, grid, dim3(256), 0, st, p);
+void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit) {
+  const int M = a.N * a.G;
+  *wq = M <= 32 ? 1 : (M <= 64 ? 2 : 4);
+  *mtiles = (M + *wq * 32 - 1) / (*wq * 32);
+  // frames of the longest row, and as many splits as give the chip's 256 CUs two
+  // workgroups each, of at least 8 frames
+  const int64_t dense = (a.tmax + kFrame - 1) / kFrame;
+  const int64_t sparse = (int64_t)a.s * ((1 << a.lsh) / kFrame) + (a.w + a.N) / kFrame + 2;
+  const int64_t frames = a.sparse && sparse < dense ? sparse : dense;
+  const int64_t tiles = (int64_t)a.B * a.hkv * *mtiles;
+  int64_t n = (512 + tiles - 1) / tiles;
+  n = n < frames / 8 ? n : frames / 8;
+  *nsplit = (int)(n < 1 ? 1 : (n > 128 ? 128 : n));
+}
+
+// Upper bound over the attended sets (the plan of a sparse call has no more splits than the dense one).
+size_t tree_workspace(const AttendParams& a) {
+  AttendParams x = a;
+  x.sparse = 0;
+  int wq, mtiles, nsplit;
+  tree_plan(x, &wq, &mtiles, &nsplit);
+  const size_t rows = (size_t)a.B * a.hkv * nsplit * a.N * a.G;
+  const size_t ml = (rows * 2 * sizeof(float) + 255) / 256 * 256;
+  return ml + (rows * a.d * sizeof(float) + 255) / 256 * 256;
+}
+
+hipError_t launch_tree(const TreeParams& q, hipStream_t st) {
+  TreeParams p = q;
+  int wq;
+  tree_plan(p.a, &wq, &p.mtiles, &p.nsplit);
+  p.units = p.a.B * p.a.hkv;
+  const size_t rows = (size_t)p.units * p.nsplit * p.a.N * p.a.G;
+  p.part_o = p.part_ml + (rows * 2 * sizeof(float) + 255) / 256 * 256 / sizeof(float);
+  // eight XCDs: a multiple of 8 workgroup slots (see tree_kernel)
+  const int64_t groups = ((int64_t)p.units * p.nsplit + 7) / 8 * 8, grid = groups * p.mtiles;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const int g = (int)grid;
+  hipError_t e;
+  if (p.a.kv_f32) e = p.a.d == 64 ? launch_tree_f32_d64(p, wq, g, st) : launch_tree_f32_d128(p, wq, g, st);
+  else e = p.a.d == 64 ? launch_tree_bf16_d64(p, wq, g, st) : launch_tree_bf16_d128(p, wq, g, st);
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  const int64_t rows_out = (int64_t)p.units * p.a.N * p.a.G, per = kMergeThreads / (p.a.d / 4);
+  const dim3 mg((unsigned)((rows_out + per - 1) / per));
+  if (p.a.d == 64) hipLaunchKernelGGL(tree_merge_kernel<64>, mg, dim3(kMergeThreads), 0, st, p);
+  else hipLaunchKernelGGL(tree_merge_kernel<128>, mg, dim3(kMergeThreads), 0, st, p);
   return hipGetLastError();
 }
 

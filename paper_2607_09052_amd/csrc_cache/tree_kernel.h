@@ -1,0 +1,476 @@
+// Attention of several query tokens a row over the cache and their draft
+// (cobs_tree_decode), on the matrix cores.
+//
+// The M = N G query rows of one (batch row, KV head) share its keys and values, so
+// they are the columns of the products: S^T = K Q^T (32 tokens by 32 rows a tile)
+// and O^T = V^T P^T.  With tokens as rows the probabilities that a lane holds
+// after the softmax are the operand of the second product as they stand (the
+// token order inside a k-step is permuted, which V's reads follow), every row's
+// maximum, sum and output scale are one value a lane, and a maximum needs one
+// exchange between the two halves of the wave.
+//
+// A workgroup is WQ x WT waves: WQ waves take 32 query rows each and share the
+// frames in LDS, WT groups of them take different frames.  Few rows (M <= 32) are
+// bound by HBM: four waves with a frame each in flight.  Many rows are bound by
+// the matrix cores: 128 rows a workgroup read each key and value once.  The frames
+// of a row's context are split over workgroups; tree_merge_kernel joins the
+// parts.
+//
+// Frames travel HBM -> registers (a frame ahead) -> LDS, in 16-byte chunks that
+// are swizzled by row against bank conflicts:
+//   bf16 K  chunk c of row r at c ^ (r % 16): the A operand of 32x32x16 reads 16
+//           bytes of 32 rows;
+//   bf16 V  at c ^ 4 (r % 4) (64-element heads: c ^ 2 (r & 2)): the transposing read
+//           (ds_read_b64_tr_b16) takes 4 tokens by 16 columns per 16 lanes;
+//   fp32 K  at c ^ (r % 32); fp32 V by column, as stored.
+// fp32 products run on 32x32x2 fp32 operands.  bf16 products take an fp32 query
+// and its probabilities as two bf16 parts (the rest is below 2^-17 of them), since
+// the outputs are fp32; with bf16 outputs, whose rounding is 2^-8, one part.
+//
+// Drafted tokens stand in the frames behind the context; what a query's mask
+// leaves out gets score -inf.  A value that is not finite would still reach every
+// row of the product as 0 times it, so such elements of drafted tokens enter LDS
+// as 0 and are added afterwards to the rows that see them (add_nonfinite).
+#pragma once
+
+#include "cache_device.h"
+
+namespace cobs {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kTreeThreads = 256;
+constexpr int kTable = 256;            // frame descriptors held in LDS at a time
+
+template <int D, int WQ, bool F32>
+struct TreeShape {
+  static constexpr int WT = 4 / WQ;                       // frame groups
+  static constexpr int ES = F32 ? 4 : 2;
+  static constexpr int CPR = D * ES / 16;                 // 16-byte chunks of a row
+  static constexpr int FPI = (WQ == 4 && !F32) ? 2 : 1;   // frames of a group's pass
+  static constexpr int ROWS = FPI * kFrame;
+  static constexpr int NBUF = WQ == 1 ? 1 : 2;            // wave-private frames need no second buffer
+  static constexpr int TILE = ROWS * D * ES;              // bytes of a K or V tile
+  static constexpr int STAGE = 2 * TILE;
+  static constexpr int POOL = WT * NBUF * STAGE;          // at least 4 waves' outputs, 32 x D fp32 each
+  static_assert(POOL >= 4 * 32 * D * 4 || WQ == 2, "room for the waves' outputs");
+  static constexpr int LDS = POOL > 4 * 32 * D * 4 ? POOL : 4 * 32 * D * 4;
+  static constexpr int NT = WQ * 64;                      // threads of a group
+  static constexpr int RPP = NT / CPR;                    // rows a load instruction of the group covers
+  static constexpr int LD = ROWS / RPP;                   // loads of a thread for K (as many for V)
+};
+
+// A frame in the table: element offset of its first row; its live rows lo .. hi - 1 (relative), position a.
+struct FrameEntry {
+  int64_t base;
+  int a;
+  int16_t lo, hi;
+};
+
+template <int CPR, bool F32>
+__device__ __forceinline__ int k_chunk(int row, int c) {
+  return c ^ (row & (CPR < 32 ? CPR - 1 : 31));
+}
+template <int CPR, bool F32>
+__device__ __forceinline__ int v_chunk(int row, int c) {
+  if constexpr (F32) return c;
+  else return CPR == 16 ? c ^ ((row & 3) << 2) : c ^ ((row & 2) << 1);
+}
+
+// 16 bytes with the elements that are not finite cleared; `found`: whether there were any.
+template <bool F32>
+__device__ __forceinline__ uint4 finite_only(uint4 x, bool& found) {
+  uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  found = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F32) {
+      if ((w[i] & 0x7f800000u) == 0x7f800000u) { w[i] = 0; found = true; }
+    } else {
+      if ((w[i] & 0x7f80u) == 0x7f80u) { w[i] &= 0xffff0000u; found = true; }
+      if ((w[i] & 0x7f800000u) == 0x7f800000u) { w[i] &= 0x0000ffffu; found = true; }
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The rows of a wave: query row `r` of the M = N G of a (row, KV head), or none.
+struct QueryRow {
+  int64_t at;        // (b N + i) Hq + head: row of q, out and lse
+  bool live;
+  uint64_t bits;     // drafted tokens that it sees
+};
+__device__ __forceinline__ QueryRow query_row(const AttendParams& a, const Attended& x, int b, int h, int r) {
+  QueryRow q;
+  const int i = r / a.G, g = r - i * a.G;
+  q.live = i < x.nq;
+  q.at = ((int64_t)b * a.N + i) * a.hq + h * a.G + g;
+  q.bits = (q.live && a.mask) ? a.mask[(int64_t)b * a.N + i] : 0;
+  return q;
+}
+
+// Sum over visible drafted tokens j in `bad` of p V[j][d] for the elements of V that are not finite,
+// added to the lane's outputs.  Rare (an overflowed value), so from memory and element by element.
+template <int D, bool F32>
+__device__ __forceinline__ void add_nonfinite(const AttendParams& a, const Attended& x, int b, int h, const QueryRow& q,
+                                           uint64_t bad, float m, float c2, f32x16_t (&o)[D / 32]) {
+  const int half = (threadIdx.x & 63) >> 5;
+  while (bad) {
+    const int j = __builtin_ctzll(bad);
+    bad &= bad - 1;
+    const int64_t off = kv_offset(a.kv, b, h, x.C + j);
+    if (off < 0) continue;
+    const bool see = q.live && ((q.bits >> j) & 1);
+    float s = 0.0f;
+    if (see)
+      for (int e = 0; e < D; ++e) s += load_elem(a.q, q.at * D + e, !a.io_bf16) * load_elem(a.kv.k, off + e, F32);
+    const float p = see ? __builtin_amdgcn_exp2f(s * c2 - m * c2) : 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float v = load_elem(a.kv.v, off + 32 * dt + 8 * (i >> 2) + 4 * half + (i & 3), F32);
+        if (see && !(fabsf(v) < INFINITY)) o[dt][i] += p * v;
+      }
+  }
+}
+
+// Partial of a split, per query row: (log2-domain maximum, sum) and D unnormalised outputs.
+__device__ __forceinline__ int64_t part_row(const TreeParams& p, int unit, int split, int r) {
+  return ((int64_t)unit * p.nsplit + split) * (p.a.N * p.a.G) + r;
+}
+
+// Outputs 0 and lse -inf for the rows of a tile that belong to no live query.
+template <int D>
+__device__ __forceinline__ void clear_padding(const TreeParams& p, int b, int h, int first, int rows, int nq) {
+  const AttendParams& a = p.a;
+  const int end = min(first + rows, a.N * a.G);
+  for (int idx = max(first, nq * a.G) * (D / 4) + threadIdx.x; idx < end * (D / 4); idx += kTreeThreads) {
+    const int row = idx / (D / 4), d4 = idx % (D / 4), i = row / a.G;
+    const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
+    store_row4(p.out, at * D + 4 * d4, make_float4(0.0f, 0.0f, 0.0f, 0.0f), 0.0f, a.io_bf16);
+    if (d4 == 0 && p.lse) p.lse[at] = -INFINITY;
+  }
+}
+
+template <int D, int WQ, bool F32, int PARTS>
+__global__ __launch_bounds__(kTreeThreads, F32 ? 1 : 2) void tree_kernel(TreeParams p) {
+  using S = TreeShape<D, WQ, F32>;
+  constexpr int WT = S::WT, CPR = S::CPR, LD = S::LD, NT = S::NT, FPI = S::FPI;
+  constexpr int NDT = D / 32;
+  __shared__ __align__(16) char pool[S::LDS];
+  __shared__ FrameEntry table[kTable];
+  __shared__ float s_m[4][32], s_l[4][32];
+  __shared__ unsigned long long s_bad[WT];
+  __shared__ int red[4];
+
+  const AttendParams& a = p.a;
+  // Workgroups go round-robin to the 8 XCDs; the row tiles of one part of the
+  // context, which read the same keys and values, follow each other on one.
+  const int slot = blockIdx.x >> 3, group = (slot / p.mtiles) * 8 + (blockIdx.x & 7), mt = slot % p.mtiles;
+  if (group >= p.units * p.nsplit) return;
+  const int unit = group / p.nsplit, split = group % p.nsplit;
+  const int b = unit / a.hkv, h = unit % a.hkv;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tg = wave / WQ, wq = wave % WQ, half = lane >> 5, gt = tid % NT;
+  const Attended x = attended<kTreeThreads>(a, b, h, red);
+  const int row0 = (mt * WQ + wq) * 32;                         // the wave's query rows
+  if (p.nsplit == 1) clear_padding<D>(p, b, h, mt * WQ * 32, WQ * 32, x.nq);
+  if (mt * WQ * 32 >= x.nq * a.G) return;                       // the tile's rows are all padding
+  const QueryRow q = query_row(a, x, b, h, row0 + (lane & 31));
+  const float c2 = a.c * 1.4426950408889634f;
+  if (tid < WT) s_bad[tid] = 0;
+
+  // ---- the query rows as the B operand: column lane % 32, k = 8 half + j of every step
+  constexpr int QR = F32 ? D / 2 : 1, QK = F32 ? 1 : D / 16;
+  float qf[QR];
+  sbf16x8_t qb[QK][F32 ? 1 : PARTS];
+  if constexpr (F32) {
+#pragma unroll
+    for (int u = 0; u < D / 8; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        qf[4 * u + j] = q.live ? load_elem(a.q, q.at * D + 8 * u + 4 * half + j, !a.io_bf16) : 0.0f;
+  } else {
+#pragma unroll
+    for (int ks = 0; ks < QK; ++ks) {
+      const int e = 16 * ks + 8 * half;
+      if constexpr (PARTS == 1) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (q.live) w = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + q.at * D + e);
+        qb[ks][0] = __builtin_bit_cast(sbf16x8_t, w);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        if (q.live) {
+          const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + q.at * D + e);
+          const float4 s0 = s[0], s1 = s[1];
+          v[0] = s0.x; v[1] = s0.y; v[2] = s0.z; v[3] = s0.w;
+          v[4] = s1.x; v[5] = s1.y; v[6] = s1.z; v[7] = s1.w;
+        }
+        split_bf16x8<PARTS>(v, qb[ks]);
+      }
+    }
+  }
+
+  f32x16_t o[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+  float m = -INFINITY, l = 0.0f;          // raw units; the lane's own half of the sum
+
+  const int nf = x.frames();
+  const int per = ((nf + p.nsplit - 1) / p.nsplit + WT * FPI - 1) / (WT * FPI) * (WT * FPI);
+  const int f_lo = min(split * per, nf), f_hi = min(f_lo + per, nf);
+  const int64_t rs = a.kv.table ? a.kv.d : a.kv.st;
+  const int64_t rsb = rs * S::ES;
+  char* const mine = pool + tg * S::NBUF * S::STAGE;
+
+  uint4 kr[LD], vr[LD];
+  // pass `it` of this group: frames first + it WT FPI + tg FPI ..
+  auto load = [&](int fi0, int cnt) {
+#pragma unroll
+    for (int j = 0; j < LD; ++j) {
+      const int row = j * S::RPP + gt / CPR, fi = fi0 + (j * S::RPP) / kFrame;
+      const int fc = fi < cnt ? fi : 0;
+      const FrameEntry e = table[fc];
+      if (fi < cnt && e.hi > e.lo) {
+        const int64_t off = e.base * S::ES + (row % kFrame) * rsb + (gt % CPR) * 16;
+        kr[j] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.kv.k) + off);
+        vr[j] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.kv.v) + off);
+      }
+    }
+  };
+  auto store = [&](int fi0, int cnt, char* buf) {
+#pragma unroll
+    for (int j = 0; j < LD; ++j) {
+      const int row = j * S::RPP + gt / CPR, fi = fi0 + (j * S::RPP) / kFrame, c = gt % CPR;
+      uint4 k = kr[j], v = vr[j];
+      const FrameEntry e = table[fi < cnt ? fi : 0];
+      const int r = row % kFrame;
+      if (fi >= cnt || r < e.lo || r >= e.hi) {       // rows that take no part: whatever memory holds there
+        k = make_uint4(0, 0, 0, 0);
+        v = k;
+      } else if (e.a + r >= x.C) {
+        bool found;
+        v = finite_only<F32>(v, found);
+        if (found) atomicOr(&s_bad[tg], 1ull << (e.a + r - x.C));
+      }
+      *reinterpret_cast<uint4*>(buf + (row * CPR + k_chunk<CPR, F32>(row, c)) * 16) = k;
+      *reinterpret_cast<uint4*>(buf + S::TILE + (row * CPR + v_chunk<CPR, F32>(row, c)) * 16) = v;
+    }
+  };
+  auto attend = [&](int fi0, int cnt, const char* buf) {
+#pragma unroll
+    for (int fr = 0; fr < FPI; ++fr) {
+      if (fi0 + fr >= cnt) break;
+      const FrameEntry e = table[fi0 + fr];
+      const int lo = wave_uniform32(e.lo), hi = wave_uniform32(e.hi), ea = wave_uniform32(e.a);
+      if (hi <= lo) continue;
+      // ---- S^T: 32 tokens x 32 query rows
+      const int kr0 = fr * kFrame + (lane & 31);
+      f32x16_t s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+      if constexpr (F32) {
+#pragma unroll
+        for (int u = 0; u < D / 8; ++u) {
+          const float4 kk = *reinterpret_cast<const float4*>(buf + (kr0 * CPR + k_chunk<CPR, F32>(kr0, 2 * u + half)) * 16);
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.x, qf[4 * u], s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.y, qf[4 * u + 1], s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.z, qf[4 * u + 2], s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.w, qf[4 * u + 3], s, 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const sbf16x8_t kk =
+              *reinterpret_cast<const sbf16x8_t*>(buf + (kr0 * CPR + k_chunk<CPR, F32>(kr0, 2 * ks + half)) * 16);
+#pragma unroll
+          for (int k = PARTS - 1; k >= 0; --k) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qb[ks][k], s, 0, 0, 0);
+        }
+      }
+      if (lo > 0 || hi < kFrame || ea + hi > x.C) {
+        // bit t of `vis`: whether the lane's query row sees token t of the frame
+        const int to_c = x.C - ea;                        // tokens of the context (32 and more: all)
+        uint32_t vis = to_c >= kFrame ? ~0u : (to_c > 0 ? (1u << to_c) - 1u : 0u);
+        vis |= to_c >= kFrame ? 0u : (uint32_t)(to_c > 0 ? q.bits << to_c : q.bits >> -to_c);
+        vis &= (hi < kFrame ? (1u << hi) - 1u : ~0u) & (~0u << lo);
+        vis >>= 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (vis >> (8 * (i >> 2) + (i & 3))) & 1u ? s[i] : -INFINITY;
+      }
+      // ---- streaming softmax: lane l has row l % 32, the tokens of its half
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      top = fmaxf(top, other_half(top));
+      if (__ballot(top > m)) {
+        const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
+        const float alpha = __builtin_amdgcn_exp2f((m - ref) * c2);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+      }
+      const float mc = m == -INFINITY ? 0.0f : m * c2;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -mc));
+        l += s[i];
+      }
+      // ---- O^T += V^T P^T
+      const char* vt = buf + S::TILE + fr * kFrame * CPR * 16;
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = 8 * (i >> 2) + 4 * half + (i & 3);
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            const float v = *reinterpret_cast<const float*>(vt + r * CPR * 16 + (32 * dt + (lane & 31)) * 4);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], o[dt], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          sbf16x8_t pb[PARTS];
+          float pv[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) pv[j] = s[8 * ks + j];
+          split_bf16x8<PARTS>(pv, pb);
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) {
+            // tokens 16 ks + 4 half + 0..3 and + 8 more, columns 32 dt + lane % 32
+            const int r = 16 * ks + 4 * half + ((lane & 15) >> 2), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            const char* at = vt + (lane & 1) * 8;
+            const s16x4_t v0 = tr_read(at + (r * CPR + v_chunk<CPR, F32>(r, c)) * 16);
+            const s16x4_t v1 = tr_read(at + ((r + 8) * CPR + v_chunk<CPR, F32>(r + 8, c)) * 16);
+            typedef short s16x8_t __attribute__((ext_vector_type(8)));
+            const s16x8_t vv = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int k = PARTS - 1; k >= 0; --k)
+              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(sbf16x8_t, vv), pb[k], o[dt], 0, 0, 0);
+          }
+        }
+      }
+    }
+  };
+
+  for (int t0 = f_lo; t0 < f_hi; t0 += kTable) {
+    const int cnt = min(kTable, f_hi - t0);
+    __syncthreads();                                    // the table and the tiles are free
+    if (tid < cnt) {
+      int fa, lo, hi;
+      x.frame(t0 + tid, fa, lo, hi);
+      int64_t base = hi > lo ? kv_offset(a.kv, b, h, fa) : -1;
+      FrameEntry e;
+      e.base = base < 0 ? 0 : base;
+      e.a = fa;
+      e.lo = (int16_t)(base < 0 ? 0 : lo - fa);
+      e.hi = (int16_t)(base < 0 ? 0 : hi - fa);
+      table[tid] = e;
+    }
+    __syncthreads();
+    constexpr int STEP = WT * FPI;
+    const int passes = (cnt + STEP - 1) / STEP, mineoff = tg * FPI;
+    load(mineoff, cnt);
+    if constexpr (WQ == 1) {
+      for (int it = 0; it < passes; ++it) {
+        const int fi = it * STEP + mineoff;
+        store(fi, cnt, mine);
+        wave_lds_sync();
+        if (it + 1 < passes) load(fi + STEP, cnt);
+        attend(fi, cnt, mine);
+        wave_lds_sync();
+      }
+    } else {
+      store(mineoff, cnt, mine);
+      if (passes > 1) load(mineoff + STEP, cnt);
+      __syncthreads();
+      for (int it = 0; it < passes; ++it) {
+        const int fi = it * STEP + mineoff;
+        attend(fi, cnt, mine + (it & 1) * S::STAGE);
+        if (it + 1 < passes) store(fi + STEP, cnt, mine + ((it + 1) & 1) * S::STAGE);
+        if (it + 2 < passes) load(fi + 2 * STEP, cnt);
+        __syncthreads();
+      }
+    }
+  }
+
+  __syncthreads();                                      // the pool is free; s_bad is complete
+  if (s_bad[tg] != 0) add_nonfinite<D, F32>(a, x, b, h, q, s_bad[tg], m == -INFINITY ? 0.0f : m, c2, o);
+
+  // ---- join the WT groups through LDS, in group order; the rows leave in their memory order
+  l += other_half(l);
+  if (half == 0) { s_m[wave][lane] = m; s_l[wave][lane] = l; }
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int t = 0; t < WT; ++t) top = fmaxf(top, s_m[t * WQ + wq][lane & 31]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  const float scale = __builtin_amdgcn_exp2f((m - ref) * c2);
+  float* const wo = reinterpret_cast<float*>(pool) + wave * 32 * D;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int r = lane & 31, d4 = (32 * dt + 2 * i + 4 * half) / 4;
+      *reinterpret_cast<float4*>(wo + r * D + 4 * (d4 ^ (r & (D / 4 - 1)))) =
+          make_float4(o[dt][i] * scale, o[dt][i + 1] * scale, o[dt][i + 2] * scale, o[dt][i + 3] * scale);
+    }
+  __syncthreads();
+  for (int idx = tid; idx < WQ * 32 * (D / 4); idx += kTreeThreads) {
+    const int rr = idx / (D / 4), d4 = idx % (D / 4), w = rr / 32, r = rr % 32;
+    const int row = mt * WQ * 32 + rr;
+    if (row >= x.nq * a.G) continue;
+    float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+    for (int t = 0; t < WT; ++t) mm = fmaxf(mm, s_m[t * WQ + w][r]);
+    const float rm = mm == -INFINITY ? 0.0f : mm;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int t = 0; t < WT; ++t) {
+      ll += __builtin_amdgcn_exp2f((s_m[t * WQ + w][r] - rm) * c2) * s_l[t * WQ + w][r];
+      const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<float*>(pool) + ((t * WQ + w) * 32 + r) * D +
+                                                        4 * (d4 ^ (r & (D / 4 - 1))));
+      sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
+    }
+    if (p.nsplit == 1) {
+      const int i = row / a.G;
+      const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
+      store_row4(p.out, at * D + 4 * d4, sum, ll, a.io_bf16);
+      if (d4 == 0 && p.lse) p.lse[at] = ll != 0.0f ? rm * a.c + logf(ll) : -INFINITY;
+    } else {
+      const int64_t at = part_row(p, unit, split, row);
+      *reinterpret_cast<float4*>(p.part_o + at * D + 4 * d4) = sum;
+      if (d4 == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(mm * c2, ll);
+    }
+  }
+}
+
+template <int D, bool F32>
+hipError_t launch_tree_kernels(const TreeParams& p, int wq, int grid, hipStream_t st) {
+  const dim3 g(grid), t(kTreeThreads);
+  auto go = [&](auto parts) {
+    constexpr int P = decltype(parts)::value;
+    if (wq == 1) hipLaunchKernelGGL((tree_kernel<D, 1, F32, P>), g, t, 0, st, p);
+    else if (wq == 2) hipLaunchKernelGGL((tree_kernel<D, 2, F32, P>), g, t, 0, st, p);
+    else hipLaunchKernelGGL((tree_kernel<D, 4, F32, P>), g, t, 0, st, p);
+  };
+  if constexpr (F32) {
+    go(std::integral_constant<int, 1>());
+  } else {
+    if (p.a.io_bf16) go(std::integral_constant<int, 1>());
+    else go(std::integral_constant<int, 2>());
+  }
+  return hipGetLastError();
+}
+
+}  // namespace cobs
