@@ -38,6 +38,7 @@ struct WeightsParams {
   const float* lse;
   const float* prev;
   float* weights;
+  int passes;                   // passes of a workgroup (set by the launcher)
 };
 
 struct EvictParams {
