@@ -78,8 +78,8 @@ cobs_status_t cobs_attention_weights(const cobs_config_t* cfg, const void* q, co
                                      const int32_t* sel, const float* lse, const float* prev, float* weights,
                                      void* stream);
 
-/* Workspace bytes of cobs_evict (0 if none is needed or invalid); zero-filled
- * before its first use and left zeroed by every call.                            */
+/* Workspace bytes of cobs_evict (0 if none is needed, or cfg is invalid).  It needs
+ * no clearing.                                                                    */
 size_t cobs_evict_workspace_bytes(const cobs_config_t* cfg);
 
 /* The tokens a cache keeps.  For every (batch row, KV head) with T = seq_lens[b]
@@ -89,7 +89,8 @@ size_t cobs_evict_workspace_bytes(const cobs_config_t* cfg);
  *   weights:  device fp32 [B, Hkv, max_seq_len].
  *   1 <= keep <= max_seq_len; sinks, recent >= 0, sinks + recent <= keep.
  *   kept:     device int32 [B, Hkv, keep], written: positions, ascending, then -1.
- *   new_lens: optional device int32 [B], written: min(T, keep); not seq_lens itself.  */
+ *   new_lens: optional device int32 [B], written: min(T, keep); not seq_lens itself.
+ *   ws:       cobs_evict_workspace_bytes(cfg), 256-byte aligned; may be NULL if that is 0.  */
 cobs_status_t cobs_evict(const cobs_config_t* cfg, const float* weights, const int32_t* seq_lens, int32_t keep,
                          int32_t sinks, int32_t recent, int32_t* kept, int32_t* new_lens, void* ws, size_t ws_bytes,
                          void* stream);

@@ -69,8 +69,7 @@ def new_tree_workspace(cfg, num_queries, device):
 
 
 def new_evict_workspace(cfg, device):
-    """Zero-filled workspace of cobs_evict (the library requires zeros before first use)."""
-    return torch.zeros(max(evict_workspace_bytes(cfg), 256), dtype=torch.uint8, device=device)
+    return torch.empty(max(evict_workspace_bytes(cfg), 256), dtype=torch.uint8, device=device)
 
 
 def _queries(cfg, q, seq_lens, draft_lens, tree_mask, sel):

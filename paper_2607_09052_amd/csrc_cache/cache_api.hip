@@ -147,7 +147,7 @@ cobs_status_t cobs_attention_weights(const cobs_config_t* cfg, const void* q, co
 }
 
 size_t cobs_evict_workspace_bytes(const cobs_config_t* cfg) {
-  return 0;
+  return check_shape(cfg) == COBS_OK ? evict_workspace(cfg->batch, cfg->num_kv_heads, cfg->max_seq_len) : 0;
 }
 
 cobs_status_t cobs_evict(const cobs_config_t* cfg, const float* weights, const int32_t* seq_lens, int32_t keep,
@@ -158,7 +158,10 @@ cobs_status_t cobs_evict(const cobs_config_t* cfg, const float* weights, const i
   if (!weights || !seq_lens || !kept || new_lens == seq_lens) return COBS_ERR_INVALID_ARG;
   if (keep < 1 || keep > cfg->max_seq_len || sinks < 0 || recent < 0 || sinks > keep || recent > keep - sinks)
     return COBS_ERR_INVALID_ARG;
+  const size_t bytes = cobs_evict_workspace_bytes(cfg);
+  if (bytes > 0 && (!ws || ws_bytes < bytes || !aligned(ws, 256))) return COBS_ERR_WORKSPACE;
   EvictParams p = {};
+  p.hist = static_cast<uint16_t*>(ws);
   p.weights = weights;
   p.seq_lens = seq_lens;
   p.kept = kept;

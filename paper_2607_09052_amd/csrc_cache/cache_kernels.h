@@ -22,6 +22,14 @@ struct AttendParams {
   float c;
 };
 
+// Frames of the longest row that a call can attend to.
+inline int max_frames(const AttendParams& a) {
+  const int64_t dense = (a.tmax + kFrame - 1) / kFrame;
+  const int64_t sparse = (int64_t)a.s * ((1 << a.lsh) / kFrame) + ((int64_t)a.w + a.N) / kFrame + 2;
+  // (a selected block that the window start cuts has frames on both sides of it)
+  return (int)(a.sparse && sparse < dense + 4 ? sparse : dense + (a.sparse ? 4 : 0));
+}
+
 struct TreeParams {
   AttendParams a;
   void* out;
@@ -38,7 +46,7 @@ struct WeightsParams {
   const float* lse;
   const float* prev;
   float* weights;
-  int passes;                   // passes of a workgroup (set by the launcher)
+  int passes, lg;               // passes of a workgroup, log2 of G (set by the launcher)
 };
 
 struct EvictParams {
@@ -47,6 +55,8 @@ struct EvictParams {
   int32_t* kept;
   int32_t* new_lens;
   int B, hkv, tmax, keep, sinks, recent;
+  uint16_t* hist;               // digit histograms of the chunks (evict_workspace)
+  int chunks;                   // chunks of the longest row (set by the launcher)
 };
 
 struct CompactParams {
@@ -65,6 +75,7 @@ void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit);
 size_t tree_workspace(const AttendParams& a);
 hipError_t launch_tree(const TreeParams& p, hipStream_t st);
 hipError_t launch_weights(const WeightsParams& p, hipStream_t st);
+size_t evict_workspace(int B, int hkv, int tmax);
 hipError_t launch_evict(const EvictParams& p, hipStream_t st);
 hipError_t launch_compact(const CompactParams& p, hipStream_t st);
 

@@ -1,12 +1,32 @@
-// Which tokens a cache keeps (cobs_evict).  One workgroup per (batch row, KV
-// head): the (keep - sinks - recent)-th largest weight between the first and the
-// last tokens by four passes of a radix search over order-preserving 32-bit
-// keys, then one pass that writes the kept positions in order.
+// Which tokens a cache keeps (cobs_evict): per (batch row, KV head) the first and
+// the last tokens and the `need` largest weights of those between, in order.
+//
+// Radix search over order-preserving 32-bit keys in digits of 11, 11 and 10 bits
+// from the top: the histogram of the keys that share the digits found so far gives
+// the digit of the need-th largest key and how many keys above it are kept.  After
+// three digits the key itself is known; every larger one is kept, and the first
+// of the equal ones.
+//
+// A workgroup of 16 waves holds a chunk of up to 32768 keys in registers (wave w a
+// run of 64 KPT positions, so ranks come from ballots and one sum over waves).
+// Rows of one chunk are done by one launch.  Longer ones take four: each writes the
+// chunks' histograms of one digit (16-bit counts, 4 KB a chunk), and the next sums
+// them anew in every workgroup, which costs less than a wait between workgroups,
+// needs no atomics across them and no cleared memory.  The sums over the chunks
+// before a workgroup's own are its ranks in the last launch.
+//
+// Bound by HBM for many long rows (four reads of the weights, the later ones mostly
+// from the last-level cache), by the launches for few.
 #include "cache_device.h"
 
 namespace cobs {
 
-constexpr int kEvictThreads = 1024;
+constexpr int kEvictThreads = 1024, kEvictWaves = 16;
+constexpr int kEvictChunk = 32768;
+constexpr int kBins = 2048;                                  // of a digit; the last has 1024
+constexpr int kChunkHist = (2 * kBins + kBins / 2);          // 16-bit counts of a chunk: three digits
+__device__ __forceinline__ int digit_shift(int lv) { return lv == 0 ? 21 : (lv == 1 ? 10 : 0); }
+__device__ __forceinline__ int digit_bins(int lv) { return lv == 2 ? kBins / 2 : kBins; }
 
 // Larger weight, larger key; NaN with -inf.  -0 and 0 are one weight.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -14,76 +34,198 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return order_key(w + 0.0f);
 }
 
+// Set bits of a ballot below this lane.
+__device__ __forceinline__ int lanes_below(unsigned long long m) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
+// Sum over the wave, in every lane; all lanes active.
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_incl_scan(x), 63); }
+
+struct EvictShared {
+  int hist[kBins];
+  int wsum[kEvictWaves], wsum2[kEvictWaves];
+  int digit, left;
+};
+
+// Sum over the workgroup of x, and over the waves before this one (barriers inside).
+__device__ __forceinline__ int sum_before(int x, int* wsum, int wave, int lane, int& before) {
+  const int inc = wave_incl_scan(x);
+  if (lane == 63) wsum[wave] = inc;
+  __syncthreads();
+  int all = 0;
+  before = 0;
+#pragma unroll
+  for (int i = 0; i < kEvictWaves; ++i) {
+    const int v = wsum[i];
+    before += i < wave ? v : 0;
+    all += v;
+  }
+  __syncthreads();
+  return all;
+}
+
+// The digit that holds the need-th largest key, from this thread's counts of bins 2 tid and 2 tid + 1;
+// `need` becomes what is still needed of that bin.
+__device__ __forceinline__ int find_digit(int c0, int c1, int& need, EvictShared& s, int wave, int lane) {
+  const int v = c0 + c1, inc = wave_incl_scan(v);
+  int before;
+  const int all = sum_before(v, s.wsum, wave, lane, before);
+  const int after = all - before - inc;                      // keys in higher bins than this thread's
+  if (after < need && need <= after + v) {
+    const bool upper = need <= after + c1;
+    s.digit = 2 * threadIdx.x + (upper ? 1 : 0);
+    s.left = need - after - (upper ? 0 : c1);
+  }
+  __syncthreads();
+  const int d = s.digit;
+  need = s.left;
+  __syncthreads();
+  return d;
+}
+
+// LV 0..2: the launch of that digit; 3: the last launch; 4: all of it for rows of one chunk.
+template <int KPT, int LV>
 __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
-  __shared__ int hist[256];
-  __shared__ int wsum[2][16];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need;
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int T = clamp_len(p.seq_lens[b], p.tmax);
-  const float* w = p.weights + ((int64_t)b * p.hkv + h) * p.tmax;
-  int32_t* out = p.kept + ((int64_t)b * p.hkv + h) * p.keep;
-  if (p.new_lens && h == 0 && tid == 0) p.new_lens[b] = min(T, p.keep);
+  __shared__ EvictShared s;
+  const int chunk = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6);
+  const int T = clamp_len(p.seq_lens[b], p.tmax), unit = b * p.hkv + h;
+  const float* w = p.weights + (int64_t)unit * p.tmax;
+  int32_t* out = p.kept + (int64_t)unit * p.keep;
+  constexpr bool LAST = LV >= 3;
+  if (LAST && p.new_lens && chunk == 0 && h == 0 && tid == 0) p.new_lens[b] = min(T, p.keep);
   if (T <= p.keep) {
-    for (int j = tid; j < p.keep; j += kEvictThreads) out[j] = j < T ? j : -1;
+    if (LAST)
+      for (int j = chunk * kEvictThreads + tid; j < p.keep; j += gridDim.x * kEvictThreads) out[j] = j < T ? j : -1;
     return;
   }
-  const int lo = p.sinks, hi = T - p.recent;     // the tokens to choose from; T > keep >= sinks + recent
+  const int t_first = chunk * kEvictChunk;
+  if (t_first >= T) return;
+  const int nch = (T + kEvictChunk - 1) / kEvictChunk;
+  const int lo = p.sinks, hi = T - p.recent;                 // the tokens to choose from
+  int need = p.keep - p.sinks - p.recent;                    // fewer than those: T > keep
+  const bool choose = need > 0;
+
+  uint32_t key[KPT];
+  const int t0 = t_first + wave * 64 * KPT + lane;
+#pragma unroll
+  for (int i = 0; i < KPT; ++i) {
+    const int t = t0 + 64 * i;
+    key[i] = (t >= lo && t < hi) ? weight_key(w[t]) : 0;
+  }
+
+  // histogram of digit `lv` of the chunk's keys that share the digits above it, in s.hist
+  auto count = [&](int lv, uint32_t prefix) {
+    for (int i = tid; i < kBins; i += kEvictThreads) s.hist[i] = 0;
+    __syncthreads();
+    const int sh = digit_shift(lv), up = sh + (lv == 2 ? 10 : 11);
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const int t = t0 + 64 * i;
+      const bool in = t >= lo && t < hi && (lv == 0 || (key[i] >> up) == (prefix >> up));
+      if (in) atomicAdd(&s.hist[(key[i] >> sh) & (digit_bins(lv) - 1)], 1);
+    }
+    __syncthreads();
+  };
   uint32_t prefix = 0;
-  int need = p.keep - p.sinks - p.recent;        // < hi - lo
-  if (need > 0)
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kEvictThreads) hist[i] = 0;
-      __syncthreads();
-      for (int t = lo + tid; t < hi; t += kEvictThreads) {
-        const uint32_t k = weight_key(w[t]);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+  int above = 0, equal = 0;                                  // kept, and equal keys, of the chunks before
+  uint16_t* hists = p.hist + (int64_t)unit * p.chunks * kChunkHist;
+  if (choose) {
+#pragma unroll 1
+    for (int lv = 0; lv < (LV == 4 ? 3 : LV); ++lv) {
+      int c0 = 0, c1 = 0, b0 = 0, b1 = 0;                    // all chunks; those before this one
+      if (LV == 4) {
+        count(lv, prefix);
+        c0 = s.hist[2 * tid];
+        c1 = s.hist[2 * tid + 1];
+      } else if (tid < digit_bins(lv) / 2) {
+        for (int c = 0; c < nch; ++c) {
+          const uint32_t x = reinterpret_cast<const uint32_t*>(hists + c * kChunkHist + lv * kBins)[tid];
+          c0 += x & 0xffff;
+          c1 += x >> 16;
+          if (c < chunk) { b0 += x & 0xffff; b1 += x >> 16; }
+        }
       }
-      __syncthreads();
-      if (tid == 0) {
-        int left = need, d = 255;
-        while (hist[d] < left) left -= hist[d--];
-        s_prefix = prefix | ((uint32_t)d << shift);
-        s_need = left;
+      const int d = find_digit(c0, c1, need, s, wave, lane);
+      prefix |= (uint32_t)d << digit_shift(lv);
+      if (LV == 3) {
+        int before;
+        above += sum_before((2 * tid > d ? b0 : 0) + (2 * tid + 1 > d ? b1 : 0), s.wsum, wave, lane, before);
+        if (lv == 2) equal = sum_before((2 * tid == d ? b0 : 0) + (2 * tid + 1 == d ? b1 : 0), s.wsum, wave, lane, before);
       }
-      __syncthreads();
-      prefix = s_prefix;
-      need = s_need;
     }
-  // keep every key above `prefix` and the first `need` equal to it
-  int done = 0, equal = 0;                       // kept tokens and equal keys before this round
-  for (int t0 = 0; t0 < T; t0 += kEvictThreads) {
-    const int t = t0 + tid;
-    const bool mid = t >= lo && t < hi && p.keep > p.sinks + p.recent;
-    const uint32_t k = mid ? weight_key(w[t]) : 0;
-    const bool eq = mid && k == prefix;
-    const unsigned long long eqs = __ballot(eq), below = ((1ull << lane) - 1);
-    if (lane == 0) wsum[0][wave] = __popcll(eqs);
-    __syncthreads();
-    int rank = equal + __popcll(eqs & below), all = 0;
-    for (int i = 0; i < 16; ++i) {
-      if (i < wave) rank += wsum[0][i];
-      all += wsum[0][i];
+    if (LV < 3) {
+      count(LV, prefix);
+      if (tid < digit_bins(LV) / 2)
+        reinterpret_cast<uint32_t*>(hists + chunk * kChunkHist + LV * kBins)[tid] =
+            (uint32_t)s.hist[2 * tid] | ((uint32_t)s.hist[2 * tid + 1] << 16);
+      return;
     }
-    equal += all;
-    const bool take = t < T && (t < lo || t >= hi || (mid && (k > prefix || (eq && rank < need))));
-    const unsigned long long tk = __ballot(take);
-    if (lane == 0) wsum[1][wave] = __popcll(tk);
-    __syncthreads();
-    int at = done + __popcll(tk & below);
-    all = 0;
-    for (int i = 0; i < 16; ++i) {
-      if (i < wave) at += wsum[1][i];
-      all += wsum[1][i];
+  }
+  if constexpr (LAST) {
+    // Keep the ends, every key above `prefix` and the first `need` equal to it.  Bit i
+    // of a lane's masks is its key i; ranks inside a wave go by i, then by lane.
+    uint32_t take = 0, same = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const int t = t0 + 64 * i;
+      const bool mid = t >= lo && t < hi;
+      take |= (t < T && (!mid || (choose && key[i] > prefix)) ? 1u : 0u) << i;
+      same |= (choose && mid && key[i] == prefix ? 1u : 0u) << i;
     }
-    done += all;
-    if (take) out[at] = t;
-    __syncthreads();
+    const int mine = wave_total(__popc(same));
+    int eq;
+    sum_before(lane == 0 ? mine : 0, s.wsum, wave, lane, eq);
+    eq += equal;
+    if (mine > 0 && eq < need) {
+      if (eq + mine <= need) {
+        take |= same;
+      } else {                                   // the wave where they run out
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+          const unsigned long long eqs = __ballot((same >> i) & 1u);
+          if (((same >> i) & 1u) && eq + lanes_below(eqs) < need) take |= 1u << i;
+          eq += __popcll(eqs);
+        }
+      }
+    }
+    const int taken = wave_total(__popc(take));
+    int at;
+    sum_before(lane == 0 ? taken : 0, s.wsum, wave, lane, at);
+    // chunks before this one: their ends, keys above and kept equal ones
+    if (chunk > 0) at += min(lo, t_first) + max(0, t_first - hi) + above + min(equal, choose ? need : 0);
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const unsigned long long tk = __ballot((take >> i) & 1u);
+      if ((take >> i) & 1u) out[at + lanes_below(tk)] = t0 + 64 * i;
+      at += __popcll(tk);
+    }
   }
 }
 
-hipError_t launch_evict(const EvictParams& p, hipStream_t st) {
-  hipLaunchKernelGGL(evict_kernel, dim3(p.hkv, p.B), dim3(kEvictThreads), 0, st, p);
+static int evict_chunks(int tmax) { return (tmax + kEvictChunk - 1) / kEvictChunk; }
+
+size_t evict_workspace(int B, int hkv, int tmax) {
+  const int n = evict_chunks(tmax);
+  return n == 1 ? 0 : ((size_t)B * hkv * n * kChunkHist * sizeof(uint16_t) + 255) / 256 * 256;
+}
+
+hipError_t launch_evict(const EvictParams& q, hipStream_t st) {
+  EvictParams p = q;
+  p.chunks = evict_chunks(p.tmax);
+  const dim3 grid(p.chunks, p.hkv, p.B), t(kEvictThreads);
+  if (p.chunks == 1) {
+    // keys of a thread: as few as hold the longest row
+    if (p.tmax <= 4 * kEvictThreads) hipLaunchKernelGGL((evict_kernel<4, 4>), grid, t, 0, st, p);
+    else if (p.tmax <= 16 * kEvictThreads) hipLaunchKernelGGL((evict_kernel<16, 4>), grid, t, 0, st, p);
+    else hipLaunchKernelGGL((evict_kernel<32, 4>), grid, t, 0, st, p);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((evict_kernel<32, 0>), grid, t, 0, st, p);
+  hipLaunchKernelGGL((evict_kernel<32, 1>), grid, t, 0, st, p);
+  hipLaunchKernelGGL((evict_kernel<32, 2>), grid, t, 0, st, p);
+  hipLaunchKernelGGL((evict_kernel<32, 3>), grid, t, 0, st, p);
   return hipGetLastError();
 }
 

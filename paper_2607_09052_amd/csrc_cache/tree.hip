@@ -52,21 +52,23 @@ void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit) {
   *mtiles = (M + *wq * 32 - 1) / (*wq * 32);
   // frames of the longest row, and as many splits as give the chip's 256 CUs two
   // workgroups each, of at least 8 frames
-  const int64_t dense = (a.tmax + kFrame - 1) / kFrame;
-  const int64_t sparse = (int64_t)a.s * ((1 << a.lsh) / kFrame) + (a.w + a.N) / kFrame + 2;
-  const int64_t frames = a.sparse && sparse < dense ? sparse : dense;
+  const int64_t frames = max_frames(a);
   const int64_t tiles = (int64_t)a.B * a.hkv * *mtiles;
   int64_t n = (512 + tiles - 1) / tiles;
   n = n < frames / 8 ? n : frames / 8;
   *nsplit = (int)(n < 1 ? 1 : (n > 128 ? 128 : n));
 }
 
-// Upper bound over the attended sets (the plan of a sparse call has no more splits than the dense one).
+// Enough for both attended sets.
 size_t tree_workspace(const AttendParams& a) {
-  AttendParams x = a;
-  x.sparse = 0;
-  int wq, mtiles, nsplit;
-  tree_plan(x, &wq, &mtiles, &nsplit);
+  int wq, mtiles, nsplit = 1;
+  for (int sparse = 0; sparse < 2; ++sparse) {
+    AttendParams x = a;
+    x.sparse = sparse;
+    int n;
+    tree_plan(x, &wq, &mtiles, &n);
+    nsplit = n > nsplit ? n : nsplit;
+  }
   const size_t rows = (size_t)a.B * a.hkv * nsplit * a.N * a.G;
   const size_t ml = (rows * 2 * sizeof(float) + 255) / 256 * 256;
   return ml + (rows * a.d * sizeof(float) + 255) / 256 * 256;

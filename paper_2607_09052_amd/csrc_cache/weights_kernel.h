@@ -1,14 +1,16 @@
 // Attention weights that cached tokens receive (cobs_attention_weights), on the
 // matrix cores.
 //
-// The work goes by position, so that each weight is written once and no sum
-// depends on an order of arrival.  A wave owns frames of 32 positions (TF at a
-// time) whose keys it loads straight into the operand layout, a pass ahead; the
-// M = N G query rows of the KV head come from LDS, staged once a workgroup in
-// operand order (128 rows at a time where there are more).  S = Q K^T with tokens
-// as columns: a lane holds one token's scores against 16 rows of a tile, so the sum
-// over queries and heads of exp2(c2 s - log2(e) lse) is a sum within the lane and
-// one exchange between the halves of the wave.
+// The work goes by the frames that are attended to (Attended), each of them one
+// wave's, so that each weight is written once and no sum depends on an order of
+// arrival; in a sparse call a copy of the earlier weights goes before.  A wave
+// loads the keys of its frames (TF at a time) straight into the operand layout, a
+// pass ahead; the M = N G query rows of the KV head come from LDS in operand order, 64
+// rows a step: up to 128 rows stay there for the workgroup's whole work, more
+// rotate through two buffers, their loads a step ahead.  S = Q K^T with tokens as
+// columns: a lane holds one token's scores against 16 rows of a tile, so the sum over
+// queries and heads of exp2(c2 s - log2(e) lse) is a sum within the lane and one
+// exchange between the halves of the wave.
 //
 // Bound by HBM (each key once) up to M ~ 256, then by the exponentials: 24 cycles
 // of a SIMD per 64 scores beside 32 of the matrix core's (one bf16 part).
@@ -21,235 +23,266 @@ namespace cobs {
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kWeightsThreads = 256;
-constexpr int kWeightsTiles = 4;            // row tiles of 32 staged at a time
+constexpr int kStepTiles = 2;               // row tiles of 32 in a buffer
 
 template <int D, bool F32, int PARTS>
 struct WeightsShape {
   static constexpr int TF = F32 ? 1 : 2;                // frames of a wave's pass
   static constexpr int KS = F32 ? D / 8 : D / 16;       // 16-byte pieces of a lane per row
   static constexpr int TILE = KS * 1024 * PARTS;        // bytes of a staged row tile
-  static constexpr int MAXP = 8;                        // passes of a workgroup: 64 blocks of 32 at most
+  static constexpr int STEP = kStepTiles * TILE;
+  static constexpr int PER = kStepTiles * KS * 64 / kWeightsThreads;   // staged pieces of a thread
+  static constexpr int LPP = PARTS;                     // 16-byte loads of a piece
 };
 
 template <int D, bool F32, int PARTS>
 __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsParams p) {
   using S = WeightsShape<D, F32, PARTS>;
-  constexpr int TF = S::TF, KS = S::KS;
-  __shared__ __align__(16) char tiles[kWeightsTiles * S::TILE];
-  __shared__ __align__(16) float s_lse[kWeightsTiles * 32];          // log2 units; +inf: adds nothing
-  __shared__ __align__(16) unsigned long long s_bits[kWeightsTiles * 32];
-  __shared__ unsigned long long s_blocks;
+  constexpr int TF = S::TF, KS = S::KS, PER = S::PER;
+  constexpr int ES = F32 ? 4 : 2;
+  __shared__ __align__(16) char tiles[2 * S::STEP];
+  __shared__ __align__(16) float s_lse[2][kStepTiles * 32];          // log2 units; +inf: adds nothing
+  __shared__ __align__(16) unsigned long long s_bits[2][kStepTiles * 32];
+  __shared__ unsigned long long s_live[2];                           // rows that add something
   __shared__ int red[4];
   const AttendParams& a = p.a;
   const int h = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), half = lane >> 5;
-  const int T0 = blockIdx.x * (p.passes * 4 * TF * kFrame);
-  if (tid == 0) s_blocks = 0;
   const Attended x = attended<kWeightsThreads>(a, b, h, red);
-  if (T0 >= x.E) return;
+  const int nf = x.frames(), F0 = blockIdx.x * (p.passes * 4 * TF);
+  if (F0 >= nf) return;
   const int M = x.nq * a.G;
   const float c2 = a.c * 1.4426950408889634f;
-  // selected blocks within the workgroup's positions, one bit each
-  if (a.sparse) {
-    __syncthreads();
-    for (int i = tid; i < x.nsel; i += kWeightsThreads) {
-      const int at = x.sel[i] - (T0 >> a.lsh);
-      if (at >= 0 && at < 64) atomicOr(&s_blocks, 1ull << at);
-    }
-    __syncthreads();
-  }
-  // lane f: the wave's frame f (pass f / TF)
-  int my_lo = 0, my_hi = 0;
+
+  // lane f: the wave's frame f (pass f / TF): position, live tokens, first row
+  int my_a = 0, my_lo = 0, my_hi = 0;
   int64_t my_base = 0;
-  const int frames = p.passes * TF;
-  if (lane < frames) {
-    const int t0 = T0 + (((lane / TF) * 4 + wave) * TF + lane % TF) * kFrame;
-    int lo = t0;
-    if (a.sparse && !((s_blocks >> ((t0 >> a.lsh) - (T0 >> a.lsh))) & 1)) lo = max(t0, x.ws);
-    const int hi = min(t0 + kFrame, x.E);
-    if (lo < hi && M > 0) {
-      const int64_t base = kv_offset(a.kv, b, h, t0);
-      if (base >= 0) { my_base = base; my_lo = lo - t0; my_hi = hi - t0; }
+  if (lane < p.passes * TF) {
+    const int f = F0 + ((lane / TF) * 4 + wave) * TF + lane % TF;
+    if (f < nf) {
+      int lo, hi;
+      x.frame(f, my_a, lo, hi);
+      if (lo < hi) {
+        my_lo = lo - my_a;
+        my_hi = hi - my_a;
+        my_base = kv_offset(a.kv, b, h, my_a);
+      }
     }
   }
   const int64_t rs = a.kv.table ? a.kv.d : a.kv.st;
-  constexpr int ES = F32 ? 4 : 2;
   const int64_t my_row = (int64_t)(lane & 31) * rs * ES + half * 16;
+  const int64_t wrow = ((int64_t)b * a.hkv + h) * a.tmax;
 
+  auto base_of = [&](int at) {
+    const uint32_t l32 = __builtin_amdgcn_readlane((uint32_t)my_base, at);
+    const uint32_t h32 = __builtin_amdgcn_readlane((uint32_t)((uint64_t)my_base >> 32), at);
+    return (int64_t)(((uint64_t)h32 << 32) | l32);
+  };
   uint4 kn[TF][KS];                           // the next pass's keys
   auto load = [&](int ps) {
 #pragma unroll
     for (int f = 0; f < TF; ++f) {
       const int at = ps * TF + f;
-      const int hi = __builtin_amdgcn_readlane(my_hi, at);
-      if (hi <= __builtin_amdgcn_readlane(my_lo, at)) continue;
-      const uint32_t lo32 = __builtin_amdgcn_readlane((uint32_t)my_base, at);
-      const uint32_t hi32 = __builtin_amdgcn_readlane((uint32_t)((uint64_t)my_base >> 32), at);
-      const char* k = static_cast<const char*>(a.kv.k) + (int64_t)(((uint64_t)hi32 << 32) | lo32) * ES + my_row;
+      if (__builtin_amdgcn_readlane(my_hi, at) == 0) continue;
+      const int64_t base = base_of(at);
+      if (base < 0) continue;                 // a page out of range
+      const char* k = static_cast<const char*>(a.kv.k) + base * ES + my_row;
 #pragma unroll
       for (int s = 0; s < KS; ++s) kn[f][s] = *reinterpret_cast<const uint4*>(k + s * 32);
     }
   };
-  // rows of tile tl of the staged round: lane l of piece s holds row l % 32, 16 bytes at 2 s + l / 32
-  auto stage = [&](int first, int tiles_n) {
-    for (int it = tid; it < tiles_n * KS * 64; it += kWeightsThreads) {
-      const int tl = it / (KS * 64), s = it / 64 % KS, ln = it & 63;
-      const int r = first + tl * 32 + (ln & 31), i = r / a.G;
-      const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (r - i * a.G);
-      char* dst = tiles + tl * S::TILE + s * 1024 + ln * 16;
-      if constexpr (F32) {
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const int e = 8 * s + 4 * (ln >> 5);
-        if (r < M) {
-          v.x = load_elem(a.q, at * D + e, !a.io_bf16);
-          v.y = load_elem(a.q, at * D + e + 1, !a.io_bf16);
-          v.z = load_elem(a.q, at * D + e + 2, !a.io_bf16);
-          v.w = load_elem(a.q, at * D + e + 3, !a.io_bf16);
-        }
-        *reinterpret_cast<float4*>(dst) = v;
-      } else if constexpr (PARTS == 1) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (r < M) v = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + at * D + 16 * s + 8 * (ln >> 5));
-        *reinterpret_cast<uint4*>(dst) = v;
-      } else {
-        float v[8];
+
+  // ---- staging: lane l of piece s of a tile holds row l % 32, 16 bytes (fp32 queries
+  // over bf16 keys: 8 values) at 2 s + l / 32
+  uint4 qx[PER][S::LPP];
+  float qz = INFINITY;
+  unsigned long long qbits = 0;
+  auto fetch = [&](int step) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-        if (r < M) {
-          const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + at * D + 16 * s + 8 * (ln >> 5));
-          const float4 q0 = q[0], q1 = q[1];
-          v[0] = q0.x; v[1] = q0.y; v[2] = q0.z; v[3] = q0.w;
-          v[4] = q1.x; v[5] = q1.y; v[6] = q1.z; v[7] = q1.w;
+    for (int j = 0; j < PER; ++j) {
+      const int piece = wave + 4 * j, tl = piece / KS, s = piece % KS;
+      const int r = (step * kStepTiles + tl) * 32 + (lane & 31), i = r >> p.lg;
+      const int64_t at = (((int64_t)b * a.N + i) * a.hq + h * a.G + (r - (i << p.lg))) * D;
+      const char* q = static_cast<const char*>(a.q) +
+                      (at + (F32 ? 8 * s + 4 * half : 16 * s + 8 * half)) * (a.io_bf16 ? 2 : 4);
+#pragma unroll
+      for (int k = 0; k < S::LPP; ++k) qx[j][k] = make_uint4(0, 0, 0, 0);
+      if (r < M) {
+        if (F32 && a.io_bf16) {
+          const uint2 v = *reinterpret_cast<const uint2*>(q);
+          qx[j][0] = make_uint4(v.x << 16, v.x & 0xffff0000u, v.y << 16, v.y & 0xffff0000u);
+        } else {
+#pragma unroll
+          for (int k = 0; k < S::LPP; ++k) qx[j][k] = reinterpret_cast<const uint4*>(q)[k];
         }
+      }
+    }
+    if (wave == 0) {
+      const int r = step * kStepTiles * 32 + lane, i = r >> p.lg;
+      qz = INFINITY;
+      qbits = 0;
+      if (r < M) {
+        qz = p.lse[((int64_t)b * a.N + i) * a.hq + h * a.G + (r - (i << p.lg))];
+        if (a.mask) qbits = a.mask[(int64_t)b * a.N + i];
+      }
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int piece = wave + 4 * j, tl = piece / KS, s = piece % KS;
+      char* dst = tiles + buf * S::STEP + tl * S::TILE + s * 1024 + lane * 16;
+      if constexpr (PARTS == 1) {
+        *reinterpret_cast<uint4*>(dst) = qx[j][0];
+      } else {
+        const float v[8] = {__uint_as_float(qx[j][0].x), __uint_as_float(qx[j][0].y), __uint_as_float(qx[j][0].z),
+                            __uint_as_float(qx[j][0].w), __uint_as_float(qx[j][1].x), __uint_as_float(qx[j][1].y),
+                            __uint_as_float(qx[j][1].z), __uint_as_float(qx[j][1].w)};
         sbf16x8_t w[PARTS];
         split_bf16x8<PARTS>(v, w);
 #pragma unroll
         for (int k = 0; k < PARTS; ++k) *reinterpret_cast<sbf16x8_t*>(dst + k * KS * 1024) = w[k];
       }
     }
-    for (int r0 = tid; r0 < tiles_n * 32; r0 += kWeightsThreads) {
-      const int r = first + r0, i = r / a.G;
-      float z = INFINITY;
-      unsigned long long bits = 0;
-      if (r < M) {
-        const float v = p.lse[((int64_t)b * a.N + i) * a.hq + h * a.G + (r - i * a.G)];
-        z = v == -INFINITY ? INFINITY : v * 1.4426950408889634f;
-        if (a.mask) bits = a.mask[(int64_t)b * a.N + i];
-      }
-      s_lse[r0] = z;
-      s_bits[r0] = bits;
+    if (wave == 0) {
+      const float z = qz == -INFINITY ? INFINITY : qz * 1.4426950408889634f;
+      s_lse[buf][lane] = z;
+      s_bits[buf][lane] = qbits;
+      const unsigned long long live = __ballot(z != INFINITY);
+      if (lane == 0) s_live[buf] = live;
     }
   };
+  static_assert(kStepTiles * 32 == 64, "one wave holds a step's normalisers");
 
-  const int rounds = (M + kWeightsTiles * 32 - 1) / (kWeightsTiles * 32);
-  if (rounds > 0) load(0);
-  for (int ps = 0; ps < p.passes; ++ps) {
-    const int p0 = T0 + (ps * 4 * TF) * kFrame;
-    if (p0 >= x.E) break;                            // the same for all waves
+  const int steps = (M + kStepTiles * 32 - 1) / (kStepTiles * 32);
+  const int passes = min(p.passes, (nf - F0 + 4 * TF - 1) / (4 * TF));       // the same for all waves
+  const bool resident = steps <= 2;
+  if (steps > 0) {
+    fetch(0);
+    load(0);
+    put(0);
+    if (steps > 1) fetch(1);
+    if (steps == 2) put(1);
+    __syncthreads();
+  }
+  int n = 0;                                                                 // steps done
+  for (int ps = 0; ps < passes; ++ps) {
     uint4 kc[TF][KS];
 #pragma unroll
     for (int f = 0; f < TF; ++f)
 #pragma unroll
       for (int s = 0; s < KS; ++s) kc[f][s] = kn[f][s];
-    if (rounds > 0 && ps + 1 < p.passes) load(ps + 1);
+    // lane l of the pass: token l % 32 of frame l / 32 (fp32 caches: of the one frame, lower half)
+    const int mine = ps * TF + (TF == 2 ? half : 0), r32 = lane & 31;
+    const int fa = __shfl(my_a, mine, 64), flo = __shfl(my_lo, mine, 64), fhi = __shfl(my_hi, mine, 64);
+    const bool writes = (TF == 2 || half == 0) && r32 >= flo && r32 < fhi;
+    float prev = 0.0f;
+    if (writes && p.prev) prev = p.prev[wrow + fa + r32];
+    if (steps > 0 && ps + 1 < passes) load(ps + 1);
     float sum[TF];
-#pragma unroll
-    for (int f = 0; f < TF; ++f) sum[f] = 0.0f;
-    bool any = false;
-#pragma unroll
-    for (int f = 0; f < TF; ++f)
-      any |= __builtin_amdgcn_readlane(my_hi, ps * TF + f) > __builtin_amdgcn_readlane(my_lo, ps * TF + f);
-    for (int rd = 0; rd < rounds; ++rd) {
-      const int first = rd * kWeightsTiles * 32, tiles_n = min(kWeightsTiles, (M - first + 31) / 32);
-      if (rounds > 1 || ps == 0) {
-        __syncthreads();                             // the staged rows are free
-        stage(first, tiles_n);
-        __syncthreads();
-      }
-      if (!any) continue;
-      for (int tl = 0; tl < tiles_n; ++tl) {
-        const char* qt = tiles + tl * S::TILE;
-        f32x16_t sc[TF];
-#pragma unroll
-        for (int f = 0; f < TF; ++f)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sc[f][i] = 0.0f;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          if constexpr (F32) {
-            const float4 q = *reinterpret_cast<const float4*>(qt + s * 1024 + lane * 16);
-#pragma unroll
-            for (int f = 0; f < TF; ++f) {
-              sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.x, __uint_as_float(kc[f][s].x), sc[f], 0, 0, 0);
-              sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.y, __uint_as_float(kc[f][s].y), sc[f], 0, 0, 0);
-              sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.z, __uint_as_float(kc[f][s].z), sc[f], 0, 0, 0);
-              sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.w, __uint_as_float(kc[f][s].w), sc[f], 0, 0, 0);
-            }
-          } else {
-#pragma unroll
-            for (int k = PARTS - 1; k >= 0; --k) {
-              const sbf16x8_t q = *reinterpret_cast<const sbf16x8_t*>(qt + (k * KS + s) * 1024 + lane * 16);
-#pragma unroll
-              for (int f = 0; f < TF; ++f)
-                sc[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, __builtin_bit_cast(sbf16x8_t, kc[f][s]), sc[f], 0, 0, 0);
-            }
-          }
-        }
-        float z[16];                                 // rows 8 (i / 4) + 4 half + i % 4 of the tile
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(&s_lse[tl * 32 + 2 * i + 4 * half]);
-          z[i] = v.x; z[i + 1] = v.y; z[i + 2] = v.z; z[i + 3] = v.w;
-        }
-        bool live = false;                           // a tile that adds nothing adds no NaN either
-#pragma unroll
-        for (int i = 0; i < 16; ++i) live |= z[i] != INFINITY;
-        if (!__ballot(live)) continue;
-#pragma unroll
-        for (int f = 0; f < TF; ++f) {
-          const int t0 = p0 + (wave * TF + f) * kFrame;
-          if (t0 + kFrame <= x.C) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sum[f] += __builtin_amdgcn_exp2f(fmaf(sc[f][i], c2, -z[i]));
-          } else {
-            // drafted tokens: the rows that see them
-            const int j = t0 + (lane & 31) - x.C;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const unsigned long long bits = s_bits[tl * 32 + 8 * (i >> 2) + 4 * half + (i & 3)];
-              const bool see = (j < 0) | (((bits >> (j & 63)) & 1) != 0);
-              const float e = __builtin_amdgcn_exp2f(fmaf(sc[f][i], c2, -z[i]));
-              sum[f] += (see & (z[i] != INFINITY)) ? e : 0.0f;
-            }
-          }
-        }
-      }
-    }
+    bool good[TF], any = false;
 #pragma unroll
     for (int f = 0; f < TF; ++f) {
-      const int at = ps * TF + f, lo = __builtin_amdgcn_readlane(my_lo, at), hi = __builtin_amdgcn_readlane(my_hi, at);
-      const float total = sum[f] + other_half(sum[f]);
-      const int r = lane & 31, t = p0 + (wave * TF + f) * kFrame + r;
-      if (half == 0 && t < x.E) {
-        const int64_t w = ((int64_t)b * a.hkv + h) * a.tmax + t;
-        const bool in = r >= lo && r < hi;
-        if (in || p.prev != p.weights) p.weights[w] = (p.prev ? p.prev[w] : 0.0f) + (in ? total : 0.0f);
+      sum[f] = 0.0f;
+      good[f] = __builtin_amdgcn_readlane(my_hi, ps * TF + f) > 0 && base_of(ps * TF + f) >= 0;
+      any |= good[f];
+    }
+    for (int st = 0; st < steps; ++st, ++n) {
+      const int buf = resident ? st : (n & 1);
+      const bool more = !resident && (st + 1 < steps || ps + 1 < passes);
+      // (the first step's successor is already in registers)
+      if (any) {
+        const unsigned long long live = s_live[buf];
+#pragma unroll 1
+        for (int tl = 0; tl < kStepTiles; ++tl) {
+          if ((uint32_t)(live >> (32 * tl)) == 0) continue;  // adds nothing, NaN neither
+          const char* qt = tiles + buf * S::STEP + tl * S::TILE;
+          f32x16_t sc[TF];
+#pragma unroll
+          for (int f = 0; f < TF; ++f)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[f][i] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < KS; ++s) {
+            if constexpr (F32) {
+              const float4 q = *reinterpret_cast<const float4*>(qt + s * 1024 + lane * 16);
+#pragma unroll
+              for (int f = 0; f < TF; ++f) {
+                sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.x, __uint_as_float(kc[f][s].x), sc[f], 0, 0, 0);
+                sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.y, __uint_as_float(kc[f][s].y), sc[f], 0, 0, 0);
+                sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.z, __uint_as_float(kc[f][s].z), sc[f], 0, 0, 0);
+                sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.w, __uint_as_float(kc[f][s].w), sc[f], 0, 0, 0);
+              }
+            } else {
+#pragma unroll
+              for (int k = PARTS - 1; k >= 0; --k) {
+                const sbf16x8_t q = *reinterpret_cast<const sbf16x8_t*>(qt + (k * KS + s) * 1024 + lane * 16);
+#pragma unroll
+                for (int f = 0; f < TF; ++f)
+                  sc[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, __builtin_bit_cast(sbf16x8_t, kc[f][s]), sc[f], 0, 0, 0);
+              }
+            }
+          }
+          float z[16];                                 // rows 8 (i / 4) + 4 half + i % 4 of the tile
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(&s_lse[buf][tl * 32 + 2 * i + 4 * half]);
+            z[i] = v.x; z[i + 1] = v.y; z[i + 2] = v.z; z[i + 3] = v.w;
+          }
+#pragma unroll
+          for (int f = 0; f < TF; ++f) {
+            const int t0 = __builtin_amdgcn_readlane(my_a, ps * TF + f);
+            if (t0 + kFrame <= x.C) {
+              float even = 0.0f, odd = 0.0f;
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                even += __builtin_amdgcn_exp2f(fmaf(sc[f][i], c2, -z[i]));
+                odd += __builtin_amdgcn_exp2f(fmaf(sc[f][i + 1], c2, -z[i + 1]));
+              }
+              sum[f] += even + odd;
+            } else {
+              // drafted tokens: the rows that see them
+              const int j = t0 + r32 - x.C;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const unsigned long long bits = s_bits[buf][tl * 32 + 8 * (i >> 2) + 4 * half + (i & 3)];
+                const bool see = (j < 0) | (((bits >> (j & 63)) & 1) != 0);
+                const float e = __builtin_amdgcn_exp2f(fmaf(sc[f][i], c2, -z[i]));
+                sum[f] += (see & (z[i] != INFINITY)) ? e : 0.0f;
+              }
+            }
+          }
+        }
+      }
+      if (more) {
+        put((n + 1) & 1);
+        fetch((st + 2) % steps);
+        __syncthreads();
       }
     }
+    float total = 0.0f;
+#pragma unroll
+    for (int f = 0; f < TF; ++f) {
+      const float v = sum[f] + other_half(sum[f]);
+      if (TF == 1 || half == f) total = good[f] ? v : 0.0f;
+    }
+    if (writes) p.weights[wrow + fa + r32] = prev + total;
   }
 }
 
 template <int D, bool F32>
 hipError_t launch_weights_kernels(WeightsParams p, hipStream_t st) {
-  // as many passes of a workgroup (its staged queries serve them all) as leave
+  // as many passes of a workgroup (a wave's lanes hold its frames; 16 at most) as leave
   // the chip's 256 CUs two rounds of two workgroups
-  constexpr int TOK = 4 * (F32 ? 1 : 2) * kFrame;
-  const int64_t one = (int64_t)((p.a.tmax + TOK - 1) / TOK) * p.a.hkv * p.a.B;
+  constexpr int PASS = 4 * (F32 ? 1 : 2);
+  const int frames = max_frames(p.a);
+  const int64_t one = (int64_t)((frames + PASS - 1) / PASS) * p.a.hkv * p.a.B;
   int64_t passes = one / 1024;
   passes = passes < 1 ? 1 : (passes > 8 ? 8 : passes);
   p.passes = (int)passes;
-  const int64_t span = TOK * passes;
-  const dim3 grid((unsigned)((p.a.tmax + span - 1) / span), p.a.hkv, p.a.B), t(kWeightsThreads);
+  p.lg = p.a.G == 1 ? 0 : (p.a.G == 2 ? 1 : (p.a.G == 4 ? 2 : (p.a.G == 8 ? 3 : 4)));
+  const int span = PASS * p.passes;
+  const dim3 grid((frames + span - 1) / span, p.a.hkv, p.a.B), t(kWeightsThreads);
   if constexpr (F32) {
     hipLaunchKernelGGL((weights_kernel<D, true, 1>), grid, t, 0, st, p);
   } else {
