@@ -8,9 +8,12 @@
 // pass ahead; the M = N G query rows of the KV head come from LDS in operand order, 64
 // rows a step: up to 128 rows stay there for the workgroup's whole work, more
 // rotate through two buffers, their loads a step ahead.  S = Q K^T with tokens as
-// columns: a lane holds one token's scores against 16 rows of a tile, so the sum over
-// queries and heads of exp2(c2 s - log2(e) lse) is a sum within the lane and one
-// exchange between the halves of the wave.
+// columns: a lane holds one token's scores against 4 rows of a tile, so the sum over
+// queries and heads of exp2(c2 s - log2(e) lse) is a sum within the lane and, at the
+// end, over the four lanes of a token.  16 x 16 products, because a load of their
+// key operand covers 64 contiguous bytes of 16 keys; that of 32 x 32 products covers 32
+// bytes of 32 keys, whose lines did not stay in the vector cache between the eight
+// loads of a frame (4.5 TB/s at 4 rows of 32k tokens).
 //
 // Bound by HBM (each key once) up to M ~ 256, then by the exponentials: 24 cycles
 // of a SIMD per 64 scores beside 32 of the matrix core's (one bf16 part).
@@ -20,15 +23,16 @@
 
 namespace cobs {
 
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x4w_t __attribute__((ext_vector_type(4)));
 
 constexpr int kWeightsThreads = 256;
-constexpr int kStepTiles = 2;               // row tiles of 32 in a buffer
+constexpr int kStepTiles = 4;               // row tiles of 16 in a buffer
 
 template <int D, bool F32, int PARTS>
 struct WeightsShape {
   static constexpr int TF = F32 ? 1 : 2;                // frames of a wave's pass
-  static constexpr int KS = F32 ? D / 8 : D / 16;       // 16-byte pieces of a lane per row
+  static constexpr int TG = 2 * TF;                     // groups of 16 tokens
+  static constexpr int KS = F32 ? D / 16 : D / 32;      // 16-byte pieces of a lane per row
   static constexpr int TILE = KS * 1024 * PARTS;        // bytes of a staged row tile
   static constexpr int STEP = kStepTiles * TILE;
   static constexpr int PER = kStepTiles * KS * 64 / kWeightsThreads;   // staged pieces of a thread
@@ -38,16 +42,16 @@ struct WeightsShape {
 template <int D, bool F32, int PARTS>
 __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsParams p) {
   using S = WeightsShape<D, F32, PARTS>;
-  constexpr int TF = S::TF, KS = S::KS, PER = S::PER;
+  constexpr int TF = S::TF, TG = S::TG, KS = S::KS, PER = S::PER;
   constexpr int ES = F32 ? 4 : 2;
   __shared__ __align__(16) char tiles[2 * S::STEP];
-  __shared__ __align__(16) float s_lse[2][kStepTiles * 32];          // log2 units; +inf: adds nothing
-  __shared__ __align__(16) unsigned long long s_bits[2][kStepTiles * 32];
+  __shared__ __align__(16) float s_lse[2][kStepTiles * 16];          // log2 units; +inf: adds nothing
+  __shared__ __align__(16) unsigned long long s_bits[2][kStepTiles * 16];
   __shared__ unsigned long long s_live[2];                           // rows that add something
   __shared__ int red[4];
   const AttendParams& a = p.a;
   const int h = blockIdx.y, b = blockIdx.z;
-  const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), half = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), quad = lane >> 4;
   const Attended x = attended<kWeightsThreads>(a, b, h, red);
   const int nf = x.frames(), F0 = blockIdx.x * (p.passes * 4 * TF);
   if (F0 >= nf) return;
@@ -70,7 +74,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     }
   }
   const int64_t rs = a.kv.table ? a.kv.d : a.kv.st;
-  const int64_t my_row = (int64_t)(lane & 31) * rs * ES + half * 16;
+  const int64_t my_row = (int64_t)(lane & 15) * rs * ES + quad * 16;
   const int64_t wrow = ((int64_t)b * a.hkv + h) * a.tmax;
 
   auto base_of = [&](int at) {
@@ -78,7 +82,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     const uint32_t h32 = __builtin_amdgcn_readlane((uint32_t)((uint64_t)my_base >> 32), at);
     return (int64_t)(((uint64_t)h32 << 32) | l32);
   };
-  uint4 kn[TF][KS];                           // the next pass's keys
+  uint4 kn[TG][KS];                           // the next pass's keys
   auto load = [&](int ps) {
 #pragma unroll
     for (int f = 0; f < TF; ++f) {
@@ -88,12 +92,14 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
       if (base < 0) continue;                 // a page out of range
       const char* k = static_cast<const char*>(a.kv.k) + base * ES + my_row;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) kn[f][s] = *reinterpret_cast<const uint4*>(k + s * 32);
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kn[2 * f + g][s] = *reinterpret_cast<const uint4*>(k + 16 * g * rs * ES + s * 64);
     }
   };
 
-  // ---- staging: lane l of piece s of a tile holds row l % 32, 16 bytes (fp32 queries
-  // over bf16 keys: 8 values) at 2 s + l / 32
+  // ---- staging: lane l of piece s of a tile holds row l % 16, 16 bytes (fp32 queries
+  // over bf16 keys: 8 values) at 4 s + l / 16
   uint4 qx[PER][S::LPP];
   float qz = INFINITY;
   unsigned long long qbits = 0;
@@ -101,10 +107,10 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int piece = wave + 4 * j, tl = piece / KS, s = piece % KS;
-      const int r = (step * kStepTiles + tl) * 32 + (lane & 31), i = r >> p.lg;
+      const int r = (step * kStepTiles + tl) * 16 + (lane & 15), i = r >> p.lg;
       const int64_t at = (((int64_t)b * a.N + i) * a.hq + h * a.G + (r - (i << p.lg))) * D;
       const char* q = static_cast<const char*>(a.q) +
-                      (at + (F32 ? 8 * s + 4 * half : 16 * s + 8 * half)) * (a.io_bf16 ? 2 : 4);
+                      (at + (F32 ? 16 * s + 4 * quad : 32 * s + 8 * quad)) * (a.io_bf16 ? 2 : 4);
 #pragma unroll
       for (int k = 0; k < S::LPP; ++k) qx[j][k] = make_uint4(0, 0, 0, 0);
       if (r < M) {
@@ -118,7 +124,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
       }
     }
     if (wave == 0) {
-      const int r = step * kStepTiles * 32 + lane, i = r >> p.lg;
+      const int r = step * kStepTiles * 16 + lane, i = r >> p.lg;
       qz = INFINITY;
       qbits = 0;
       if (r < M) {
@@ -152,9 +158,9 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
       if (lane == 0) s_live[buf] = live;
     }
   };
-  static_assert(kStepTiles * 32 == 64, "one wave holds a step's normalisers");
+  static_assert(kStepTiles * 16 == 64, "one wave holds a step's normalisers");
 
-  const int steps = (M + kStepTiles * 32 - 1) / (kStepTiles * 32);
+  const int steps = (M + kStepTiles * 16 - 1) / (kStepTiles * 16);
   const int passes = min(p.passes, (nf - F0 + 4 * TF - 1) / (4 * TF));       // the same for all waves
   const bool resident = steps <= 2;
   if (steps > 0) {
@@ -167,23 +173,24 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   }
   int n = 0;                                                                 // steps done
   for (int ps = 0; ps < passes; ++ps) {
-    uint4 kc[TF][KS];
+    uint4 kc[TG][KS];
 #pragma unroll
-    for (int f = 0; f < TF; ++f)
+    for (int g = 0; g < TG; ++g)
 #pragma unroll
-      for (int s = 0; s < KS; ++s) kc[f][s] = kn[f][s];
-    // lane l of the pass: token l % 32 of frame l / 32 (fp32 caches: of the one frame, lower half)
-    const int mine = ps * TF + (TF == 2 ? half : 0), r32 = lane & 31;
+      for (int s = 0; s < KS; ++s) kc[g][s] = kn[g][s];
+    // lane l writes token l of the pass (fp32 caches: 32 tokens)
+    const int mine = ps * TF + (TF == 2 ? lane >> 5 : 0), r32 = lane & 31;
     const int fa = __shfl(my_a, mine, 64), flo = __shfl(my_lo, mine, 64), fhi = __shfl(my_hi, mine, 64);
-    const bool writes = (TF == 2 || half == 0) && r32 >= flo && r32 < fhi;
+    const bool writes = lane < 32 * TF && r32 >= flo && r32 < fhi;
     float prev = 0.0f;
     if (writes && p.prev) prev = p.prev[wrow + fa + r32];
     if (steps > 0 && ps + 1 < passes) load(ps + 1);
-    float sum[TF];
+    float sum[TG];
     bool good[TF], any = false;
 #pragma unroll
+    for (int g = 0; g < TG; ++g) sum[g] = 0.0f;
+#pragma unroll
     for (int f = 0; f < TF; ++f) {
-      sum[f] = 0.0f;
       good[f] = __builtin_amdgcn_readlane(my_hi, ps * TF + f) > 0 && base_of(ps * TF + f) >= 0;
       any |= good[f];
     }
@@ -193,62 +200,54 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
       // (the first step's successor is already in registers)
       if (any) {
         const unsigned long long live = s_live[buf];
-#pragma unroll 1
+#pragma unroll
         for (int tl = 0; tl < kStepTiles; ++tl) {
-          if ((uint32_t)(live >> (32 * tl)) == 0) continue;  // adds nothing, NaN neither
+          if (((uint32_t)(live >> (16 * tl)) & 0xffffu) == 0) continue;      // adds nothing, NaN neither
           const char* qt = tiles + buf * S::STEP + tl * S::TILE;
-          f32x16_t sc[TF];
+          f32x4w_t sc[TG];
 #pragma unroll
-          for (int f = 0; f < TF; ++f)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[f][i] = 0.0f;
+          for (int g = 0; g < TG; ++g) sc[g] = f32x4w_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int s = 0; s < KS; ++s) {
             if constexpr (F32) {
               const float4 q = *reinterpret_cast<const float4*>(qt + s * 1024 + lane * 16);
 #pragma unroll
-              for (int f = 0; f < TF; ++f) {
-                sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.x, __uint_as_float(kc[f][s].x), sc[f], 0, 0, 0);
-                sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.y, __uint_as_float(kc[f][s].y), sc[f], 0, 0, 0);
-                sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.z, __uint_as_float(kc[f][s].z), sc[f], 0, 0, 0);
-                sc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(q.w, __uint_as_float(kc[f][s].w), sc[f], 0, 0, 0);
+              for (int g = 0; g < TG; ++g) {
+                sc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(q.x, __uint_as_float(kc[g][s].x), sc[g], 0, 0, 0);
+                sc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(q.y, __uint_as_float(kc[g][s].y), sc[g], 0, 0, 0);
+                sc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(q.z, __uint_as_float(kc[g][s].z), sc[g], 0, 0, 0);
+                sc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(q.w, __uint_as_float(kc[g][s].w), sc[g], 0, 0, 0);
               }
             } else {
 #pragma unroll
               for (int k = PARTS - 1; k >= 0; --k) {
                 const sbf16x8_t q = *reinterpret_cast<const sbf16x8_t*>(qt + (k * KS + s) * 1024 + lane * 16);
 #pragma unroll
-                for (int f = 0; f < TF; ++f)
-                  sc[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, __builtin_bit_cast(sbf16x8_t, kc[f][s]), sc[f], 0, 0, 0);
+                for (int g = 0; g < TG; ++g)
+                  sc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, __builtin_bit_cast(sbf16x8_t, kc[g][s]), sc[g], 0, 0, 0);
               }
             }
           }
-          float z[16];                                 // rows 8 (i / 4) + 4 half + i % 4 of the tile
+          // rows 4 quad + i of the tile
+          const float4 zv = *reinterpret_cast<const float4*>(&s_lse[buf][tl * 16 + 4 * quad]);
+          const float z[4] = {zv.x, zv.y, zv.z, zv.w};
 #pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(&s_lse[buf][tl * 32 + 2 * i + 4 * half]);
-            z[i] = v.x; z[i + 1] = v.y; z[i + 2] = v.z; z[i + 3] = v.w;
-          }
-#pragma unroll
-          for (int f = 0; f < TF; ++f) {
-            const int t0 = __builtin_amdgcn_readlane(my_a, ps * TF + f);
+          for (int g = 0; g < TG; ++g) {
+            const int t0 = __builtin_amdgcn_readlane(my_a, ps * TF + g / 2);
             if (t0 + kFrame <= x.C) {
-              float even = 0.0f, odd = 0.0f;
+              float e[4];
 #pragma unroll
-              for (int i = 0; i < 16; i += 2) {
-                even += __builtin_amdgcn_exp2f(fmaf(sc[f][i], c2, -z[i]));
-                odd += __builtin_amdgcn_exp2f(fmaf(sc[f][i + 1], c2, -z[i + 1]));
-              }
-              sum[f] += even + odd;
+              for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g][i], c2, -z[i]));
+              sum[g] += (e[0] + e[1]) + (e[2] + e[3]);
             } else {
               // drafted tokens: the rows that see them
-              const int j = t0 + r32 - x.C;
+              const int j = t0 + 16 * (g % 2) + (lane & 15) - x.C;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const unsigned long long bits = s_bits[buf][tl * 32 + 8 * (i >> 2) + 4 * half + (i & 3)];
+              for (int i = 0; i < 4; ++i) {
+                const unsigned long long bits = s_bits[buf][tl * 16 + 4 * quad + i];
                 const bool see = (j < 0) | (((bits >> (j & 63)) & 1) != 0);
-                const float e = __builtin_amdgcn_exp2f(fmaf(sc[f][i], c2, -z[i]));
-                sum[f] += (see & (z[i] != INFINITY)) ? e : 0.0f;
+                const float e = __builtin_amdgcn_exp2f(fmaf(sc[g][i], c2, -z[i]));
+                sum[g] += (see & (z[i] != INFINITY)) ? e : 0.0f;
               }
             }
           }
@@ -262,9 +261,11 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     }
     float total = 0.0f;
 #pragma unroll
-    for (int f = 0; f < TF; ++f) {
-      const float v = sum[f] + other_half(sum[f]);
-      if (TF == 1 || half == f) total = good[f] ? v : 0.0f;
+    for (int g = 0; g < TG; ++g) {
+      float v = sum[g];
+      v += __shfl_xor(v, 16, 64);
+      v += other_half(v);
+      if (quad == g) total = good[g / 2] ? v : 0.0f;
     }
     if (writes) p.weights[wrow + fa + r32] = prev + total;
   }
