@@ -30,6 +30,23 @@ inline int max_frames(const AttendParams& a) {
   return (int)(a.sparse && sparse < dense + 4 ? sparse : dense + (a.sparse ? 4 : 0));
 }
 
+// Passes of a workgroup, at most `most`, when `passes` of each of `units` equal pieces of work are
+// split over at most `parts` workgroups a piece, on 512 slots (256 CUs, two workgroups each): the
+// split with the least time of its rounds, where a workgroup costs two passes besides its own
+// (measured: 3 to 5 us of dependent loads before the first product, 1.5 to 2.5 us a pass).
+inline int parts_of(int64_t passes, int64_t units, int most, int64_t parts) {
+  int64_t best = -1, cost = 0;
+  for (int64_t rounds = 1; rounds <= 64; ++rounds) {
+    int64_t n = 512 * rounds / units;
+    n = n < 1 ? 1 : (n < parts ? n : parts);
+    const int64_t per = (passes + n - 1) / n, r = (units * ((passes + per - 1) / per) + 511) / 512;
+    if (per > most) continue;
+    if (best < 0 || r * (per + 2) < cost) { best = per; cost = r * (per + 2); }
+    if (per == 1) break;
+  }
+  return (int)(best < 0 ? most : best);
+}
+
 struct TreeParams {
   AttendParams a;
   void* out;

@@ -186,25 +186,23 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     if (writes && p.prev) prev = p.prev[wrow + fa + r32];
     if (steps > 0 && ps + 1 < passes) load(ps + 1);
     float sum[TG];
-    bool good[TF], any = false;
+    bool good[TF], any = false, drafted = false;          // drafted: a frame reaches into the draft
 #pragma unroll
     for (int g = 0; g < TG; ++g) sum[g] = 0.0f;
 #pragma unroll
     for (int f = 0; f < TF; ++f) {
       good[f] = __builtin_amdgcn_readlane(my_hi, ps * TF + f) > 0 && base_of(ps * TF + f) >= 0;
       any |= good[f];
+      drafted |= __builtin_amdgcn_readlane(my_a, ps * TF + f) + __builtin_amdgcn_readlane(my_hi, ps * TF + f) > x.C;
     }
     for (int st = 0; st < steps; ++st, ++n) {
       const int buf = resident ? st : (n & 1);
       const bool more = !resident && (st + 1 < steps || ps + 1 < passes);
-      // (the first step's successor is already in registers)
-      if (any) {
-        const unsigned long long live = s_live[buf];
-#pragma unroll
-        for (int tl = 0; tl < kStepTiles; ++tl) {
-          if (((uint32_t)(live >> (16 * tl)) & 0xffffu) == 0) continue;      // adds nothing, NaN neither
+      // A step whose rows all add nothing is left out, so that it adds no NaN either (in a live one every token
+      // of the context is attended to by some row).
+      if (any && s_live[buf] != 0) {
+        auto scores = [&](int tl, f32x4w_t (&sc)[TG]) {
           const char* qt = tiles + buf * S::STEP + tl * S::TILE;
-          f32x4w_t sc[TG];
 #pragma unroll
           for (int g = 0; g < TG; ++g) sc[g] = f32x4w_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -228,20 +226,54 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
               }
             }
           }
-          // rows 4 quad + i of the tile
-          const float4 zv = *reinterpret_cast<const float4*>(&s_lse[buf][tl * 16 + 4 * quad]);
-          const float z[4] = {zv.x, zv.y, zv.z, zv.w};
+        };
+        // normalisers of rows 4 quad + i of a tile
+        auto normalisers = [&](int tl, float (&z)[4]) {
+          const float4 v = *reinterpret_cast<const float4*>(&s_lse[buf][tl * 16 + 4 * quad]);
+          z[0] = v.x; z[1] = v.y; z[2] = v.z; z[3] = v.w;
+        };
+        const int nt = min(kStepTiles, (M + 15) / 16 - st * kStepTiles);      // the step's tiles that hold rows
+        auto add = [&](const f32x4w_t (&sc)[TG], const float (&z)[4]) {
 #pragma unroll
           for (int g = 0; g < TG; ++g) {
-            const int t0 = __builtin_amdgcn_readlane(my_a, ps * TF + g / 2);
-            if (t0 + kFrame <= x.C) {
-              float e[4];
+            float e[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g][i], c2, -z[i]));
-              sum[g] += (e[0] + e[1]) + (e[2] + e[3]);
-            } else {
+            for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g][i], c2, -z[i]));
+            sum[g] += (e[0] + e[1]) + (e[2] + e[3]);
+          }
+        };
+        if (PARTS == 1 && !F32 && !drafted && nt == kStepTiles) {
+          // straight-line code: a tile's products among the exponentials of the tile before (two
+          // parts or fp32 keys leave no registers for it: the spilled values cost a wait a pass)
+          f32x4w_t sc[2][TG];
+          scores(0, sc[0]);
+#pragma unroll
+          for (int tl = 0; tl < kStepTiles; ++tl) {
+            float z[4];
+            normalisers(tl, z);
+            if (tl + 1 < kStepTiles) scores(tl + 1, sc[(tl + 1) & 1]);
+            add(sc[tl & 1], z);
+          }
+        } else if (!drafted) {
+#pragma unroll 1
+          for (int tl = 0; tl < nt; ++tl) {
+            f32x4w_t sc[TG];
+            float z[4];
+            scores(tl, sc);
+            normalisers(tl, z);
+            add(sc, z);
+          }
+        } else {
+#pragma unroll 1
+          for (int tl = 0; tl < nt; ++tl) {
+            f32x4w_t sc[TG];
+            scores(tl, sc);
+            float z[4];
+            normalisers(tl, z);
+#pragma unroll
+            for (int g = 0; g < TG; ++g) {
               // drafted tokens: the rows that see them
-              const int j = t0 + 16 * (g % 2) + (lane & 15) - x.C;
+              const int j = __builtin_amdgcn_readlane(my_a, ps * TF + g / 2) + 16 * (g % 2) + (lane & 15) - x.C;
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const unsigned long long bits = s_bits[buf][tl * 16 + 4 * quad + i];
@@ -273,14 +305,10 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
 
 template <int D, bool F32>
 hipError_t launch_weights_kernels(WeightsParams p, hipStream_t st) {
-  // as many passes of a workgroup (a wave's lanes hold its frames; 16 at most) as leave
-  // the chip's 256 CUs two rounds of two workgroups
-  constexpr int PASS = 4 * (F32 ? 1 : 2);
+  // a wave's lanes hold its frames: at most 64
+  constexpr int TF = F32 ? 1 : 2, PASS = 4 * TF;
   const int frames = max_frames(p.a);
-  const int64_t one = (int64_t)((frames + PASS - 1) / PASS) * p.a.hkv * p.a.B;
-  int64_t passes = one / 1024;
-  passes = passes < 1 ? 1 : (passes > 8 ? 8 : passes);
-  p.passes = (int)passes;
+  p.passes = parts_of((frames + PASS - 1) / PASS, (int64_t)p.a.hkv * p.a.B, 64 / TF, 1 << 30);
   p.lg = p.a.G == 1 ? 0 : (p.a.G == 2 ? 1 : (p.a.G == 4 ? 2 : (p.a.G == 8 ? 3 : 4)));
   const int span = PASS * p.passes;
   const dim3 grid((frames + span - 1) / span, p.a.hkv, p.a.B), t(kWeightsThreads);
