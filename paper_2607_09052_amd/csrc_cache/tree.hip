@@ -4,41 +4,67 @@
 
 namespace cobs {
 
-constexpr int kMergeThreads = 256;
+constexpr int kMergeThreads = 256, kMergeGroups = 4;
 
-// One thread per 4 outputs of a query row: the parts' weights 2^(m_k - max m) and
-// sums in split order.
+// One output row per kMergeGroups groups of D / 4 threads, 4 outputs a thread: group g
+// takes the splits g, g + 4, ... (their loads in flight together) with the
+// weights 2^(m_k - max m), and the groups' sums meet in LDS in group order.
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeParams p) {
-  constexpr int TPR = D / 4;
+  constexpr int TPR = D / 4, RPB = kMergeThreads / (TPR * kMergeGroups), U = 8;
+  __shared__ float4 s_sum[RPB][kMergeGroups][TPR];
+  __shared__ float s_total[RPB][kMergeGroups];
   const AttendParams& a = p.a;
   const int M = a.N * a.G;
-  const int64_t idx = (int64_t)blockIdx.x * (kMergeThreads / TPR) + threadIdx.x / TPR;
-  const int d4 = threadIdx.x % TPR;
-  if (idx >= (int64_t)p.units * M) return;
-  const int unit = (int)(idx / M), row = (int)(idx % M), b = unit / a.hkv, h = unit % a.hkv;
+  const int rb = threadIdx.x / (TPR * kMergeGroups), g = threadIdx.x / TPR % kMergeGroups, d4 = threadIdx.x % TPR;
+  const int64_t idx = (int64_t)blockIdx.x * RPB + rb;
+  const bool here = idx < (int64_t)p.units * M;
+  const int unit = here ? (int)(idx / M) : 0, row = here ? (int)(idx % M) : 0, b = unit / a.hkv, h = unit % a.hkv;
   const int i = row / a.G;
   const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
   const int C = clamp_len(a.seq_lens[b], a.tmax);
   const int nq = a.mask ? clamp_len(a.draft_lens[b], min(a.N, a.tmax - C)) : a.N;
-  float top = -INFINITY, total = 0.0f;
+  const int64_t first = (int64_t)unit * p.nsplit * M + row;
+  const int n = here && i < nq ? p.nsplit : 0;
+  // the splits' maxima: each thread of a group loads its share
+  float top = -INFINITY;
+  for (int k = d4; k < n; k += TPR) top = fmaxf(top, p.part_ml[2 * (first + (int64_t)k * M)]);
+#pragma unroll
+  for (int o = TPR / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float total = 0.0f;
   float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  if (i < nq) {
-    const int64_t first = (int64_t)unit * p.nsplit * M + row;
-    for (int k = 0; k < p.nsplit; ++k) top = fmaxf(top, p.part_ml[2 * (first + (int64_t)k * M)]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    for (int k = 0; k < p.nsplit; ++k) {
-      const int64_t r = first + (int64_t)k * M;
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * r);
-      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-      const float4 o = *reinterpret_cast<const float4*>(p.part_o + r * D + 4 * d4);
-      total += f * ml.y;
-      sum.x += f * o.x; sum.y += f * o.y; sum.z += f * o.z; sum.w += f * o.w;
+  for (int k0 = g; k0 < n; k0 += U * kMergeGroups) {
+    float2 ml[U];
+    float4 o[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * kMergeGroups;
+      const int64_t r = first + (int64_t)(k < n ? k : g) * M;
+      ml[u] = *reinterpret_cast<const float2*>(p.part_ml + 2 * r);
+      o[u] = *reinterpret_cast<const float4*>(p.part_o + r * D + 4 * d4);
     }
-    top = ref;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k0 + u * kMergeGroups < n) {
+        const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
+        total += f * ml[u].y;
+        sum.x += f * o[u].x; sum.y += f * o[u].y; sum.z += f * o[u].z; sum.w += f * o[u].w;
+      }
+    }
+  }
+  s_sum[rb][g][d4] = sum;
+  if (d4 == 0) s_total[rb][g] = total;
+  __syncthreads();
+  if (g != 0 || !here) return;
+#pragma unroll
+  for (int k = 1; k < kMergeGroups; ++k) {
+    const float4 o = s_sum[rb][k][d4];
+    sum.x += o.x; sum.y += o.y; sum.z += o.z; sum.w += o.w;
+    total += s_total[rb][k];
   }
   store_row4(p.out, at * D + 4 * d4, sum, total, a.io_bf16);
-  if (d4 == 0 && p.lse) p.lse[at] = total != 0.0f ? top * 0.6931471805599453f + logf(total) : -INFINITY;
+  if (d4 == 0 && p.lse) p.lse[at] = total != 0.0f ? ref * 0.6931471805599453f + logf(total) : -INFINITY;
 }
 
 hipError_t launch_tree_bf16_d64(const TreeParams& p, int wq, int grid, hipStream_t st);
@@ -50,13 +76,11 @@ void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit) {
   const int M = a.N * a.G;
   *wq = M <= 32 ? 1 : (M <= 64 ? 2 : 4);
   *mtiles = (M + *wq * 32 - 1) / (*wq * 32);
-  // frames of the longest row, and as many splits as give the chip's 256 CUs two
-  // workgroups each, of at least 8 frames
-  const int64_t frames = max_frames(a);
-  const int64_t tiles = (int64_t)a.B * a.hkv * *mtiles;
-  int64_t n = (512 + tiles - 1) / tiles;
-  n = n < frames / 8 ? n : frames / 8;
-  *nsplit = (int)(n < 1 ? 1 : (n > 128 ? 128 : n));
+  // the longest row's frames, by a pass of a workgroup's waves at a time
+  const int step = *wq == 1 ? 4 : (*wq == 2 || !a.kv_f32 ? 2 : 1);
+  const int64_t passes = (max_frames(a) + step - 1) / step;
+  const int64_t per = parts_of(passes, (int64_t)a.B * a.hkv * *mtiles, 1 << 30, 128);
+  *nsplit = (int)((passes + per - 1) / per);
 }
 
 // Enough for both attended sets.
@@ -89,7 +113,7 @@ hipError_t launch_tree(const TreeParams& q, hipStream_t st) {
   if (p.a.kv_f32) e = p.a.d == 64 ? launch_tree_f32_d64(p, wq, g, st) : launch_tree_f32_d128(p, wq, g, st);
   else e = p.a.d == 64 ? launch_tree_bf16_d64(p, wq, g, st) : launch_tree_bf16_d128(p, wq, g, st);
   if (e != hipSuccess || p.nsplit == 1) return e;
-  const int64_t rows_out = (int64_t)p.units * p.a.N * p.a.G, per = kMergeThreads / (p.a.d / 4);
+  const int64_t rows_out = (int64_t)p.units * p.a.N * p.a.G, per = kMergeThreads / (p.a.d / 4 * kMergeGroups);
   const dim3 mg((unsigned)((rows_out + per - 1) / per));
   if (p.a.d == 64) hipLaunchKernelGGL(tree_merge_kernel<64>, mg, dim3(kMergeThreads), 0, st, p);
   else hipLaunchKernelGGL(tree_merge_kernel<128>, mg, dim3(kMergeThreads), 0, st, p);

@@ -156,7 +156,7 @@ __device__ __forceinline__ void clear_padding(const TreeParams& p, int b, int h,
 }
 
 template <int D, int WQ, bool F32, int PARTS>
-__global__ __launch_bounds__(kTreeThreads, F32 ? 1 : 2) void tree_kernel(TreeParams p) {
+__global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D == 128) ? 1 : 2) void tree_kernel(TreeParams p) {
   using S = TreeShape<D, WQ, F32>;
   constexpr int WT = S::WT, CPR = S::CPR, LD = S::LD, NT = S::NT, FPI = S::FPI;
   constexpr int NDT = D / 32;
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 ? 1 : 2) void tree_kernel(TreePar
   if (p.nsplit == 1) clear_padding<D>(p, b, h, mt * WQ * 32, WQ * 32, x.nq);
   if (mt * WQ * 32 >= x.nq * a.G) return;                       // the tile's rows are all padding
   const QueryRow q = query_row(a, x, b, h, row0 + (lane & 31));
-  const float c2 = a.c * 1.4426950408889634f;
+  const float c2 = a.c * 1.4426950408889634f, slack = 8.0f / c2;
   if (tid < WT) s_bad[tid] = 0;
 
   // ---- the query rows as the B operand: column lane % 32, k = 8 half + j of every step
@@ -226,72 +226,97 @@ __global__ __launch_bounds__(kTreeThreads, F32 ? 1 : 2) void tree_kernel(TreePar
   const int nf = x.frames();
   const int per = ((nf + p.nsplit - 1) / p.nsplit + WT * FPI - 1) / (WT * FPI) * (WT * FPI);
   const int f_lo = min(split * per, nf), f_hi = min(f_lo + per, nf);
-  const int64_t rs = a.kv.table ? a.kv.d : a.kv.st;
-  const int64_t rsb = rs * S::ES;
+  const uint32_t rsb = (uint32_t)((a.kv.table ? a.kv.d : a.kv.st) * S::ES);     // 32 rows: below 2^32 bytes
   char* const mine = pool + tg * S::NBUF * S::STAGE;
 
-  uint4 kr[LD], vr[LD];
-  // pass `it` of this group: frames first + it WT FPI + tg FPI ..
-  auto load = [&](int fi0, int cnt) {
-#pragma unroll
-    for (int j = 0; j < LD; ++j) {
-      const int row = j * S::RPP + gt / CPR, fi = fi0 + (j * S::RPP) / kFrame;
-      const int fc = fi < cnt ? fi : 0;
-      const FrameEntry e = table[fc];
-      if (fi < cnt && e.hi > e.lo) {
-        const int64_t off = e.base * S::ES + (row % kFrame) * rsb + (gt % CPR) * 16;
-        kr[j] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.kv.k) + off);
-        vr[j] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.kv.v) + off);
-      }
-    }
+  // A frame's entry in scalar registers; one past the table's end is empty.
+  struct Frame {
+    int64_t base;
+    int a, lo, hi;
   };
-  auto store = [&](int fi0, int cnt, char* buf) {
-#pragma unroll
-    for (int j = 0; j < LD; ++j) {
-      const int row = j * S::RPP + gt / CPR, fi = fi0 + (j * S::RPP) / kFrame, c = gt % CPR;
-      uint4 k = kr[j], v = vr[j];
-      const FrameEntry e = table[fi < cnt ? fi : 0];
-      const int r = row % kFrame;
-      if (fi >= cnt || r < e.lo || r >= e.hi) {       // rows that take no part: whatever memory holds there
-        k = make_uint4(0, 0, 0, 0);
-        v = k;
-      } else if (e.a + r >= x.C) {
-        bool found;
-        v = finite_only<F32>(v, found);
-        if (found) atomicOr(&s_bad[tg], 1ull << (e.a + r - x.C));
-      }
-      *reinterpret_cast<uint4*>(buf + (row * CPR + k_chunk<CPR, F32>(row, c)) * 16) = k;
-      *reinterpret_cast<uint4*>(buf + S::TILE + (row * CPR + v_chunk<CPR, F32>(row, c)) * 16) = v;
+  auto entry = [&](int fi, int cnt) {
+    Frame f = {0, 0, 0, 0};
+    if (fi < cnt) {
+      const uint4 e = *reinterpret_cast<const uint4*>(&table[fi]);
+      const uint32_t b0 = wave_uniform32((int)e.x), b1 = wave_uniform32((int)e.y), w = wave_uniform32((int)e.w);
+      f.base = (int64_t)(((uint64_t)b1 << 32) | b0);
+      f.a = wave_uniform32((int)e.z);
+      f.lo = (int)(int16_t)(w & 0xffff);
+      f.hi = (int)(int16_t)(w >> 16);
     }
+    return f;
   };
-  auto attend = [&](int fi0, int cnt, const char* buf) {
+
+  // K and V of a pass's frames, 16 bytes a load: row gt / CPR + RPP j of the frame, chunk gt % CPR
+  constexpr int LDF = LD / FPI;
+  uint4 kr[FPI][LDF], vr[FPI][LDF];
+  const uint32_t voff = (uint32_t)(gt / CPR) * rsb + (uint32_t)(gt % CPR) * 16;
+  auto load = [&](const Frame (&f)[FPI]) {
 #pragma unroll
     for (int fr = 0; fr < FPI; ++fr) {
-      if (fi0 + fr >= cnt) break;
-      const FrameEntry e = table[fi0 + fr];
-      const int lo = wave_uniform32(e.lo), hi = wave_uniform32(e.hi), ea = wave_uniform32(e.a);
+      if (f[fr].hi <= f[fr].lo) continue;
+      const char* kb = static_cast<const char*>(a.kv.k) + f[fr].base * S::ES;
+      const char* vb = static_cast<const char*>(a.kv.v) + f[fr].base * S::ES;
+#pragma unroll
+      for (int j = 0; j < LDF; ++j) kr[fr][j] = *reinterpret_cast<const uint4*>(kb + (voff + (uint32_t)(j * S::RPP) * rsb));
+#pragma unroll
+      for (int j = 0; j < LDF; ++j) vr[fr][j] = *reinterpret_cast<const uint4*>(vb + (voff + (uint32_t)(j * S::RPP) * rsb));
+    }
+  };
+  auto store = [&](const Frame (&f)[FPI], char* buf) {
+#pragma unroll
+    for (int fr = 0; fr < FPI; ++fr) {
+      if (f[fr].hi <= f[fr].lo) continue;                    // not read either
+      const bool whole = f[fr].lo == 0 && f[fr].hi == kFrame && f[fr].a + kFrame <= x.C;
+#pragma unroll
+      for (int j = 0; j < LDF; ++j) {
+        const int r = gt / CPR + j * S::RPP, row = fr * kFrame + r, c = gt % CPR;
+        uint4 k = kr[fr][j], v = vr[fr][j];
+        if (!whole) {
+          if (r < f[fr].lo || r >= f[fr].hi) {               // rows that take no part: whatever memory holds there
+            k = make_uint4(0, 0, 0, 0);
+            v = k;
+          } else if (f[fr].a + r >= x.C) {
+            bool found;
+            v = finite_only<F32>(v, found);
+            if (found) atomicOr(&s_bad[tg], 1ull << (f[fr].a + r - x.C));
+          }
+        }
+        *reinterpret_cast<uint4*>(buf + (row * CPR + k_chunk<CPR, F32>(r, c)) * 16) = k;
+        *reinterpret_cast<uint4*>(buf + S::TILE + (row * CPR + v_chunk<CPR, F32>(r, c)) * 16) = v;
+      }
+    }
+  };
+  auto attend = [&](const Frame (&fs)[FPI], const char* buf) {
+#pragma unroll
+    for (int fr = 0; fr < FPI; ++fr) {
+      const int lo = fs[fr].lo, hi = fs[fr].hi, ea = fs[fr].a;
       if (hi <= lo) continue;
       // ---- S^T: 32 tokens x 32 query rows
-      const int kr0 = fr * kFrame + (lane & 31);
+      const int kr0 = lane & 31;
+      const char* kt = buf + fr * kFrame * CPR * 16;
       f32x16_t s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.0f;
       if constexpr (F32) {
 #pragma unroll
         for (int u = 0; u < D / 8; ++u) {
-          const float4 kk = *reinterpret_cast<const float4*>(buf + (kr0 * CPR + k_chunk<CPR, F32>(kr0, 2 * u + half)) * 16);
+          const float4 kk = *reinterpret_cast<const float4*>(kt + (kr0 * CPR + k_chunk<CPR, F32>(kr0, 2 * u + half)) * 16);
           s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.x, qf[4 * u], s, 0, 0, 0);
           s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.y, qf[4 * u + 1], s, 0, 0, 0);
           s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.z, qf[4 * u + 2], s, 0, 0, 0);
           s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.w, qf[4 * u + 3], s, 0, 0, 0);
         }
       } else {
+        sbf16x8_t kk[D / 16];
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+          kk[ks] = *reinterpret_cast<const sbf16x8_t*>(kt + (kr0 * CPR + k_chunk<CPR, F32>(kr0, 2 * ks + half)) * 16);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-          const sbf16x8_t kk =
-              *reinterpret_cast<const sbf16x8_t*>(buf + (kr0 * CPR + k_chunk<CPR, F32>(kr0, 2 * ks + half)) * 16);
 #pragma unroll
-          for (int k = PARTS - 1; k >= 0; --k) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qb[ks][k], s, 0, 0, 0);
+          for (int k = PARTS - 1; k >= 0; --k)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[ks], qb[ks][k], s, 0, 0, 0);
         }
       }
       if (lo > 0 || hi < kFrame || ea + hi > x.C) {
@@ -304,12 +329,14 @@ __global__ __launch_bounds__(kTreeThreads, F32 ? 1 : 2) void tree_kernel(TreePar
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = (vis >> (8 * (i >> 2) + (i & 3))) & 1u ? s[i] : -INFINITY;
       }
-      // ---- streaming softmax: lane l has row l % 32, the tokens of its half
+      // ---- streaming softmax: lane l has row l % 32, the tokens of its half.  The
+      // maximum is followed with a slack of 2^8 in the probabilities, so that few
+      // frames scale the outputs anew; probabilities and sums keep their precision.
       float top = s[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
       top = fmaxf(top, other_half(top));
-      if (__ballot(top > m)) {
+      if (__ballot(top > m + slack)) {
         const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
         const float alpha = __builtin_amdgcn_exp2f((m - ref) * c2);
         m = mn;
@@ -380,26 +407,38 @@ __global__ __launch_bounds__(kTreeThreads, F32 ? 1 : 2) void tree_kernel(TreePar
     __syncthreads();
     constexpr int STEP = WT * FPI;
     const int passes = (cnt + STEP - 1) / STEP, mineoff = tg * FPI;
-    load(mineoff, cnt);
+    auto frames_of = [&](int it, Frame (&f)[FPI]) {
+#pragma unroll
+      for (int fr = 0; fr < FPI; ++fr) f[fr] = entry(it * STEP + mineoff + fr, cnt);
+    };
+    Frame now[FPI], next[FPI];
+    frames_of(0, now);
+    load(now);
     if constexpr (WQ == 1) {
       for (int it = 0; it < passes; ++it) {
-        const int fi = it * STEP + mineoff;
-        store(fi, cnt, mine);
+        store(now, mine);
         wave_lds_sync();
-        if (it + 1 < passes) load(fi + STEP, cnt);
-        attend(fi, cnt, mine);
+        frames_of(it + 1, next);
+        load(next);
+        attend(now, mine);
         wave_lds_sync();
+#pragma unroll
+        for (int fr = 0; fr < FPI; ++fr) now[fr] = next[fr];
       }
     } else {
-      store(mineoff, cnt, mine);
-      if (passes > 1) load(mineoff + STEP, cnt);
+      store(now, mine);
+      frames_of(1, next);
+      load(next);
       __syncthreads();
       for (int it = 0; it < passes; ++it) {
-        const int fi = it * STEP + mineoff;
-        attend(fi, cnt, mine + (it & 1) * S::STAGE);
-        if (it + 1 < passes) store(fi + STEP, cnt, mine + ((it + 1) & 1) * S::STAGE);
-        if (it + 2 < passes) load(fi + 2 * STEP, cnt);
+        Frame after[FPI];
+        frames_of(it + 2, after);
+        attend(now, mine + (it & 1) * S::STAGE);
+        store(next, mine + ((it + 1) & 1) * S::STAGE);
+        load(after);
         __syncthreads();
+#pragma unroll
+        for (int fr = 0; fr < FPI; ++fr) { now[fr] = next[fr]; next[fr] = after[fr]; }
       }
     }
   }
