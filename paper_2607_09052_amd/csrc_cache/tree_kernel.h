@@ -18,11 +18,13 @@
 //
 // Frames travel HBM -> registers (a frame ahead) -> LDS, in 16-byte chunks that
 // are swizzled by row against bank conflicts:
-//   bf16 K  chunk c of row r at c ^ (r % 16): the A operand of 32x32x16 reads 16
-//           bytes of 32 rows;
-//   bf16 V  at c ^ 4 (r % 4) (64-element heads: c ^ 2 (r & 2)): the transposing read
-//           (ds_read_b64_tr_b16) takes 4 tokens by 16 columns per 16 lanes;
-//   fp32 K  at c ^ (r % 32); fp32 V by column, as stored.
+//   K       chunk c of row r at c (32 + 1) + r: the operand of a k-step is 32 rows of two
+//           chunks, consecutive lanes at consecutive addresses, and every step at a
+//           constant offset; the 33rd place keeps a row's writes on different banks;
+//   bf16 V  row-major, chunk c of row r at c ^ 4 (r % 4) (64-element heads: c ^ 2 (r & 2)):
+//           the transposing read (ds_read_b64_tr_b16) takes 4 tokens by 16 columns per
+//           16 lanes;
+//   fp32 V  by column, as stored.
 // fp32 products run on 32x32x2 fp32 operands.  bf16 products take an fp32 query
 // and its probabilities as two bf16 parts (the rest is below 2^-17 of them), since
 // the outputs are fp32; with bf16 outputs, whose rounding is 2^-8, one part.
@@ -52,8 +54,9 @@ struct TreeShape {
   static constexpr int FPI = (WQ == 4 && !F32) ? 2 : 1;   // frames of a group's pass
   static constexpr int ROWS = FPI * kFrame;
   static constexpr int NBUF = WQ == 1 ? 1 : 2;            // wave-private frames need no second buffer
-  static constexpr int TILE = ROWS * D * ES;              // bytes of a K or V tile
-  static constexpr int STAGE = 2 * TILE;
+  static constexpr int KSTEP = (kFrame + 1) * 16;         // bytes from a K chunk to the next
+  static constexpr int KF = CPR * KSTEP, VF = kFrame * D * ES;   // bytes of a frame's K and V tiles
+  static constexpr int STAGE = FPI * (KF + VF);
   static constexpr int POOL = WT * NBUF * STAGE;          // at least 4 waves' outputs, 32 x D fp32 each
   static_assert(POOL >= 4 * 32 * D * 4 || WQ == 2, "room for the waves' outputs");
   static constexpr int LDS = POOL > 4 * 32 * D * 4 ? POOL : 4 * 32 * D * 4;
@@ -69,10 +72,6 @@ struct FrameEntry {
   int16_t lo, hi;
 };
 
-template <int CPR, bool F32>
-__device__ __forceinline__ int k_chunk(int row, int c) {
-  return c ^ (row & (CPR < 32 ? CPR - 1 : 31));
-}
 template <int CPR, bool F32>
 __device__ __forceinline__ int v_chunk(int row, int c) {
   if constexpr (F32) return c;
@@ -160,6 +159,8 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
   using S = TreeShape<D, WQ, F32>;
   constexpr int WT = S::WT, CPR = S::CPR, LD = S::LD, NT = S::NT, FPI = S::FPI;
   constexpr int NDT = D / 32;
+  constexpr bool JOINT = FPI == 2 && PARTS == 1;          // a pass's frames at one maximum (two parts: too many registers)
+  constexpr int NF = JOINT ? 2 : 1;
   __shared__ __align__(16) char pool[S::LDS];
   __shared__ FrameEntry table[kTable];
   __shared__ float s_m[4][32], s_l[4][32];
@@ -266,11 +267,14 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
   auto store = [&](const Frame (&f)[FPI], char* buf) {
 #pragma unroll
     for (int fr = 0; fr < FPI; ++fr) {
-      if (f[fr].hi <= f[fr].lo) continue;                    // not read either
+      const bool empty = f[fr].hi <= f[fr].lo;
+      if (empty && !JOINT) continue;                         // not read either
       const bool whole = f[fr].lo == 0 && f[fr].hi == kFrame && f[fr].a + kFrame <= x.C;
+      char* const kb = buf + fr * (S::KF + S::VF) + (gt % CPR) * S::KSTEP + (gt / CPR) * 16;
+      char* const vb = buf + fr * (S::KF + S::VF) + S::KF;
 #pragma unroll
       for (int j = 0; j < LDF; ++j) {
-        const int r = gt / CPR + j * S::RPP, row = fr * kFrame + r, c = gt % CPR;
+        const int r = gt / CPR + j * S::RPP, c = gt % CPR;
         uint4 k = kr[fr][j], v = vr[fr][j];
         if (!whole) {
           if (r < f[fr].lo || r >= f[fr].hi) {               // rows that take no part: whatever memory holds there
@@ -282,78 +286,83 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
             if (found) atomicOr(&s_bad[tg], 1ull << (f[fr].a + r - x.C));
           }
         }
-        *reinterpret_cast<uint4*>(buf + (row * CPR + k_chunk<CPR, F32>(r, c)) * 16) = k;
-        *reinterpret_cast<uint4*>(buf + S::TILE + (row * CPR + v_chunk<CPR, F32>(r, c)) * 16) = v;
+        *reinterpret_cast<uint4*>(kb + j * S::RPP * 16) = k;
+        *reinterpret_cast<uint4*>(vb + (r * CPR + v_chunk<CPR, F32>(r, c)) * 16) = v;
       }
     }
   };
-  auto attend = [&](const Frame (&fs)[FPI], const char* buf) {
+  // NF frames of a pass from fr0 on, at one maximum
+  auto attend_frames = [&](const Frame (&fs)[FPI], int fr0, const char* buf) {
+    const char* const kt = buf + fr0 * (S::KF + S::VF) + half * S::KSTEP + (lane & 31) * 16;
+    // ---- S^T: 32 tokens x 32 query rows a frame
+    f32x16_t s[NF];
 #pragma unroll
-    for (int fr = 0; fr < FPI; ++fr) {
-      const int lo = fs[fr].lo, hi = fs[fr].hi, ea = fs[fr].a;
-      if (hi <= lo) continue;
-      // ---- S^T: 32 tokens x 32 query rows
-      const int kr0 = lane & 31;
-      const char* kt = buf + fr * kFrame * CPR * 16;
-      f32x16_t s;
+    for (int fr = 0; fr < NF; ++fr) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+      for (int i = 0; i < 16; ++i) s[fr][i] = 0.0f;
+      const char* const kf = kt + fr * (S::KF + S::VF);
       if constexpr (F32) {
 #pragma unroll
         for (int u = 0; u < D / 8; ++u) {
-          const float4 kk = *reinterpret_cast<const float4*>(kt + (kr0 * CPR + k_chunk<CPR, F32>(kr0, 2 * u + half)) * 16);
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.x, qf[4 * u], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.y, qf[4 * u + 1], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.z, qf[4 * u + 2], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.w, qf[4 * u + 3], s, 0, 0, 0);
+          const float4 kk = *reinterpret_cast<const float4*>(kf + 2 * u * S::KSTEP);
+          s[fr] = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.x, qf[4 * u], s[fr], 0, 0, 0);
+          s[fr] = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.y, qf[4 * u + 1], s[fr], 0, 0, 0);
+          s[fr] = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.z, qf[4 * u + 2], s[fr], 0, 0, 0);
+          s[fr] = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.w, qf[4 * u + 3], s[fr], 0, 0, 0);
         }
       } else {
         sbf16x8_t kk[D / 16];
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-          kk[ks] = *reinterpret_cast<const sbf16x8_t*>(kt + (kr0 * CPR + k_chunk<CPR, F32>(kr0, 2 * ks + half)) * 16);
+        for (int ks = 0; ks < D / 16; ++ks) kk[ks] = *reinterpret_cast<const sbf16x8_t*>(kf + 2 * ks * S::KSTEP);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
 #pragma unroll
           for (int k = PARTS - 1; k >= 0; --k)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[ks], qb[ks][k], s, 0, 0, 0);
+            s[fr] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[ks], qb[ks][k], s[fr], 0, 0, 0);
         }
       }
+    }
+#pragma unroll
+    for (int fr = 0; fr < NF; ++fr) {
+      const int lo = fs[fr0 + fr].lo, hi = fs[fr0 + fr].hi, ea = fs[fr0 + fr].a;
       if (lo > 0 || hi < kFrame || ea + hi > x.C) {
         // bit t of `vis`: whether the lane's query row sees token t of the frame
-        const int to_c = x.C - ea;                        // tokens of the context (32 and more: all)
+        const int to_c = x.C - ea;                          // tokens of the context (32 and more: all)
         uint32_t vis = to_c >= kFrame ? ~0u : (to_c > 0 ? (1u << to_c) - 1u : 0u);
         vis |= to_c >= kFrame ? 0u : (uint32_t)(to_c > 0 ? q.bits << to_c : q.bits >> -to_c);
         vis &= (hi < kFrame ? (1u << hi) - 1u : ~0u) & (~0u << lo);
         vis >>= 4 * half;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = (vis >> (8 * (i >> 2) + (i & 3))) & 1u ? s[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[fr][i] = (vis >> (8 * (i >> 2) + (i & 3))) & 1u ? s[fr][i] : -INFINITY;
       }
-      // ---- streaming softmax: lane l has row l % 32, the tokens of its half.  The
-      // maximum is followed with a slack of 2^8 in the probabilities, so that few
-      // frames scale the outputs anew; probabilities and sums keep their precision.
-      float top = s[0];
+    }
+    // ---- streaming softmax: lane l has row l % 32, the tokens of its half.  The
+    // maximum is followed with a slack of 2^8 in the probabilities, so that few
+    // frames scale the outputs anew; probabilities and sums keep their precision.
+    float top = s[0][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-      top = fmaxf(top, other_half(top));
-      if (__ballot(top > m + slack)) {
-        const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = __builtin_amdgcn_exp2f((m - ref) * c2);
-        m = mn;
-        l *= alpha;
+    for (int i = 1; i < 16 * NF; ++i) top = fmaxf(top, s[i / 16][i % 16]);
+    top = fmaxf(top, other_half(top));
+    if (__ballot(top > m + slack)) {
+      const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
+      const float alpha = __builtin_amdgcn_exp2f((m - ref) * c2);
+      m = mn;
+      l *= alpha;
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt)
+      for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
-      }
-      const float mc = m == -INFINITY ? 0.0f : m * c2;
+        for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+    }
+    const float mc = m == -INFINITY ? 0.0f : m * c2;
+#pragma unroll
+    for (int fr = 0; fr < NF; ++fr) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -mc));
-        l += s[i];
+        s[fr][i] = __builtin_amdgcn_exp2f(fmaf(s[fr][i], c2, -mc));
+        l += s[fr][i];
       }
       // ---- O^T += V^T P^T
-      const char* vt = buf + S::TILE + fr * kFrame * CPR * 16;
+      const char* const vt = buf + (fr0 + fr) * (S::KF + S::VF) + S::KF;
       if constexpr (F32) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -361,7 +370,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
             const float v = *reinterpret_cast<const float*>(vt + r * CPR * 16 + (32 * dt + (lane & 31)) * 4);
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], o[dt], 0, 0, 0);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[fr][i], o[dt], 0, 0, 0);
           }
         }
       } else {
@@ -370,11 +379,11 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
           sbf16x8_t pb[PARTS];
           float pv[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) pv[j] = s[8 * ks + j];
+          for (int j = 0; j < 8; ++j) pv[j] = s[fr][8 * ks + j];
           split_bf16x8<PARTS>(pv, pb);
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
-            // tokens 16 ks + 4 half + 0..3 and + 8 more, columns 32 dt + lane % 32
+            // tokens 16 ks + 4 half + 0..3 and 8 more on, columns 32 dt + lane % 32
             const int r = 16 * ks + 4 * half + ((lane & 15) >> 2), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
             const char* at = vt + (lane & 1) * 8;
             const s16x4_t v0 = tr_read(at + (r * CPR + v_chunk<CPR, F32>(r, c)) * 16);
@@ -388,6 +397,11 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
         }
       }
     }
+  };
+  auto attend = [&](const Frame (&fs)[FPI], const char* buf) {
+#pragma unroll
+    for (int fr = 0; fr < FPI; fr += NF)
+      if (JOINT || fs[fr].hi > fs[fr].lo) attend_frames(fs, fr, buf);
   };
 
   for (int t0 = f_lo; t0 < f_hi; t0 += kTable) {
