@@ -7,13 +7,12 @@ problem; its record fields are not read here.  The work runs on the current stre
 the tensors' GPU unless one is passed, also where another GPU is the current one.
 """
 
-import contextlib
 import ctypes
 
 import torch
 
 from . import cobs
-from .cobs import CobsError, _KV, _check, _kv, _need, _opt, _ptr, _same_gpu, _stream, _units, _ws
+from .cobs import CobsError, _KV, _check, _fits, _gpu, _kv, _kv_fits, _need, _opt, _ptr, _same_gpu, _stream, _units, _ws
 
 MAX_QUERIES = 64
 
@@ -45,15 +44,45 @@ def lib():
     return _lib
 
 
-def _on(t):
-    """Makes the tensor's GPU the current one for the launch, where it is not."""
+def _call(fn, t, *args):
+    """The C call on the GPU of tensor `t`, which becomes the current one for it where it is not."""
     if t.get_device() == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(t.device)
+        return _check(fn(*args))
+    with torch.cuda.device(t.device):
+        return _check(fn(*args))
 
 
 def _struct(cfg):
     return cfg.marshalled()[0]
+
+
+# As in ``cobs``, a call looks its arguments over in one pass; only when something does
+# not fit do the separate checks run, which name the fault, or find that there is none.
+
+def _cache_fits(cfg, dtype, dev, k, v, block_table, num_pages):
+    """The C view of a cache on GPU `dev`, or None if anything does not fit."""
+    if block_table is None:
+        return _kv_fits(cfg, dtype, dev, k, v)
+    shape = k.shape
+    if (not _fits(dev, (k, dtype, 0), (v, dtype, 0), (block_table, torch.int32, cfg.batch * cfg.num_blocks)) or
+            v.shape != shape or shape[1:] != (cfg.num_kv_heads, cfg.block_size, cfg.head_dim) or
+            type(num_pages) is not int or not 1 <= num_pages <= shape[0]):
+        return None
+    return _KV(k.data_ptr(), v.data_ptr(), 0, 0, 0, block_table.data_ptr(), num_pages)
+
+
+def _queries_fit(cfg, dtype, q, k, v, seq_lens, draft_lens, tree_mask, sel, block_table, num_pages, *more):
+    """The C view of the cache if every argument of a call with queries fits, else None; `more` as for _fits."""
+    if q is None or k is None or v is None or seq_lens is None or (draft_lens is None) != (tree_mask is None):
+        return None
+    dev, shape = _gpu(q), q.shape
+    if (len(shape) != 4 or shape[0] != cfg.batch or shape[2] != cfg.num_q_heads or shape[3] != cfg.head_dim or
+            q.dtype not in _IO or (tree_mask is not None and tree_mask.shape != shape[:2])):
+        return None
+    if not _fits(dev, (q, q.dtype, 0), (seq_lens, torch.int32, cfg.batch), (draft_lens, torch.int32, cfg.batch),
+                 (tree_mask, torch.int64, 0), (sel, torch.int32, _units(cfg) * cfg.budget), *more):
+        return None
+    return _cache_fits(cfg, dtype, dev, k, v, block_table, num_pages)
 
 
 def tree_workspace_bytes(cfg, num_queries):
@@ -97,51 +126,70 @@ def cobs_tree_decode(cfg, q, k, v, seq_lens, draft_lens, tree_mask, out, ws, sel
                      num_pages=0, stream=None):
     """Attention of the N queries q [B, N, Hq, d] of each row over the cached context (sel None: all of it; else
     the selected blocks and the window) and the drafted tokens that tree_mask [B, N] (bit j: token j) lets them see."""
-    n = _queries(cfg, q, seq_lens, draft_lens, tree_mask, sel)
-    _need("out", out, q.dtype, q.numel())
-    _opt("lse", lse, torch.float32, cfg.batch * n * cfg.num_q_heads)
-    kv = _kv(cfg, k, v, block_table, num_pages)
-    nws = _ws(ws)
-    _same_gpu(q=q, k=k, v=v, seq_lens=seq_lens, draft_lens=draft_lens, tree_mask=tree_mask, sel=sel, out=out, lse=lse,
-              ws=ws, block_table=block_table)
-    with _on(q):
-        _check(lib().cobs_tree_decode(ctypes.byref(_struct(cfg)), _ptr(q), _IO[q.dtype], n, ctypes.byref(kv),
-                                      _ptr(seq_lens), _ptr(draft_lens), _ptr(tree_mask), int(sel is not None),
-                                      _ptr(sel) or None, _ptr(out), _ptr(lse), _ptr(ws), nws, _stream(stream, q)))
+    c, _, kvt = cfg.marshalled()
+    kv = None
+    if out is not None and ws is not None:
+        nq = q.numel() if isinstance(q, torch.Tensor) else 0
+        kv = _queries_fit(cfg, kvt, q, k, v, seq_lens, draft_lens, tree_mask, sel, block_table, num_pages,
+                          (out, getattr(q, "dtype", None), nq), (lse, torch.float32, nq // cfg.head_dim),
+                          (ws, ws.dtype, 0))
+    if kv is None:
+        n = _queries(cfg, q, seq_lens, draft_lens, tree_mask, sel)
+        _need("out", out, q.dtype, q.numel())
+        _opt("lse", lse, torch.float32, cfg.batch * n * cfg.num_q_heads)
+        kv = _kv(cfg, k, v, block_table, num_pages)
+        _ws(ws)
+        _same_gpu(q=q, k=k, v=v, seq_lens=seq_lens, draft_lens=draft_lens, tree_mask=tree_mask, sel=sel, out=out,
+                  lse=lse, ws=ws, block_table=block_table)
+    _call(lib().cobs_tree_decode, q, ctypes.byref(c), q.data_ptr(), _IO[q.dtype], q.shape[1], ctypes.byref(kv),
+          seq_lens.data_ptr(), _ptr(draft_lens), _ptr(tree_mask), sel is not None, _ptr(sel) or None, out.data_ptr(),
+          _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream, q))
 
 
 def cobs_attention_weights(cfg, q, k, v, seq_lens, draft_lens, tree_mask, lse, weights, prev=None, sel=None,
                            block_table=None, num_pages=0, stream=None):
     """weights [B, Hkv, T_max] = prev + the attention weights that the queries give each cached token; lse
     [B, N, Hq] as the queries' attention returned it.  prev None: zeros; it may be `weights`."""
-    n = _queries(cfg, q, seq_lens, draft_lens, tree_mask, sel)
-    _need("lse", lse, torch.float32, cfg.batch * n * cfg.num_q_heads)
-    _need("weights", weights, torch.float32, _units(cfg) * cfg.max_seq_len)
-    _opt("prev", prev, torch.float32, _units(cfg) * cfg.max_seq_len)
-    kv = _kv(cfg, k, v, block_table, num_pages)
-    _same_gpu(q=q, k=k, v=v, seq_lens=seq_lens, draft_lens=draft_lens, tree_mask=tree_mask, sel=sel, lse=lse,
-              weights=weights, prev=prev, block_table=block_table)
-    with _on(q):
-        _check(lib().cobs_attention_weights(ctypes.byref(_struct(cfg)), _ptr(q), _IO[q.dtype], n, ctypes.byref(kv),
-                                            _ptr(seq_lens), _ptr(draft_lens), _ptr(tree_mask), int(sel is not None),
-                                            _ptr(sel) or None, _ptr(lse), _ptr(prev), _ptr(weights),
-                                            _stream(stream, q)))
+    c, _, kvt = cfg.marshalled()
+    kv, nw = None, _units(cfg) * cfg.max_seq_len
+    if lse is not None and weights is not None:
+        nq = q.numel() if isinstance(q, torch.Tensor) else 0
+        kv = _queries_fit(cfg, kvt, q, k, v, seq_lens, draft_lens, tree_mask, sel, block_table, num_pages,
+                          (lse, torch.float32, nq // cfg.head_dim), (weights, torch.float32, nw),
+                          (prev, torch.float32, nw))
+    if kv is None:
+        n = _queries(cfg, q, seq_lens, draft_lens, tree_mask, sel)
+        _need("lse", lse, torch.float32, cfg.batch * n * cfg.num_q_heads)
+        _need("weights", weights, torch.float32, nw)
+        _opt("prev", prev, torch.float32, nw)
+        kv = _kv(cfg, k, v, block_table, num_pages)
+        _same_gpu(q=q, k=k, v=v, seq_lens=seq_lens, draft_lens=draft_lens, tree_mask=tree_mask, sel=sel, lse=lse,
+                  weights=weights, prev=prev, block_table=block_table)
+    _call(lib().cobs_attention_weights, q, ctypes.byref(c), q.data_ptr(), _IO[q.dtype], q.shape[1], ctypes.byref(kv),
+          seq_lens.data_ptr(), _ptr(draft_lens), _ptr(tree_mask), sel is not None, _ptr(sel) or None, lse.data_ptr(),
+          _ptr(prev), weights.data_ptr(), _stream(stream, q))
 
 
 def cobs_evict(cfg, weights, seq_lens, kept, ws, sinks=0, recent=0, new_lens=None, stream=None):
     """The positions that each (batch row, KV head) keeps, kept [B, Hkv, keep]: the first `sinks`, the last
     `recent` and the heaviest between, ascending, then -1; new_lens [B]: how many."""
-    if kept is None or kept.dim() != 3 or tuple(kept.shape[:2]) != (cfg.batch, cfg.num_kv_heads):
-        raise CobsError(f"kept must have shape [{cfg.batch}, {cfg.num_kv_heads}, keep]")
-    _need("kept", kept, torch.int32, kept.numel())
-    _need("weights", weights, torch.float32, _units(cfg) * cfg.max_seq_len)
-    _need("seq_lens", seq_lens, torch.int32, cfg.batch)
-    _opt("new_lens", new_lens, torch.int32, cfg.batch)
-    nws = _ws(ws)
-    _same_gpu(weights=weights, seq_lens=seq_lens, kept=kept, new_lens=new_lens, ws=ws)
-    with _on(kept):
-        _check(lib().cobs_evict(ctypes.byref(_struct(cfg)), _ptr(weights), _ptr(seq_lens), int(kept.shape[2]), int(sinks),
-                                int(recent), _ptr(kept), _ptr(new_lens), _ptr(ws), nws, _stream(stream, kept)))
+    c = _struct(cfg)
+    nw = _units(cfg) * cfg.max_seq_len
+    if (kept is None or weights is None or seq_lens is None or ws is None or
+            kept.shape[:-1] != (cfg.batch, cfg.num_kv_heads) or
+            not _fits(_gpu(kept), (kept, torch.int32, 0), (weights, torch.float32, nw), (seq_lens, torch.int32, cfg.batch),
+                      (new_lens, torch.int32, cfg.batch), (ws, ws.dtype, 0))):
+        if kept is None or kept.dim() != 3 or tuple(kept.shape[:2]) != (cfg.batch, cfg.num_kv_heads):
+            raise CobsError(f"kept must have shape [{cfg.batch}, {cfg.num_kv_heads}, keep]")
+        _need("kept", kept, torch.int32, kept.numel())
+        _need("weights", weights, torch.float32, nw)
+        _need("seq_lens", seq_lens, torch.int32, cfg.batch)
+        _opt("new_lens", new_lens, torch.int32, cfg.batch)
+        _ws(ws)
+        _same_gpu(weights=weights, seq_lens=seq_lens, kept=kept, new_lens=new_lens, ws=ws)
+    _call(lib().cobs_evict, kept, ctypes.byref(c), weights.data_ptr(), seq_lens.data_ptr(), kept.shape[2], int(sinks),
+          int(recent), kept.data_ptr(), _ptr(new_lens), ws.data_ptr(), ws.numel() * ws.element_size(),
+          _stream(stream, kept))
 
 
 def _destination(cfg, k, k_out, v_out, table, num_pages):
@@ -173,6 +221,52 @@ def cobs_compact_cache(cfg, k, v, kept, seq_lens, first=None, k_out=None, v_out=
     """Move the tokens kept [B, Hkv, n] (or [B, n], one list for all heads) of each row to the positions
     first[b] + 0, 1, ...: in place, or into another cache k_out, v_out (contiguous or pages).  weights
     [B, Hkv, T_max] move to weights_out (in place: to themselves) and are 0 from the last moved token to seq_lens."""
+    c, _, kvt = cfg.marshalled()
+    kv = dst = None
+    capacity, nw = cfg.max_seq_len, _units(cfg) * cfg.max_seq_len
+    if kept is not None and k is not None and v is not None and seq_lens is not None and weights_out is not None:
+        # another cache, with weights, everything in place
+        dev, shape = _gpu(kept), kept.shape
+        if (k_out is not None and v_out is not None and weights is not None and len(weights_out.shape) == 3 and
+                (shape[:-1] == (cfg.batch, cfg.num_kv_heads) or shape[:-1] == (cfg.batch,)) and
+                _fits(dev, (kept, torch.int32, 0), (seq_lens, torch.int32, cfg.batch), (first, torch.int32, cfg.batch),
+                      (weights, torch.float32, nw), (weights_out, torch.float32, 0))):
+            view = _out_fits(cfg, kvt, dev, k_out, v_out, out_block_table, out_num_pages)
+            if view is not None and weights_out.shape == (cfg.batch, cfg.num_kv_heads, view[1]):
+                kv = _cache_fits(cfg, kvt, dev, k, v, block_table, num_pages)
+                if kv is not None:
+                    dst, capacity = view
+    if kv is None:
+        kv, dst, capacity, weights_out = _compaction(cfg, k, v, kept, seq_lens, first, k_out, v_out, weights,
+                                                     weights_out, block_table, num_pages, out_block_table, out_num_pages)
+    _call(lib().cobs_compact_cache, kept, ctypes.byref(c), ctypes.byref(kv), _ptr(kept) or None, kept.dim() == 3,
+          kept.shape[-1], seq_lens.data_ptr(), _ptr(first), None if dst is None else ctypes.byref(dst), capacity,
+          _ptr(weights), _ptr(weights_out), _stream(stream, kept))
+
+
+def _out_fits(cfg, dtype, dev, k_out, v_out, table, num_pages):
+    """C view and capacity of another cache that kept tokens move to, or None if anything does not fit."""
+    shape = k_out.shape
+    if (k_out.dtype is not dtype or v_out.dtype is not dtype or len(shape) != 4 or v_out.shape != shape or
+            k_out.get_device() != dev or v_out.get_device() != dev or shape[3] != cfg.head_dim):
+        return None
+    if table is None:
+        stride = k_out.stride()
+        if stride[3] != 1 or v_out.stride() != stride or shape[0] < cfg.batch or shape[1] < cfg.num_kv_heads:
+            return None
+        return (_KV(k_out.data_ptr(), v_out.data_ptr(), stride[0], stride[1], stride[2], None, 0),
+                shape[2] // cfg.block_size * cfg.block_size)
+    if (shape[1:] != (cfg.num_kv_heads, cfg.block_size, cfg.head_dim) or not k_out.is_contiguous() or
+            not v_out.is_contiguous() or type(num_pages) is not int or not 1 <= num_pages <= shape[0] or
+            len(table.shape) != 2 or table.shape[0] != cfg.batch or not _fits(dev, (table, torch.int32, 0))):
+        return None
+    return (_KV(k_out.data_ptr(), v_out.data_ptr(), 0, 0, 0, table.data_ptr(), num_pages),
+            table.shape[1] * cfg.block_size)
+
+
+def _compaction(cfg, k, v, kept, seq_lens, first, k_out, v_out, weights, weights_out, block_table, num_pages,
+                out_block_table, out_num_pages):
+    """The separate checks of cobs_compact_cache: C views, capacity and the weights' destination."""
     if kept is None or kept.dim() not in (2, 3) or tuple(kept.shape[:-1]) != (cfg.batch, cfg.num_kv_heads)[:kept.dim() - 1]:
         raise CobsError(f"kept must have shape [{cfg.batch}, {cfg.num_kv_heads}, n] or [{cfg.batch}, n]")
     _need("kept", kept, torch.int32, kept.numel())
@@ -200,8 +294,4 @@ def cobs_compact_cache(cfg, k, v, kept, seq_lens, first=None, k_out=None, v_out=
             raise CobsError(f"weights_out must have shape [{cfg.batch}, {cfg.num_kv_heads}, {capacity}]")
     _same_gpu(kept=kept, k=k, v=v, seq_lens=seq_lens, first=first, k_out=k_out, v_out=v_out, weights=weights,
               weights_out=weights_out, block_table=block_table, out_block_table=out_block_table)
-    with _on(kept):
-        _check(lib().cobs_compact_cache(ctypes.byref(_struct(cfg)), ctypes.byref(kv), _ptr(kept) or None,
-                                        int(kept.dim() == 3), int(kept.shape[-1]), _ptr(seq_lens), _ptr(first),
-                                        None if dst is None else ctypes.byref(dst), int(capacity), _ptr(weights),
-                                        _ptr(weights_out), _stream(stream, kept)))
+    return kv, dst, capacity, weights_out
