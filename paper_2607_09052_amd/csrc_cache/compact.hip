@@ -7,6 +7,8 @@
 // source of no entry from j1 on, so a workgroup that owns a column slice of one
 // (batch row, KV head) walks the entries in order, reads a batch of rows into
 // registers, waits, and writes it: no write meets a later read.
+#include <algorithm>
+
 #include "cache_device.h"
 
 namespace cobs {
@@ -27,37 +29,34 @@ __device__ __forceinline__ bool move_of(const CompactParams& p, int b, int h, in
   return from >= 0 && to >= 0;
 }
 
-// out of place: one thread per 16 bytes of a row, K and V both
+// Out of place: the first `row_blocks` workgroups of a (row, KV head) move rows, one
+// thread per 16 bytes of K and of V (and the row's weight); the others clear the
+// weights behind the last entry, 4 a thread.
 template <int CPR>
-__global__ __launch_bounds__(kCompactThreads) void compact_copy_kernel(CompactParams p) {
+__global__ __launch_bounds__(kCompactThreads) void compact_copy_kernel(CompactParams p, int row_blocks) {
   const int h = blockIdx.y, b = blockIdx.z, es = p.kv_f32 ? 4 : 2;
   const int T = clamp_len(p.seq_lens[b], p.tmax);
   const int first = p.first ? clamp_len(p.first[b], p.dst_max) : 0;
-  const int row = (blockIdx.x * kCompactThreads + threadIdx.x) / CPR, ch = threadIdx.x % CPR;
-  if (row < p.num_kept) {
-    int64_t from, to;
-    const bool ok = move_of(p, b, h, T, first, row, from, to);
-    if (ok) {
-      const uint4 k = reinterpret_cast<const uint4*>(static_cast<const char*>(p.src.k) + from * es)[ch];
-      const uint4 v = reinterpret_cast<const uint4*>(static_cast<const char*>(p.src.v) + from * es)[ch];
-      reinterpret_cast<uint4*>(static_cast<char*>(const_cast<void*>(p.dst.k)) + to * es)[ch] = k;
-      reinterpret_cast<uint4*>(static_cast<char*>(const_cast<void*>(p.dst.v)) + to * es)[ch] = v;
-    }
-  }
-}
-
-__global__ __launch_bounds__(kCompactThreads) void compact_weights_kernel(CompactParams p) {
-  const int h = blockIdx.y, b = blockIdx.z;
-  const int T = clamp_len(p.seq_lens[b], p.tmax);
-  const int first = p.first ? clamp_len(p.first[b], p.dst_max) : 0;
   const int64_t u = (int64_t)b * p.hkv + h;
-  const int end = p.num_kept > T - first ? p.num_kept : T - first;     // entries, then the tail to T
-  const int j = blockIdx.x * kCompactThreads + threadIdx.x;
-  if (j >= end || j >= p.dst_max - first) return;
+  if ((int)blockIdx.x >= row_blocks) {
+    const int j0 = p.num_kept + ((int)blockIdx.x - row_blocks) * 4 * kCompactThreads + threadIdx.x;
+    const int end = min(T, p.dst_max) - first;
+    for (int j = j0; j < min(end, j0 + 4 * kCompactThreads); j += kCompactThreads)
+      p.weights_out[u * p.dst_max + first + j] = 0.0f;
+    return;
+  }
+  const int row = ((int)blockIdx.x * kCompactThreads + threadIdx.x) / CPR, ch = threadIdx.x % CPR;
+  if (row >= p.num_kept) return;
   int64_t from, to;
-  float w = 0.0f;
-  if (j < p.num_kept && move_of(p, b, h, T, first, j, from, to)) w = p.weights[u * p.tmax + kept_at(p, b, h, j)];
-  p.weights_out[u * p.dst_max + first + j] = w;
+  const bool ok = move_of(p, b, h, T, first, row, from, to);
+  if (ok) {
+    const uint4 k = reinterpret_cast<const uint4*>(static_cast<const char*>(p.src.k) + from * es)[ch];
+    const uint4 v = reinterpret_cast<const uint4*>(static_cast<const char*>(p.src.v) + from * es)[ch];
+    reinterpret_cast<uint4*>(static_cast<char*>(const_cast<void*>(p.dst.k)) + to * es)[ch] = k;
+    reinterpret_cast<uint4*>(static_cast<char*>(const_cast<void*>(p.dst.v)) + to * es)[ch] = v;
+  }
+  if (p.weights && ch == 0 && row < p.dst_max - first)
+    p.weights_out[u * p.dst_max + first + row] = ok ? p.weights[u * p.tmax + kept_at(p, b, h, row)] : 0.0f;
 }
 
 // in place: blockIdx.x = slice of a row's 16-byte chunks (SC of them, K then V),
@@ -120,13 +119,11 @@ static hipError_t launch_compact_rows(const CompactParams& p, hipStream_t st) {
     return hipGetLastError();
   }
   const int rpw = kCompactThreads / CPR;
-  if (p.num_kept > 0)
-    hipLaunchKernelGGL(compact_copy_kernel<CPR>, dim3((p.num_kept + rpw - 1) / rpw, p.hkv, p.B), dim3(kCompactThreads),
-                       0, st, p);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.weights) return e;
-  const int64_t span = p.num_kept > p.tmax ? p.num_kept : p.tmax;
-  hipLaunchKernelGGL(compact_weights_kernel, dim3((unsigned)((span + kCompactThreads - 1) / kCompactThreads), p.hkv, p.B),
-                     dim3(kCompactThreads), 0, st, p);
+  const int rows = (p.num_kept + rpw - 1) / rpw;
+  const int left = p.weights ? std::min(p.tmax, p.dst_max) - p.num_kept : 0;       // weights to clear, at most
+  const int tail = left > 0 ? (left + 4 * kCompactThreads - 1) / (4 * kCompactThreads) : 0;
+  if (rows + tail == 0) return hipSuccess;
+  hipLaunchKernelGGL(compact_copy_kernel<CPR>, dim3(rows + tail, p.hkv, p.B), dim3(kCompactThreads), 0, st, p, rows);
   return hipGetLastError();
 }
 

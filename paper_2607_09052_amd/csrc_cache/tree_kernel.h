@@ -95,16 +95,18 @@ __device__ __forceinline__ uint4 finite_only(uint4 x, bool& found) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The rows of a wave: query row `r` of the M = N G of a (row, KV head), or none.
+// The rows of a wave: query row `r` of the M = N G of a (row, KV head), or none.  The
+// rows of padded queries are read like the others, which needs no row length (their
+// columns of the products are computed and left).
 struct QueryRow {
   int64_t at;        // (b N + i) Hq + head: row of q, out and lse
   bool live;
   uint64_t bits;     // drafted tokens that it sees
 };
-__device__ __forceinline__ QueryRow query_row(const AttendParams& a, const Attended& x, int b, int h, int r) {
+__device__ __forceinline__ QueryRow query_row(const AttendParams& a, int b, int h, int r) {
   QueryRow q;
   const int i = r / a.G, g = r - i * a.G;
-  q.live = i < x.nq;
+  q.live = i < a.N;
   q.at = ((int64_t)b * a.N + i) * a.hq + h * a.G + g;
   q.bits = (q.live && a.mask) ? a.mask[(int64_t)b * a.N + i] : 0;
   return q;
@@ -176,11 +178,8 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
   const int b = unit / a.hkv, h = unit % a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tg = wave / WQ, wq = wave % WQ, half = lane >> 5, gt = tid % NT;
-  const Attended x = attended<kTreeThreads>(a, b, h, red);
   const int row0 = (mt * WQ + wq) * 32;                         // the wave's query rows
-  if (p.nsplit == 1) clear_padding<D>(p, b, h, mt * WQ * 32, WQ * 32, x.nq);
-  if (mt * WQ * 32 >= x.nq * a.G) return;                       // the tile's rows are all padding
-  const QueryRow q = query_row(a, x, b, h, row0 + (lane & 31));
+  const QueryRow q = query_row(a, b, h, row0 + (lane & 31));
   const float c2 = a.c * 1.4426950408889634f, slack = 8.0f / c2;
   if (tid < WT) s_bad[tid] = 0;
 
@@ -216,6 +215,10 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
       }
     }
   }
+
+  const Attended x = attended<kTreeThreads>(a, b, h, red);
+  if (p.nsplit == 1) clear_padding<D>(p, b, h, mt * WQ * 32, WQ * 32, x.nq);
+  if (mt * WQ * 32 >= x.nq * a.G) return;                       // the tile's rows are all padding
 
   f32x16_t o[NDT];
 #pragma unroll
