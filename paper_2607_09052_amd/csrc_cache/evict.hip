@@ -8,7 +8,8 @@
 // of the equal ones.
 //
 // A workgroup of 16 waves holds a chunk of up to 32768 keys in registers (wave w a
-// run of 64 KPT positions, so ranks come from ballots and one sum over waves).
+// run of 64 KPT positions, so ranks come from ballots and one sum over waves).  (With 8
+// waves and chunks of 16384 the four launches of 64 rows of 131072 took 9 % longer.)
 // Rows of one chunk are done by one launch.  Longer ones take four: each writes the
 // chunks' histograms of one digit (16-bit counts, 4 KB a chunk), and the next sums
 // them anew in every workgroup, which costs less than a wait between workgroups,
@@ -42,9 +43,10 @@ __device__ __forceinline__ int lanes_below(unsigned long long m) {
 // Sum over the wave, in every lane; all lanes active.
 __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_incl_scan(x), 63); }
 
+static_assert(kBins == 2 * kEvictThreads, "two 16-bit counts a thread");
 struct EvictShared {
   int hist[kBins];
-  int wsum[kEvictWaves], wsum2[kEvictWaves];
+  int wsum[kEvictWaves];
   int digit, left;
 };
 
@@ -65,17 +67,27 @@ __device__ __forceinline__ int sum_before(int x, int* wsum, int wave, int lane, 
   return all;
 }
 
-// The digit that holds the need-th largest key, from this thread's counts of bins 2 tid and 2 tid + 1;
-// `need` becomes what is still needed of that bin.
-__device__ __forceinline__ int find_digit(int c0, int c1, int& need, EvictShared& s, int wave, int lane) {
-  const int v = c0 + c1, inc = wave_incl_scan(v);
+constexpr int kBpt = kBins / kEvictThreads;                  // bins of a thread: kBpt tid ..
+
+// The digit that holds the need-th largest key, from this thread's counts of its bins; `need` becomes
+// what is still needed of that digit's keys.
+__device__ __forceinline__ int find_digit(const int (&c)[kBpt], int& need, EvictShared& s, int wave, int lane) {
+  int v = 0;
+#pragma unroll
+  for (int i = 0; i < kBpt; ++i) v += c[i];
+  const int inc = wave_incl_scan(v);
   int before;
   const int all = sum_before(v, s.wsum, wave, lane, before);
-  const int after = all - before - inc;                      // keys in higher bins than this thread's
+  int after = all - before - inc;                            // keys in higher bins than this thread's
   if (after < need && need <= after + v) {
-    const bool upper = need <= after + c1;
-    s.digit = 2 * threadIdx.x + (upper ? 1 : 0);
-    s.left = need - after - (upper ? 0 : c1);
+#pragma unroll
+    for (int i = kBpt - 1; i >= 0; --i) {
+      if (after < need && need <= after + c[i]) {
+        s.digit = kBpt * threadIdx.x + i;
+        s.left = need - after;
+      }
+      after += c[i];
+    }
   }
   __syncthreads();
   const int d = s.digit;
@@ -107,13 +119,26 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
   int need = p.keep - p.sinks - p.recent;                    // fewer than those: T > keep
   const bool choose = need > 0;
 
+  // (the weights' bits until the digits are found, so that their loads run meanwhile)
   uint32_t key[KPT];
-  const int t0 = t_first + wave * 64 * KPT + lane;
+  const int t_wave = t_first + wave * 64 * KPT, t0 = t_wave + lane;
+  const bool inner = t_wave >= lo && t_wave + 64 * KPT <= hi;        // the wave's positions are all to choose from
+  if (inner) {
 #pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    const int t = t0 + 64 * i;
-    key[i] = (t >= lo && t < hi) ? weight_key(w[t]) : 0;
+    for (int i = 0; i < KPT; ++i) key[i] = __float_as_uint(w[t0 + 64 * i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const int t = t0 + 64 * i;
+      key[i] = (t >= lo && t < hi) ? __float_as_uint(w[t]) : 0;
+    }
   }
+
+  auto make_keys = [&] {
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) key[i] = weight_key(__uint_as_float(key[i]));
+  };
+  if (LV == 4) make_keys();
 
   // histogram of digit `lv` of the chunk's keys that share the digits above it, in s.hist
   auto count = [&](int lv, uint32_t prefix) {
@@ -123,7 +148,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
       const int t = t0 + 64 * i;
-      const bool in = t >= lo && t < hi && (lv == 0 || (key[i] >> up) == (prefix >> up));
+      const bool in = (inner || (t >= lo && t < hi)) && (lv == 0 || (key[i] >> up) == (prefix >> up));
       if (in) atomicAdd(&s.hist[(key[i] >> sh) & (digit_bins(lv) - 1)], 1);
     }
     __syncthreads();
@@ -134,32 +159,45 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
   if (choose) {
 #pragma unroll 1
     for (int lv = 0; lv < (LV == 4 ? 3 : LV); ++lv) {
-      int c0 = 0, c1 = 0, b0 = 0, b1 = 0;                    // all chunks; those before this one
+      int c[kBpt], before_c[kBpt];                           // all chunks; those before this one
+#pragma unroll
+      for (int i = 0; i < kBpt; ++i) c[i] = before_c[i] = 0;
       if (LV == 4) {
         count(lv, prefix);
-        c0 = s.hist[2 * tid];
-        c1 = s.hist[2 * tid + 1];
-      } else if (tid < digit_bins(lv) / 2) {
-        for (int c = 0; c < nch; ++c) {
-          const uint32_t x = reinterpret_cast<const uint32_t*>(hists + c * kChunkHist + lv * kBins)[tid];
-          c0 += x & 0xffff;
-          c1 += x >> 16;
-          if (c < chunk) { b0 += x & 0xffff; b1 += x >> 16; }
+#pragma unroll
+        for (int i = 0; i < kBpt; ++i) c[i] = s.hist[kBpt * tid + i];
+      } else if (kBpt * tid < digit_bins(lv)) {
+#pragma unroll 4
+        for (int k = 0; k < nch; ++k) {
+          const uint32_t x = reinterpret_cast<const uint32_t*>(hists + k * kChunkHist + lv * kBins)[tid];
+          const int n[kBpt] = {(int)(x & 0xffff), (int)(x >> 16)};
+#pragma unroll
+          for (int i = 0; i < kBpt; ++i) {
+            c[i] += n[i];
+            before_c[i] += k < chunk ? n[i] : 0;
+          }
         }
       }
-      const int d = find_digit(c0, c1, need, s, wave, lane);
+      const int d = find_digit(c, need, s, wave, lane);
       prefix |= (uint32_t)d << digit_shift(lv);
       if (LV == 3) {
-        int before;
-        above += sum_before((2 * tid > d ? b0 : 0) + (2 * tid + 1 > d ? b1 : 0), s.wsum, wave, lane, before);
-        if (lv == 2) equal = sum_before((2 * tid == d ? b0 : 0) + (2 * tid + 1 == d ? b1 : 0), s.wsum, wave, lane, before);
+        int over = 0, same = 0, before;
+#pragma unroll
+        for (int i = 0; i < kBpt; ++i) {
+          over += kBpt * tid + i > d ? before_c[i] : 0;
+          same += kBpt * tid + i == d ? before_c[i] : 0;
+        }
+        above += sum_before(over, s.wsum, wave, lane, before);
+        if (lv == 2) equal = sum_before(same, s.wsum, wave, lane, before);
       }
     }
+    if (LV < 4) make_keys();
     if (LV < 3) {
       count(LV, prefix);
-      if (tid < digit_bins(LV) / 2)
-        reinterpret_cast<uint32_t*>(hists + chunk * kChunkHist + LV * kBins)[tid] =
-            (uint32_t)s.hist[2 * tid] | ((uint32_t)s.hist[2 * tid + 1] << 16);
+      if (kBpt * tid < digit_bins(LV)) {
+        const int* n = s.hist + kBpt * tid;
+        reinterpret_cast<uint32_t*>(hists + chunk * kChunkHist + LV * kBins)[tid] = (uint32_t)n[0] | ((uint32_t)n[1] << 16);
+      }
       return;
     }
   }
@@ -167,12 +205,20 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
     // Keep the ends, every key above `prefix` and the first `need` equal to it.  Bit i
     // of a lane's masks is its key i; ranks inside a wave go by i, then by lane.
     uint32_t take = 0, same = 0;
+    if (inner && choose) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) {
+        take |= (key[i] > prefix ? 1u : 0u) << i;
+        same |= (key[i] == prefix ? 1u : 0u) << i;
+      }
+    } else {
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
       const int t = t0 + 64 * i;
       const bool mid = t >= lo && t < hi;
       take |= (t < T && (!mid || (choose && key[i] > prefix)) ? 1u : 0u) << i;
       same |= (choose && mid && key[i] == prefix ? 1u : 0u) << i;
+    }
     }
     const int mine = wave_total(__popc(same));
     int eq;
