@@ -30,22 +30,30 @@ inline int max_frames(const AttendParams& a) {
   return (int)(a.sparse && sparse < dense + 4 ? sparse : dense + (a.sparse ? 4 : 0));
 }
 
-// Passes of a workgroup, at most `most`, when `passes` of each of `units` equal pieces of work are
-// split over at most `parts` workgroups a piece, on 512 slots (256 CUs, two workgroups each): the
-// split with the least time of its rounds, where a workgroup costs two passes besides its own
-// (measured: 3 to 5 us of dependent loads before the first product, 1.5 to 2.5 us a pass).
-inline int parts_of(int64_t passes, int64_t units, int most, int64_t parts) {
-  int64_t best = -1, cost = 0;
+// Workgroups that each of `units` pieces of work of `passes` passes is split over: at most `parts`, with
+// at most `most` passes each, on 512 slots (256 CUs, two workgroups each).  The split with the least
+// time of its rounds: a pass takes `pass_us`, and a workgroup 4 us more (measured: 3 to 5 us of
+// dependent loads before the first product).  The longest parts go first, so that only with one round
+// does a part's last, uneven pass show.
+inline int parts_of(int64_t passes, int64_t units, double pass_us, int64_t most, int64_t parts) {
+  int64_t best = 0;
+  double cost = 0.0;
   for (int64_t rounds = 1; rounds <= 64; ++rounds) {
     int64_t n = 512 * rounds / units;
-    n = n < 1 ? 1 : (n < parts ? n : parts);
-    const int64_t per = (passes + n - 1) / n, r = (units * ((passes + per - 1) / per) + 511) / 512;
-    if (per > most) continue;
-    if (best < 0 || r * (per + 2) < cost) { best = per; cost = r * (per + 2); }
+    n = n < 1 ? 1 : n;
+    n = n < parts ? n : parts;
+    n = n < passes ? n : passes;
+    const int64_t per = (passes + n - 1) / n, r = (units * n + 511) / 512;
+    const double mean = (double)passes / (double)n;
+    const double c = r * (mean * pass_us + 4.0) + (r == 1 ? (per - mean) * pass_us : 0.0);
+    if (per <= most && (best == 0 || c < cost)) { best = n; cost = c; }
     if (per == 1) break;
   }
-  return (int)(best < 0 ? most : best);
+  return (int)(best > 0 ? best : (passes + most - 1) / most);
 }
+
+// Pass that part `i` of `n` begins with when `passes` are dealt evenly.
+__host__ __device__ inline int first_pass(int passes, int i, int n) { return (int)((int64_t)passes * i / n); }
 
 struct TreeParams {
   AttendParams a;
@@ -63,7 +71,7 @@ struct WeightsParams {
   const float* lse;
   const float* prev;
   float* weights;
-  int passes, lg;               // passes of a workgroup, log2 of G (set by the launcher)
+  int parts, lg;                // workgroups of a (row, KV head), log2 of G (set by the launcher)
 };
 
 struct EvictParams {

@@ -79,8 +79,7 @@ void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit) {
   // the longest row's frames, by a pass of a workgroup's waves at a time
   const int step = *wq == 1 ? 4 : (*wq == 2 || !a.kv_f32 ? 2 : 1);
   const int64_t passes = (max_frames(a) + step - 1) / step;
-  const int64_t per = parts_of(passes, (int64_t)a.B * a.hkv * *mtiles, 1 << 30, 128);
-  *nsplit = (int)((passes + per - 1) / per);
+  *nsplit = parts_of(passes, (int64_t)a.B * a.hkv * *mtiles, 2.0, 1 << 30, 128);
 }
 
 // Enough for both attended sets.

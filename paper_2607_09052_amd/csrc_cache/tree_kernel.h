@@ -174,7 +174,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
   // context, which read the same keys and values, follow each other on one.
   const int slot = blockIdx.x >> 3, group = (slot / p.mtiles) * 8 + (blockIdx.x & 7), mt = slot % p.mtiles;
   if (group >= p.units * p.nsplit) return;
-  const int unit = group / p.nsplit, split = group % p.nsplit;
+  const int unit = group % p.units, split = p.nsplit - 1 - group / p.units;    // the draft's frames and the longer parts first
   const int b = unit / a.hkv, h = unit % a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tg = wave / WQ, wq = wave % WQ, half = lane >> 5, gt = tid % NT;
@@ -227,9 +227,9 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
   float m = -INFINITY, l = 0.0f;          // raw units; the lane's own half of the sum
 
-  const int nf = x.frames();
-  const int per = ((nf + p.nsplit - 1) / p.nsplit + WT * FPI - 1) / (WT * FPI) * (WT * FPI);
-  const int f_lo = min(split * per, nf), f_hi = min(f_lo + per, nf);
+  constexpr int STEP = WT * FPI;                                // frames of a pass of the workgroup
+  const int nf = x.frames(), all = (nf + STEP - 1) / STEP;
+  const int f_lo = first_pass(all, split, p.nsplit) * STEP, f_hi = min(first_pass(all, split + 1, p.nsplit) * STEP, nf);
   const uint32_t rsb = (uint32_t)((a.kv.table ? a.kv.d : a.kv.st) * S::ES);     // 32 rows: below 2^32 bytes
   char* const mine = pool + tg * S::NBUF * S::STAGE;
 
@@ -422,7 +422,6 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
       table[tid] = e;
     }
     __syncthreads();
-    constexpr int STEP = WT * FPI;
     const int passes = (cnt + STEP - 1) / STEP, mineoff = tg * FPI;
     auto frames_of = [&](int it, Frame (&f)[FPI]) {
 #pragma unroll

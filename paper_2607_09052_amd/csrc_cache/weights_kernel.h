@@ -50,18 +50,21 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   __shared__ unsigned long long s_live[2];                           // rows that add something
   __shared__ int red[4];
   const AttendParams& a = p.a;
-  const int h = blockIdx.y, b = blockIdx.z;
+  const int h = blockIdx.x, b = blockIdx.y;
+  const int part = p.parts - 1 - (int)blockIdx.z;       // the draft's frames and the longer parts first
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), quad = lane >> 4;
   const Attended x = attended<kWeightsThreads>(a, b, h, red);
-  const int nf = x.frames(), F0 = blockIdx.x * (p.passes * 4 * TF);
-  if (F0 >= nf) return;
+  const int nf = x.frames(), all = (nf + 4 * TF - 1) / (4 * TF);
+  const int pass0 = first_pass(all, part, p.parts), passes = first_pass(all, part + 1, p.parts) - pass0;
+  if (passes == 0) return;
+  const int F0 = pass0 * 4 * TF;
   const int M = x.nq * a.G;
   const float c2 = a.c * 1.4426950408889634f;
 
   // lane f: the wave's frame f (pass f / TF): position, live tokens, first row
   int my_a = 0, my_lo = 0, my_hi = 0;
   int64_t my_base = 0;
-  if (lane < p.passes * TF) {
+  if (lane < passes * TF) {
     const int f = F0 + ((lane / TF) * 4 + wave) * TF + lane % TF;
     if (f < nf) {
       int lo, hi;
@@ -103,14 +106,18 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   uint4 qx[PER][S::LPP];
   float qz = INFINITY;
   unsigned long long qbits = 0;
+  // (16 rows further the query is 16 / G on and the head the same: a constant stride)
+  const int64_t qstride = (int64_t)(16 >> p.lg) * a.hq * D * (a.io_bf16 ? 2 : 4);
+  const int r16 = lane & 15;
+  const char* const qrow = static_cast<const char*>(a.q) +
+                           ((((int64_t)b * a.N + (r16 >> p.lg)) * a.hq + h * a.G + (r16 & (a.G - 1))) * D +
+                            (F32 ? 4 * quad : 8 * quad)) * (a.io_bf16 ? 2 : 4);
   auto fetch = [&](int step) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int piece = wave + 4 * j, tl = piece / KS, s = piece % KS;
-      const int r = (step * kStepTiles + tl) * 16 + (lane & 15), i = r >> p.lg;
-      const int64_t at = (((int64_t)b * a.N + i) * a.hq + h * a.G + (r - (i << p.lg))) * D;
-      const char* q = static_cast<const char*>(a.q) +
-                      (at + (F32 ? 16 * s + 4 * quad : 32 * s + 8 * quad)) * (a.io_bf16 ? 2 : 4);
+      const int r = (step * kStepTiles + tl) * 16 + r16;
+      const char* q = qrow + (step * kStepTiles + tl) * qstride + (F32 ? 16 : 32) * s * (a.io_bf16 ? 2 : 4);
 #pragma unroll
       for (int k = 0; k < S::LPP; ++k) qx[j][k] = make_uint4(0, 0, 0, 0);
       if (r < M) {
@@ -161,7 +168,6 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   static_assert(kStepTiles * 16 == 64, "one wave holds a step's normalisers");
 
   const int steps = (M + kStepTiles * 16 - 1) / (kStepTiles * 16);
-  const int passes = min(p.passes, (nf - F0 + 4 * TF - 1) / (4 * TF));       // the same for all waves
   const bool resident = steps <= 2;
   if (steps > 0) {
     fetch(0);
@@ -270,14 +276,16 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
             scores(tl, sc);
             float z[4];
             normalisers(tl, z);
+            // drafted tokens: the rows that see them
+            unsigned long long bits[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits[i] = s_bits[buf][tl * 16 + 4 * quad + i];
 #pragma unroll
             for (int g = 0; g < TG; ++g) {
-              // drafted tokens: the rows that see them
               const int j = __builtin_amdgcn_readlane(my_a, ps * TF + g / 2) + 16 * (g % 2) + (lane & 15) - x.C;
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const unsigned long long bits = s_bits[buf][tl * 16 + 4 * quad + i];
-                const bool see = (j < 0) | (((bits >> (j & 63)) & 1) != 0);
+                const bool see = (j < 0) | (((uint32_t)(bits[i] >> (j & 63)) & 1u) != 0);
                 const float e = __builtin_amdgcn_exp2f(fmaf(sc[g][i], c2, -z[i]));
                 sum[g] += (see & (z[i] != INFINITY)) ? e : 0.0f;
               }
@@ -308,10 +316,12 @@ hipError_t launch_weights_kernels(WeightsParams p, hipStream_t st) {
   // a wave's lanes hold its frames: at most 64
   constexpr int TF = F32 ? 1 : 2, PASS = 4 * TF;
   const int frames = max_frames(p.a);
-  p.passes = parts_of((frames + PASS - 1) / PASS, (int64_t)p.a.hkv * p.a.B, 64 / TF, 1 << 30);
+  // a pass of up to 64 rows is bound by HBM (2 us); each 64 of more rows take 3 us (fp32 keys: 6)
+  const int steps = (p.a.N * p.a.G + 63) / 64;
+  p.parts = parts_of((frames + PASS - 1) / PASS, (int64_t)p.a.hkv * p.a.B, steps == 1 ? 2.0 : steps * (F32 ? 6.0 : 3.0),
+                     64 / TF, 65535);
   p.lg = p.a.G == 1 ? 0 : (p.a.G == 2 ? 1 : (p.a.G == 4 ? 2 : (p.a.G == 8 ? 3 : 4)));
-  const int span = PASS * p.passes;
-  const dim3 grid((frames + span - 1) / span, p.a.hkv, p.a.B), t(kWeightsThreads);
+  const dim3 grid(p.a.hkv, p.a.B, p.parts), t(kWeightsThreads);
   if constexpr (F32) {
     hipLaunchKernelGGL((weights_kernel<D, true, 1>), grid, t, 0, st, p);
   } else {
