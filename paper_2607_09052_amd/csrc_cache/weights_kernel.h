@@ -3,7 +3,8 @@
 //
 // The work goes by the frames that are attended to (Attended), each of them one
 // wave's, so that each weight is written once and no sum depends on an order of
-// arrival; in a sparse call a copy of the earlier weights goes before.  A wave
+// arrival; in a sparse call more workgroups copy the earlier weights of the other
+// positions.  A wave
 // loads the keys of its frames (TF at a time) straight into the operand layout, a
 // pass ahead; the M = N G query rows of the KV head come from LDS in operand order, 64
 // rows a step: up to 128 rows stay there for the workgroup's whole work, more
@@ -39,6 +40,35 @@ struct WeightsShape {
   static constexpr int LPP = PARTS;                     // 16-byte loads of a piece
 };
 
+constexpr int kCopySpan = 2048;             // positions of a copying workgroup: 64 blocks at most
+
+// Earlier weights (or zeros) of the positions below the window start whose blocks are not selected.
+__device__ __forceinline__ void copy_weights(const WeightsParams& p, const Attended& x, int b, int h, int t0,
+                                             unsigned long long* s_blocks) {
+  const AttendParams& a = p.a;
+  if (threadIdx.x == 0) *s_blocks = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < x.nsel; i += kWeightsThreads) {
+    const int at = x.sel[i] - (t0 >> a.lsh);
+    if (at >= 0 && at < (kCopySpan >> a.lsh)) atomicOr(s_blocks, 1ull << at);
+  }
+  __syncthreads();
+  const unsigned long long blocks = *s_blocks;
+  const int64_t row = ((int64_t)b * a.hkv + h) * a.tmax;
+  const int end = min(t0 + kCopySpan, x.ws);
+  float v[kCopySpan / kWeightsThreads];
+#pragma unroll
+  for (int k = 0; k < kCopySpan / kWeightsThreads; ++k) {
+    const int t = t0 + k * kWeightsThreads + threadIdx.x;
+    v[k] = t < end && p.prev ? p.prev[row + t] : 0.0f;
+  }
+#pragma unroll
+  for (int k = 0; k < kCopySpan / kWeightsThreads; ++k) {
+    const int t = t0 + k * kWeightsThreads + threadIdx.x;
+    if (t < end && !((blocks >> ((t - t0) >> a.lsh)) & 1)) p.weights[row + t] = v[k];
+  }
+}
+
 template <int D, bool F32, int PARTS>
 __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsParams p) {
   using S = WeightsShape<D, F32, PARTS>;
@@ -54,6 +84,10 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   const int part = p.parts - 1 - (int)blockIdx.z;       // the draft's frames and the longer parts first
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), quad = lane >> 4;
   const Attended x = attended<kWeightsThreads>(a, b, h, red);
+  if (part < 0) {
+    copy_weights(p, x, b, h, (-1 - part) * kCopySpan, &s_live[0]);
+    return;
+  }
   const int nf = x.frames(), all = (nf + 4 * TF - 1) / (4 * TF);
   const int pass0 = first_pass(all, part, p.parts), passes = first_pass(all, part + 1, p.parts) - pass0;
   if (passes == 0) return;
@@ -319,9 +353,11 @@ hipError_t launch_weights_kernels(WeightsParams p, hipStream_t st) {
   // a pass of up to 64 rows is bound by HBM (2 us); each 64 of more rows take 3 us (fp32 keys: 6)
   const int steps = (p.a.N * p.a.G + 63) / 64;
   p.parts = parts_of((frames + PASS - 1) / PASS, (int64_t)p.a.hkv * p.a.B, steps == 1 ? 2.0 : steps * (F32 ? 6.0 : 3.0),
-                     64 / TF, 65535);
+                     64 / TF, 32768);
   p.lg = p.a.G == 1 ? 0 : (p.a.G == 2 ? 1 : (p.a.G == 4 ? 2 : (p.a.G == 8 ? 3 : 4)));
-  const dim3 grid(p.a.hkv, p.a.B, p.parts), t(kWeightsThreads);
+  // a sparse call's copies of the other positions, in place not needed, follow as more parts
+  const int copies = p.a.sparse && p.prev != p.weights ? (p.a.tmax + kCopySpan - 1) / kCopySpan : 0;
+  const dim3 grid(p.a.hkv, p.a.B, p.parts + copies), t(kWeightsThreads);
   if constexpr (F32) {
     hipLaunchKernelGGL((weights_kernel<D, true, 1>), grid, t, 0, st, p);
   } else {
