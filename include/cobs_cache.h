@@ -70,7 +70,7 @@ cobs_status_t cobs_tree_decode(const cobs_config_t* cfg, const void* q, cobs_dty
  *   lse:     device fp32 [B, num_queries, Hq]: the queries' normalisers, as cobs_tree_decode
  *            or a decode step returns them.  A query head with lse -inf or +inf adds nothing
  *            (+inf leaves a rejected drafted token out).
- *   prev:    optional device fp32 [B, Hkv, max_seq_len], NULL for zeros; may be `weights`.
+ *   prev:    optional device fp32 [B, Hkv, max_seq_len], NULL for zeros; `weights` itself, or apart.
  *   weights: device fp32 [B, Hkv, max_seq_len].                                     */
 cobs_status_t cobs_attention_weights(const cobs_config_t* cfg, const void* q, cobs_dtype_t io_dtype,
                                      int32_t num_queries, const cobs_kv_t* kv, const int32_t* seq_lens,
@@ -105,10 +105,12 @@ cobs_status_t cobs_evict(const cobs_config_t* cfg, const float* weights, const i
  *              context length, when the accepted tokens of a draft move up behind it).
  *   dst:       NULL: in place.  Then the entries must ascend strictly with
  *              kept[j] >= first + j (as cobs_evict's do; otherwise the moved rows' contents are
- *              unspecified).  Else another cache, apart from the first in memory, with the strides
- *              or pages of `dst` and a capacity of dst_max_seq_len tokens (a multiple of
- *              block_size; in place max_seq_len); any order, repeats allowed.  Tokens that would
- *              go behind the capacity are dropped.
+ *              unspecified).  Else another cache with the strides or pages of `dst` and a capacity
+ *              of dst_max_seq_len tokens (a multiple of block_size; in place max_seq_len), apart
+ *              from the first in memory: other tensors, or other pages of the same pool, given by
+ *              a table of their own.  Any order, repeats allowed; tokens that would go behind the
+ *              capacity are dropped.  Rows and heads of the destination share no memory (strides
+ *              of 0 are refused; no page is in a table twice).
  *   weights:   optional device fp32 [B, Hkv, max_seq_len]; weights_out: device fp32
  *              [B, Hkv, dst_max_seq_len], both or neither; the same pointer exactly when in
  *              place.  weights_out of the positions first + j whose entry moves nothing, and of

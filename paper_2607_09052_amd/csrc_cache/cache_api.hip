@@ -29,7 +29,9 @@ cobs_status_t check_shape(const cobs_config_t* c) {
   if (c->head_dim != 64 && c->head_dim != 128) return COBS_ERR_UNSUPPORTED;
   if (c->block_size != 32 && c->block_size != 64 && c->block_size != 128) return COBS_ERR_UNSUPPORTED;
   if (c->max_seq_len / c->block_size > kMaxBlocksPerSeq) return COBS_ERR_UNSUPPORTED;
-  if (c->batch > 65535 || c->num_kv_heads > 65535) return COBS_ERR_UNSUPPORTED;   // grid dimensions
+  // grid dimensions, and row indices of 32 bits
+  if (c->batch > 65535 || c->num_kv_heads > 65535 || (int64_t)c->batch * c->num_q_heads > (1 << 22))
+    return COBS_ERR_UNSUPPORTED;
   return COBS_OK;
 }
 
@@ -188,8 +190,15 @@ cobs_status_t cobs_compact_cache(const cobs_config_t* cfg, const cobs_kv_t* kv, 
   if (dst_max_seq_len < 1 || dst_max_seq_len % cfg->block_size != 0) return COBS_ERR_INVALID_ARG;
   if (dst_max_seq_len / cfg->block_size > kMaxBlocksPerSeq) return COBS_ERR_UNSUPPORTED;
   if (!dst && dst_max_seq_len != cfg->max_seq_len) return COBS_ERR_INVALID_ARG;
-  // apart in memory: the same cache as its own destination is the call in place
-  if (dst && (dst->k == kv->k || dst->v == kv->v || dst->k == kv->v || dst->v == kv->k)) return COBS_ERR_INVALID_ARG;
+  // apart in memory: the same cache as its own destination is the call in place; other pages of the same pool are apart
+  if (dst && (dst->k == kv->v || dst->v == kv->k)) return COBS_ERR_INVALID_ARG;
+  if (dst && (dst->k == kv->k || dst->v == kv->v) &&
+      !(dst->block_table && kv->block_table && dst->block_table != kv->block_table))
+    return COBS_ERR_INVALID_ARG;
+  // rows and heads that share memory cannot be written apart
+  const cobs_kv_t* to = dst ? dst : kv;
+  if (!to->block_table && ((cfg->batch > 1 && to->stride_b == 0) || (cfg->num_kv_heads > 1 && to->stride_h == 0)))
+    return COBS_ERR_INVALID_ARG;
   if ((weights == nullptr) != (weights_out == nullptr)) return COBS_ERR_INVALID_ARG;
   if (weights && (weights == weights_out) != (dst == nullptr)) return COBS_ERR_INVALID_ARG;
   CompactParams p = {};

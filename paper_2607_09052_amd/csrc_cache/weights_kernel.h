@@ -40,20 +40,22 @@ struct WeightsShape {
   static constexpr int LPP = PARTS;                     // 16-byte loads of a piece
 };
 
-constexpr int kCopySpan = 2048;             // positions of a copying workgroup: 64 blocks at most
+constexpr int kCopySpan = 8192;             // positions of a copying workgroup
+
+static_assert(kCopySpan / kFrame / 64 <= 2 * kStepTiles * 16, "the span's block bits fit s_bits");
 
 // Earlier weights (or zeros) of the positions below the window start whose blocks are not selected.
 __device__ __forceinline__ void copy_weights(const WeightsParams& p, const Attended& x, int b, int h, int t0,
                                              unsigned long long* s_blocks) {
   const AttendParams& a = p.a;
-  if (threadIdx.x == 0) *s_blocks = 0;
+  // s_blocks: a bit per block of the span
+  if (threadIdx.x < kCopySpan / kFrame / 64) s_blocks[threadIdx.x] = 0;
   __syncthreads();
   for (int i = threadIdx.x; i < x.nsel; i += kWeightsThreads) {
     const int at = x.sel[i] - (t0 >> a.lsh);
-    if (at >= 0 && at < (kCopySpan >> a.lsh)) atomicOr(s_blocks, 1ull << at);
+    if (at >= 0 && at < (kCopySpan >> a.lsh)) atomicOr(&s_blocks[at >> 6], 1ull << (at & 63));
   }
   __syncthreads();
-  const unsigned long long blocks = *s_blocks;
   const int64_t row = ((int64_t)b * a.hkv + h) * a.tmax;
   const int end = min(t0 + kCopySpan, x.ws);
   float v[kCopySpan / kWeightsThreads];
@@ -65,7 +67,8 @@ __device__ __forceinline__ void copy_weights(const WeightsParams& p, const Atten
 #pragma unroll
   for (int k = 0; k < kCopySpan / kWeightsThreads; ++k) {
     const int t = t0 + k * kWeightsThreads + threadIdx.x;
-    if (t < end && !((blocks >> ((t - t0) >> a.lsh)) & 1)) p.weights[row + t] = v[k];
+    const int at = (t - t0) >> a.lsh;
+    if (t < end && !((s_blocks[at >> 6] >> (at & 63)) & 1)) p.weights[row + t] = v[k];
   }
 }
 
@@ -85,7 +88,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), quad = lane >> 4;
   const Attended x = attended<kWeightsThreads>(a, b, h, red);
   if (part < 0) {
-    copy_weights(p, x, b, h, (-1 - part) * kCopySpan, &s_live[0]);
+    copy_weights(p, x, b, h, (-1 - part) * kCopySpan, &s_bits[0][0]);
     return;
   }
   const int nf = x.frames(), all = (nf + 4 * TF - 1) / (4 * TF);
@@ -352,11 +355,13 @@ hipError_t launch_weights_kernels(WeightsParams p, hipStream_t st) {
   const int frames = max_frames(p.a);
   // a pass of up to 64 rows is bound by HBM (2 us); each 64 of more rows take 3 us (fp32 keys: 6)
   const int steps = (p.a.N * p.a.G + 63) / 64;
-  p.parts = parts_of((frames + PASS - 1) / PASS, (int64_t)p.a.hkv * p.a.B, steps == 1 ? 2.0 : steps * (F32 ? 6.0 : 3.0),
-                     64 / TF, 32768);
-  p.lg = p.a.G == 1 ? 0 : (p.a.G == 2 ? 1 : (p.a.G == 4 ? 2 : (p.a.G == 8 ? 3 : 4)));
-  // a sparse call's copies of the other positions, in place not needed, follow as more parts
+  // a sparse call's copies of the other positions, not needed in place, follow as more parts (each about
+  // half a part's time)
+  const int64_t units = (int64_t)p.a.hkv * p.a.B;
   const int copies = p.a.sparse && p.prev != p.weights ? (p.a.tmax + kCopySpan - 1) / kCopySpan : 0;
+  p.parts = parts_of((frames + PASS - 1) / PASS, units, steps == 1 ? 2.0 : steps * (F32 ? 6.0 : 3.0), 64 / TF, 32768,
+                     units * copies / 2);
+  p.lg = p.a.G == 1 ? 0 : (p.a.G == 2 ? 1 : (p.a.G == 4 ? 2 : (p.a.G == 8 ? 3 : 4)));
   const dim3 grid(p.a.hkv, p.a.B, p.parts + copies), t(kWeightsThreads);
   if constexpr (F32) {
     hipLaunchKernelGGL((weights_kernel<D, true, 1>), grid, t, 0, st, p);

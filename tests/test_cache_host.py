@@ -139,7 +139,7 @@ BAD_CONFIGS = [
     (dict(batch=0), 1), (dict(num_q_heads=7), 1), (dict(num_kv_heads=0), 1), (dict(max_seq_len=100), 1),
     (dict(budget=-1), 1), (dict(window=-1), 1), (dict(softmax_scale=-1.0), 1), (dict(softmax_scale=float("nan")), 1),
     (dict(num_q_heads=6), 2), (dict(head_dim=96), 2), (dict(block_size=16), 2),
-    (dict(max_seq_len=64 * 8193), 2), (dict(batch=65536), 2),
+    (dict(max_seq_len=64 * 8193), 2), (dict(batch=65536), 2), (dict(batch=65535, num_q_heads=128, num_kv_heads=8), 2),
 ]
 
 
@@ -190,6 +190,8 @@ def test_evict_refuses(edit):
     (dict(dst=None, cap=64), 1),                       # in place the capacity is the cache's
     (dict(dst=_kv()), 1), (dict(dst=_kv(v=OTHER)), 1),  # the same memory as another cache
     (dict(dst=_kv(k=FAKE + 4096, v=OTHER)), 1),
+    (dict(dst=_kv(block_table=FAKE, num_pages=4)), 1),  # the same pool, the source not in pages
+    (dict(dst=_kv(k=OTHER, v=OTHER + 4096, stride_b=0)), 1), (dict(dst=_kv(k=OTHER, v=OTHER + 4096, stride_h=0)), 1),
     (dict(w=FAKE), 1), (dict(wo=FAKE), 1), (dict(w=FAKE, wo=FAKE), 1), (dict(dst=None, w=FAKE, wo=OTHER), 1),
 ])
 def test_compact_refuses(edit, code):
@@ -199,6 +201,15 @@ def test_compact_refuses(edit, code):
     assert cache.lib().cobs_compact_cache(
         ctypes.byref(cfg), ctypes.byref(kv), a["kept"], a["per_head"], a["n"], a["seq"], a["first"],
         None if a["dst"] is None else ctypes.byref(a["dst"]), a["cap"], a["w"], a["wo"], None) == code
+
+
+def test_compaction_in_place_refuses_rows_that_share_memory_and_one_table_for_both():
+    cfg, lib, w = _cfg().c_struct(), cache.lib(), ctypes.c_void_p(FAKE)
+    for kv in (_kv(stride_b=0), _kv(stride_h=0)):
+        assert lib.cobs_compact_cache(ctypes.byref(cfg), ctypes.byref(kv), w, 1, 8, w, None, None, 4096, None, None, None) == 1
+    kv, dst = (_kv(block_table=FAKE, num_pages=9) for _ in range(2))
+    assert lib.cobs_compact_cache(ctypes.byref(cfg), ctypes.byref(kv), w, 1, 8, w, None, ctypes.byref(dst), 4096, None, None,
+                                  None) == 1
 
 
 # ----------------------------------------------------------------- binding --

@@ -315,6 +315,28 @@ def test_compaction_leaves_pages_out_of_range_alone():
         assert bool((w[0, 0, 6:] == 0).all())
 
 
+def test_compaction_to_other_pages_of_the_same_pool():
+    B, Hkv, L, d, T, keep = 2, 2, 32, 128, (200, 150), 70
+    cfg = cobs.Config(batch=B, num_q_heads=Hkv, num_kv_heads=Hkv, head_dim=d, max_seq_len=224, rank=0, budget=0, window=0,
+                      block_size=L)
+    g = torch.Generator().manual_seed(4)
+    perm = torch.randperm(24, generator=g).to(torch.int32)
+    table, new = perm[:14].view(2, 7).to(DEV), perm[14:20].view(2, 3).to(DEV)
+    k, v = (torch.randn((24, Hkv, L, d), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    k0, v0 = k.cpu().clone(), v.cpu().clone()
+    kept = torch.stack([torch.stack([torch.randperm(T[b], generator=g)[:keep].sort()[0] for _ in range(Hkv)]) for b in range(B)])
+    cache.cobs_compact_cache(cfg, k, v, kept.to(torch.int32).to(DEV), torch.tensor(T, dtype=torch.int32, device=DEV), k_out=k,
+                             v_out=v, block_table=table, num_pages=24, out_block_table=new, out_num_pages=24)
+    t, n = table.cpu(), new.cpu()
+    for b in range(B):
+        for h in range(Hkv):
+            for j in range(keep):
+                s = int(kept[b, h, j])
+                for x in (k0, v0):
+                    x[n[b, j // L], h, j % L] = x[t[b, s // L], h, s % L]
+    assert torch.equal(k.cpu(), k0) and torch.equal(v.cpu(), v0)
+
+
 def test_offsets_past_32_bits():
     """A cache whose last tokens lie 2^32 elements behind its first: rows 2^22 elements apart."""
     T, N, d, st = 1024, 3, 64, 1 << 22
@@ -332,6 +354,58 @@ def test_offsets_past_32_bits():
     want = k[:, :, 1::2].clone()
     cache.cobs_compact_cache(p.cfg, k, v, kept, torch.tensor([T], dtype=torch.int32, device=DEV))
     assert torch.equal(k[:, :, :T // 2], want)
+
+
+@pytest.mark.parametrize("kv,io,N,G", [("bf16", "bf16", 1, 1), ("bf16", "f32", 9, 4), ("bf16", "bf16", 33, 4), ("f32", "f32", 2, 1)])
+def test_long_parts_of_many_rows(kv, io, N, G):
+    """256 rows that are one row 256 times over (a batch stride of 0): few parts a row, each longer than the table of
+    frames.  Every row has the same bits, the first row is checked."""
+    say(f"long parts {kv} {io} {N} {G}")
+    p = Problem(DEV, B=1, Hkv=1, G=G, d=64, L=32, T=17000, N=N, kv=kv, io=io).upload()
+    q = Problem(DEV, B=1, Hkv=1, G=G, d=64, L=32, T=17000, N=N, kv=kv, io=io).upload()
+    B = 256
+    q.cfg.batch = q.B = B
+    q.qd, q.seq, q.drafts, q.mask = (x.repeat(B, *[1] * (x.dim() - 1)) for x in (p.qd, p.seq, p.drafts, p.mask))
+    q.kd, q.vd = (x.expand(B, -1, -1, -1) for x in (p.kd, p.vd))
+    out, lse = run_tree(q)
+    weights = run_weights(q, lse, torch.zeros((B, 1, q.cap), device=DEV))
+    sync()
+    assert torch.equal(out, out[:1].expand_as(out)) and torch.equal(lse, lse[:1].expand_as(lse))
+    assert torch.equal(weights, weights[:1].expand_as(weights))
+    p.check_tree(out[:1], lse[:1])
+    p.check_weights(weights[:1], lse[:1], None, np.zeros((1, 1, p.cap)))
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_problems(seed):
+    """Tree attention and weights over random shapes, types, layouts, selections, windows and drafts."""
+    r = np.random.default_rng(1000 + seed)
+    G = int(r.choice([1, 2, 4, 8, 16]))
+    N = int(r.integers(1, 65)) if r.random() < 0.5 else int(r.integers(1, 6))
+    B = int(r.integers(1, 4))
+    T = [int(x) for x in np.exp(r.uniform(0, np.log(2500 if N * G < 300 else 700), B))]
+    draft = bool(r.random() < 0.8)
+    sparse = bool(r.random() < 0.5)
+    a = dict(B=B, Hkv=int(r.integers(1, 4)), G=G, d=int(r.choice([64, 128])), L=int(r.choice([32, 64, 128])), T=T, N=N,
+             drafts=[int(r.integers(0, N + 1)) for _ in range(B)], draft=draft, s=int(r.integers(0, 20)) if sparse else -1,
+             w=int(r.integers(0, 300)) if sparse else 0, kv=str(r.choice(["bf16", "bf16", "f32"])),
+             io=str(r.choice(["bf16", "f32"])), layout=str(r.choice(["contiguous", "pages", "strided"])), seed=seed,
+             extra=int(r.integers(0, 200)))
+    if draft and r.random() < 0.4:      # any bits, past the draft too
+        a["bits"] = [[int(x) for x in r.integers(0, 2 ** 64, N, dtype=np.uint64)] for _ in range(B)]
+    say(f"random {a}")
+    p = Problem(DEV, **a).upload()
+    out, lse = run_tree(p)
+    sync()
+    p.check_tree(out, lse)
+    before = torch.full((p.B, p.Hkv, p.cap), 7.0, device=DEV)
+    w = run_weights(p, lse, before.clone())
+    sync()
+    p.check_weights(w, lse, None, f64(before))
+    no_lse = torch.full_like(out, float("nan"))
+    cache.cobs_tree_decode(p.cfg, p.qd, p.kd, p.vd, p.seq, p.drafts, p.mask, no_lse, cache.new_tree_workspace(p.cfg, N, DEV),
+                           sel=p.sel_d, **p.pages)
+    assert torch.equal(out, no_lse)
 
 
 def test_a_serving_loop_runs_them_in_turn():
