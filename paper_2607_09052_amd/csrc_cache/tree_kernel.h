@@ -25,9 +25,10 @@
 //           the transposing read (ds_read_b64_tr_b16) takes 4 tokens by 16 columns per
 //           16 lanes;
 //   fp32 V  by column, as stored.
-// fp32 products run on 32x32x2 fp32 operands.  bf16 products take an fp32 query
-// and its probabilities as two bf16 parts (the rest is below 2^-17 of them), since
-// the outputs are fp32; with bf16 outputs, whose rounding is 2^-8, one part.
+// fp32 products run on 32x32x2 fp32 operands.  bf16 products take an fp32 query and
+// its probabilities as three bf16 parts, which hold all 24 bits (two leave 2^-17:
+// outputs 3.6e-6 off instead of 1e-6 at 32k tokens, and 4 to 20 % faster at up to
+// 64 rows); with bf16 outputs, whose rounding is 2^-8, one part.
 //
 // Drafted tokens stand in the frames behind the context; what a query's mask
 // leaves out gets score -inf.  A value that is not finite would still reach every
@@ -157,17 +158,21 @@ __device__ __forceinline__ void clear_padding(const TreeParams& p, int b, int h,
 }
 
 template <int D, int WQ, bool F32, int PARTS>
-__global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D == 128) ? 1 : 2) void tree_kernel(TreeParams p) {
+__global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ == 1) ? 1 : 2) void tree_kernel(TreeParams p) {
   using S = TreeShape<D, WQ, F32>;
   constexpr int WT = S::WT, CPR = S::CPR, LD = S::LD, NT = S::NT, FPI = S::FPI;
   constexpr int NDT = D / 32;
-  constexpr bool JOINT = FPI == 2 && PARTS == 1;          // a pass's frames at one maximum (two parts: too many registers)
+  constexpr bool JOINT = FPI == 2 && PARTS == 1;          // a pass's frames at one maximum (three parts leave no registers for it)
   constexpr int NF = JOINT ? 2 : 1;
   __shared__ __align__(16) char pool[S::LDS];
   __shared__ FrameEntry table[kTable];
   __shared__ float s_m[4][32], s_l[4][32];
   __shared__ unsigned long long s_bad[WT];
   __shared__ int red[4];
+  // The third parts of the first QL k-steps' queries are read from LDS: they are the registers by
+  // which two workgroups a CU would spill, and a spilled value's reload waits for the frames under way.
+  constexpr int QL = PARTS == 3 && D == 128 ? (WQ == 2 ? 4 : (WQ == 4 ? 2 : 0)) : 0;
+  __shared__ __align__(16) uint4 q_low[QL > 0 ? WQ * QL * 64 : 1];
 
   const AttendParams& a = p.a;
   // Workgroups go round-robin to the 8 XCDs; the row tiles of one part of the
@@ -186,7 +191,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
   // ---- the query rows as the B operand: column lane % 32, k = 8 half + j of every step
   constexpr int QR = F32 ? D / 2 : 1, QK = F32 ? 1 : D / 16;
   float qf[QR];
-  sbf16x8_t qb[QK][F32 ? 1 : PARTS];
+  sbf16x8_t qb[QK][F32 ? 1 : PARTS];          // (the parts in q_low are dropped)
   if constexpr (F32) {
 #pragma unroll
     for (int u = 0; u < D / 8; ++u)
@@ -212,6 +217,8 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
           v[4] = s1.x; v[5] = s1.y; v[6] = s1.z; v[7] = s1.w;
         }
         split_bf16x8<PARTS>(v, qb[ks]);
+        if constexpr (PARTS == 3)
+          if (ks < QL) q_low[(wq * QL + ks) * 64 + lane] = __builtin_bit_cast(uint4, qb[ks][2]);   // the groups': the same
       }
     }
   }
@@ -314,14 +321,21 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (WQ == 1 && PARTS == 2 && D ==
           s[fr] = __builtin_amdgcn_mfma_f32_32x32x2f32(kk.w, qf[4 * u + 3], s[fr], 0, 0, 0);
         }
       } else {
-        sbf16x8_t kk[D / 16];
+        constexpr int KB = PARTS == 3 ? 2 : D / 16;       // operands read together
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) kk[ks] = *reinterpret_cast<const sbf16x8_t*>(kf + 2 * ks * S::KSTEP);
+        for (int k0 = 0; k0 < D / 16; k0 += KB) {
+          sbf16x8_t kk[KB];
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
+          for (int ks = 0; ks < KB; ++ks) kk[ks] = *reinterpret_cast<const sbf16x8_t*>(kf + 2 * (k0 + ks) * S::KSTEP);
 #pragma unroll
-          for (int k = PARTS - 1; k >= 0; --k)
-            s[fr] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[ks], qb[ks][k], s[fr], 0, 0, 0);
+          for (int ks = 0; ks < KB; ++ks) {
+#pragma unroll
+            for (int k = PARTS - 1; k >= 0; --k) {
+              sbf16x8_t qq = qb[k0 + ks][k];
+              if (k == 2 && k0 + ks < QL) qq = *reinterpret_cast<const sbf16x8_t*>(&q_low[(wq * QL + k0 + ks) * 64 + lane]);
+              s[fr] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[ks], qq, s[fr], 0, 0, 0);
+            }
+          }
         }
       }
     }
@@ -523,7 +537,7 @@ hipError_t launch_tree_kernels(const TreeParams& p, int wq, int grid, hipStream_
     go(std::integral_constant<int, 1>());
   } else {
     if (p.a.io_bf16) go(std::integral_constant<int, 1>());
-    else go(std::integral_constant<int, 2>());
+    else go(std::integral_constant<int, 3>());
   }
   return hipGetLastError();
 }

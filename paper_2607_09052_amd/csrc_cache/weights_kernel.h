@@ -7,8 +7,8 @@
 // positions.  A wave
 // loads the keys of its frames (TF at a time) straight into the operand layout, a
 // pass ahead; the M = N G query rows of the KV head come from LDS in operand order, 64
-// rows a step: up to 128 rows stay there for the workgroup's whole work, more
-// rotate through two buffers, their loads a step ahead.  S = Q K^T with tokens as
+// rows (32 of fp32 queries over bf16 keys) a step: up to two steps stay there for the
+// workgroup's whole work, more rotate through two buffers, their loads a step ahead.  S = Q K^T with tokens as
 // columns: a lane holds one token's scores against 4 rows of a tile, so the sum over
 // queries and heads of exp2(c2 s - log2(e) lse) is a sum within the lane and, at the
 // end, over the four lanes of a token.  16 x 16 products, because a load of their
@@ -27,7 +27,6 @@ namespace cobs {
 typedef float f32x4w_t __attribute__((ext_vector_type(4)));
 
 constexpr int kWeightsThreads = 256;
-constexpr int kStepTiles = 4;               // row tiles of 16 in a buffer
 
 template <int D, bool F32, int PARTS>
 struct WeightsShape {
@@ -35,14 +34,13 @@ struct WeightsShape {
   static constexpr int TG = 2 * TF;                     // groups of 16 tokens
   static constexpr int KS = F32 ? D / 16 : D / 32;      // 16-byte pieces of a lane per row
   static constexpr int TILE = KS * 1024 * PARTS;        // bytes of a staged row tile
-  static constexpr int STEP = kStepTiles * TILE;
-  static constexpr int PER = kStepTiles * KS * 64 / kWeightsThreads;   // staged pieces of a thread
-  static constexpr int LPP = PARTS;                     // 16-byte loads of a piece
+  static constexpr int ST = PARTS == 3 ? 2 : 4;         // row tiles of 16 in a buffer (two workgroups' fit a CU)
+  static constexpr int STEP = ST * TILE;
+  static constexpr int PER = ST * KS * 64 / kWeightsThreads;   // staged pieces of a thread
+  static constexpr int LPP = PARTS == 1 ? 1 : 2;        // 16-byte loads of a piece
 };
 
 constexpr int kCopySpan = 8192;             // positions of a copying workgroup
-
-static_assert(kCopySpan / kFrame / 64 <= 2 * kStepTiles * 16, "the span's block bits fit s_bits");
 
 // Earlier weights (or zeros) of the positions below the window start whose blocks are not selected.
 __device__ __forceinline__ void copy_weights(const WeightsParams& p, const Attended& x, int b, int h, int t0,
@@ -75,7 +73,7 @@ __device__ __forceinline__ void copy_weights(const WeightsParams& p, const Atten
 template <int D, bool F32, int PARTS>
 __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsParams p) {
   using S = WeightsShape<D, F32, PARTS>;
-  constexpr int TF = S::TF, TG = S::TG, KS = S::KS, PER = S::PER;
+  constexpr int TF = S::TF, TG = S::TG, KS = S::KS, PER = S::PER, kStepTiles = S::ST;
   constexpr int ES = F32 ? 4 : 2;
   __shared__ __align__(16) char tiles[2 * S::STEP];
   __shared__ __align__(16) float s_lse[2][kStepTiles * 16];          // log2 units; +inf: adds nothing
@@ -88,6 +86,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), quad = lane >> 4;
   const Attended x = attended<kWeightsThreads>(a, b, h, red);
   if (part < 0) {
+    static_assert(kCopySpan / kFrame / 64 <= 2 * kStepTiles * 16, "the span's block bits fit s_bits");
     copy_weights(p, x, b, h, (-1 - part) * kCopySpan, &s_bits[0][0]);
     return;
   }
@@ -167,7 +166,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
         }
       }
     }
-    if (wave == 0) {
+    if (wave == 0 && lane < 16 * kStepTiles) {
       const int r = step * kStepTiles * 16 + lane, i = r >> p.lg;
       qz = INFINITY;
       qbits = 0;
@@ -196,13 +195,15 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     }
     if (wave == 0) {
       const float z = qz == -INFINITY ? INFINITY : qz * 1.4426950408889634f;
-      s_lse[buf][lane] = z;
-      s_bits[buf][lane] = qbits;
+      if (lane < 16 * kStepTiles) {
+        s_lse[buf][lane] = z;
+        s_bits[buf][lane] = qbits;
+      }
       const unsigned long long live = __ballot(z != INFINITY);
       if (lane == 0) s_live[buf] = live;
     }
   };
-  static_assert(kStepTiles * 16 == 64, "one wave holds a step's normalisers");
+  static_assert(kStepTiles * 16 <= 64, "one wave holds a step's normalisers");
 
   const int steps = (M + kStepTiles * 16 - 1) / (kStepTiles * 16);
   const bool resident = steps <= 2;
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
           }
         };
         if (PARTS == 1 && !F32 && !drafted && nt == kStepTiles) {
-          // straight-line code: a tile's products among the exponentials of the tile before (two
+          // straight-line code: a tile's products among the exponentials of the tile before (more
           // parts or fp32 keys leave no registers for it: the spilled values cost a wait a pass)
           f32x4w_t sc[2][TG];
           scores(0, sc[0]);
@@ -353,13 +354,13 @@ hipError_t launch_weights_kernels(WeightsParams p, hipStream_t st) {
   // a wave's lanes hold its frames: at most 64
   constexpr int TF = F32 ? 1 : 2, PASS = 4 * TF;
   const int frames = max_frames(p.a);
-  // a pass of up to 64 rows is bound by HBM (2 us); each 64 of more rows take 3 us (fp32 keys: 6)
+  // a pass of up to 64 rows is bound by HBM (2 us); each 64 of more rows take 3 us (fp32 keys or queries: 6)
   const int steps = (p.a.N * p.a.G + 63) / 64;
   // a sparse call's copies of the other positions, not needed in place, follow as more parts (each about
   // half a part's time)
   const int64_t units = (int64_t)p.a.hkv * p.a.B;
   const int copies = p.a.sparse && p.prev != p.weights ? (p.a.tmax + kCopySpan - 1) / kCopySpan : 0;
-  p.parts = parts_of((frames + PASS - 1) / PASS, units, steps == 1 ? 2.0 : steps * (F32 ? 6.0 : 3.0), 64 / TF, 32768,
+  p.parts = parts_of((frames + PASS - 1) / PASS, units, steps == 1 ? 2.0 : steps * (F32 || !p.a.io_bf16 ? 6.0 : 3.0), 64 / TF, 32768,
                      units * copies / 2);
   p.lg = p.a.G == 1 ? 0 : (p.a.G == 2 ? 1 : (p.a.G == 4 ? 2 : (p.a.G == 8 ? 3 : 4)));
   const dim3 grid(p.a.hkv, p.a.B, p.parts + copies), t(kWeightsThreads);
@@ -367,7 +368,7 @@ hipError_t launch_weights_kernels(WeightsParams p, hipStream_t st) {
     hipLaunchKernelGGL((weights_kernel<D, true, 1>), grid, t, 0, st, p);
   } else {
     if (p.a.io_bf16) hipLaunchKernelGGL((weights_kernel<D, false, 1>), grid, t, 0, st, p);
-    else hipLaunchKernelGGL((weights_kernel<D, false, 2>), grid, t, 0, st, p);
+    else hipLaunchKernelGGL((weights_kernel<D, false, 3>), grid, t, 0, st, p);
   }
   return hipGetLastError();
 }

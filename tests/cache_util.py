@@ -102,21 +102,20 @@ class Problem:
         return q, f64(self.k)[b, h, :E], f64(self.v)[b, h, :E], self.see(b, h)
 
     def score_error(self, q, K, see):
-        """Largest error [N, G] that the score arithmetic allows in a score c q.k of a query: the fp32 products' sums
-        (d + 4 roundings at most) and, for fp32 queries over bf16 keys, the two bf16 parts of the query (2^-17)."""
-        part = 2.0 ** -17 if (self.kv == "bf16" and self.io == "f32") else 0.0
+        """Largest error [N, G] that the score arithmetic allows in a score c q.k of a query: the roundings of the
+        fp32 sums (an fp32 query over bf16 keys is three bf16 operands, so 3 d products, each exact) and 4 more."""
+        terms = 3 * self.d if (self.kv == "bf16" and self.io == "f32") else self.d
         big = np.zeros(q.shape[:2])
         for i in range(self.N):
             t = np.nonzero(see[i])[0]
             if len(t):
                 big[i] = (np.abs(q[i]) @ np.abs(K[t]).T).max(1)
-        return self.cfg.scale * big * (part + (self.d + 4) * U32)
+        return self.cfg.scale * big * (terms + 4) * U32
 
     def check_tree(self, out, lse):
         """Each output within its arithmetic's error: with |score error| <= e, every probability moves by 2 e of itself
-        at most (its own score and the normaliser's), by the exponential's (8 steps of fp32) and by its rounding for
-        the product with the values (two bf16 parts: 2^-16 of it; one, with bf16 outputs: 2^-8, and 2^-7 with both
-        the sum and the product taken of it); sums over n tokens add 4 sqrt(n) half steps (independent roundings); the
+        at most (its own score and the normaliser's), by the exponential's (8 steps of fp32) and, with bf16 outputs
+        over bf16 caches, by its rounding for the product with the values (2^-8; taken at 2^-7); sums over n tokens add 4 sqrt(n) half steps (independent roundings); the
         output is rounded to its type.  |lse - exact| <= e + the sum's error + half a step of it."""
         cfg = self.cfg
         worst = 0.0
@@ -126,7 +125,7 @@ class Problem:
                 q, K, V, see = self.unit(b, h)
                 want, wl = O.tree_attention(q, K, V, see, cfg.scale)
                 e = self.score_error(q, K, see)
-                rnd = 0.0 if self.kv == "f32" else (2.0 ** -7 if self.io == "bf16" else 2.0 ** -16)
+                rnd = 2.0 ** -7 if self.kv == "bf16" and self.io == "bf16" else 0.0
                 for i in range(self.N):
                     t = np.nonzero(see[i])[0]
                     g = got[b, i, h * self.G:(h + 1) * self.G]

@@ -134,7 +134,7 @@ def test_pages_out_of_range_are_left_out(kv):
             see[:, 64 * gone:64 * gone + 64] = False
             E = p.T[b] + 4
             want, wl = O.tree_attention(q[b, :, h], f64(p.k)[b, h, :E], f64(p.v)[b, h, :E], see, p.cfg.scale)
-            # as in check_tree: scores within 2^-17 c sum |q||k| (< 1e-3 here), loosely bounded
+            # as in check_tree, loosely bounded: scores within 388 half steps of c sum |q||k| (< 15 here), 4e-4
             assert np.abs(f64(out)[b, :, 4 * h:4 * h + 4] - want).max() < 1e-3
             assert np.abs(f64(lse)[b, :, 4 * h:4 * h + 4] - wl).max() < 1e-3
             assert bool((weights[b, h, 64 * gone:64 * gone + 64] == 0).all())
@@ -391,9 +391,9 @@ def test_random_problems(seed):
              w=int(r.integers(0, 300)) if sparse else 0, kv=str(r.choice(["bf16", "bf16", "f32"])),
              io=str(r.choice(["bf16", "f32"])), layout=str(r.choice(["contiguous", "pages", "strided"])), seed=seed,
              extra=int(r.integers(0, 200)))
+    say(f"random {a}")
     if draft and r.random() < 0.4:      # any bits, past the draft too
         a["bits"] = [[int(x) for x in r.integers(0, 2 ** 64, N, dtype=np.uint64)] for _ in range(B)]
-    say(f"random {a}")
     p = Problem(DEV, **a).upload()
     out, lse = run_tree(p)
     sync()
