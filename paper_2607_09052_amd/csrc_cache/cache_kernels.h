@@ -74,13 +74,21 @@ struct WeightsParams {
   int parts, lg;                // workgroups of a (row, KV head), log2 of G (set by the launcher)
 };
 
+// What a launch of an eviction leaves for the next, per chunk: the digits found and the keys still
+// needed (the same in each chunk), the chunk's keys above those digits.
+struct EvictState {
+  uint32_t prefix;
+  int need, over, unused;
+};
+
 struct EvictParams {
   const float* weights;
   const int32_t* seq_lens;
   int32_t* kept;
   int32_t* new_lens;
   int B, hkv, tmax, keep, sinks, recent;
-  uint16_t* hist;               // digit histograms of the chunks (evict_workspace)
+  uint16_t* hist;               // digit histograms of the chunks, then their states (evict_workspace)
+  EvictState* state;
   int chunks;                   // chunks of the longest row (set by the launcher)
 };
 

@@ -156,12 +156,20 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
   uint32_t prefix = 0;
   int above = 0, equal = 0;                                  // kept, and equal keys, of the chunks before
   uint16_t* hists = p.hist + (int64_t)unit * p.chunks * kChunkHist;
+  EvictState* const states = p.state + (int64_t)unit * p.chunks;
   if (choose) {
+    int over_here = 0;                                       // the chunk's keys above the digits found by earlier launches
+    if (LV == 2 || LV == 3) {
+      const EvictState e = states[chunk];
+      prefix = e.prefix;
+      need = e.need;
+      over_here = e.over;
+    }
 #pragma unroll 1
-    for (int lv = 0; lv < (LV == 4 ? 3 : LV); ++lv) {
-      int c[kBpt], before_c[kBpt];                           // all chunks; those before this one
+    for (int lv = LV == 4 || LV == 0 ? 0 : LV - 1; lv < (LV == 4 ? 3 : LV); ++lv) {
+      int c[kBpt], before_c[kBpt], own_c[kBpt];              // all chunks; those before this one; this one
 #pragma unroll
-      for (int i = 0; i < kBpt; ++i) c[i] = before_c[i] = 0;
+      for (int i = 0; i < kBpt; ++i) c[i] = before_c[i] = own_c[i] = 0;
       if (LV == 4) {
         count(lv, prefix);
 #pragma unroll
@@ -175,11 +183,20 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
           for (int i = 0; i < kBpt; ++i) {
             c[i] += n[i];
             before_c[i] += k < chunk ? n[i] : 0;
+            own_c[i] += k == chunk ? n[i] : 0;
           }
         }
       }
       const int d = find_digit(c, need, s, wave, lane);
       prefix |= (uint32_t)d << digit_shift(lv);
+      if (LV == 1 || LV == 2) {
+        // what the launches after need of this digit
+        int over = 0, before;
+#pragma unroll
+        for (int i = 0; i < kBpt; ++i) over += kBpt * tid + i > d ? own_c[i] : 0;
+        over = sum_before(over, s.wsum, wave, lane, before);
+        if (tid == 0) states[chunk] = {prefix, need, over_here + over, 0};
+      }
       if (LV == 3) {
         int over = 0, same = 0, before;
 #pragma unroll
@@ -187,8 +204,9 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
           over += kBpt * tid + i > d ? before_c[i] : 0;
           same += kBpt * tid + i == d ? before_c[i] : 0;
         }
-        above += sum_before(over, s.wsum, wave, lane, before);
-        if (lv == 2) equal = sum_before(same, s.wsum, wave, lane, before);
+        for (int k = tid; k < chunk; k += kEvictThreads) over += states[k].over;
+        above = sum_before(over, s.wsum, wave, lane, before);
+        equal = sum_before(same, s.wsum, wave, lane, before);
       }
     }
     if (LV < 4) make_keys();
@@ -254,7 +272,7 @@ static int evict_chunks(int tmax) { return (tmax + kEvictChunk - 1) / kEvictChun
 
 size_t evict_workspace(int B, int hkv, int tmax) {
   const int n = evict_chunks(tmax);
-  return n == 1 ? 0 : ((size_t)B * hkv * n * kChunkHist * sizeof(uint16_t) + 255) / 256 * 256;
+  return n == 1 ? 0 : ((size_t)B * hkv * n * (kChunkHist * sizeof(uint16_t) + sizeof(EvictState)) + 255) / 256 * 256;
 }
 
 hipError_t launch_evict(const EvictParams& q, hipStream_t st) {
@@ -268,6 +286,7 @@ hipError_t launch_evict(const EvictParams& q, hipStream_t st) {
     else hipLaunchKernelGGL((evict_kernel<32, 4>), grid, t, 0, st, p);
     return hipGetLastError();
   }
+  p.state = reinterpret_cast<EvictState*>(p.hist + (size_t)p.B * p.hkv * p.chunks * kChunkHist);
   hipLaunchKernelGGL((evict_kernel<32, 0>), grid, t, 0, st, p);
   hipLaunchKernelGGL((evict_kernel<32, 1>), grid, t, 0, st, p);
   hipLaunchKernelGGL((evict_kernel<32, 2>), grid, t, 0, st, p);

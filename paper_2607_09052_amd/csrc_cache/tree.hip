@@ -4,31 +4,81 @@
 
 namespace cobs {
 
-constexpr int kMergeThreads = 256, kMergeGroups = 4;
+constexpr int kMergeThreads = 256;
 
-// One output row per kMergeGroups groups of D / 4 threads, 4 outputs a thread: group g
-// takes the splits g, g + 4, ... (their loads in flight together) with the
-// weights 2^(m_k - max m), and the groups' sums meet in LDS in group order.
+struct MergeRow {
+  int64_t first, at;   // its first part; its row of out and lse
+  bool live;           // of a query that is there
+};
+__device__ __forceinline__ MergeRow merge_row(const TreeParams& p, uint32_t idx) {
+  const AttendParams& a = p.a;
+  const uint32_t M = a.N * a.G;
+  const int unit = idx / M, row = idx % M, b = unit / a.hkv, h = unit % a.hkv, i = row / a.G;
+  const int C = clamp_len(a.seq_lens[b], a.tmax);
+  const int nq = a.mask ? clamp_len(a.draft_lens[b], min(a.N, a.tmax - C)) : a.N;
+  return {(int64_t)unit * p.nsplit * M + row, ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G), i < nq};
+}
+
+// Parts joined with the weights 2^(m_k - max m).  A row of up to kFewParts parts by D / 4 threads,
+// 4 outputs a thread, all loads in one batch: many rows, bound by HBM.
+constexpr int kFewParts = 4;
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void tree_merge_few_kernel(TreeParams p) {
+  constexpr int TPR = D / 4, RPB = kMergeThreads / TPR;
+  const int M = p.a.N * p.a.G, d4 = threadIdx.x % TPR;
+  const uint32_t idx = blockIdx.x * RPB + threadIdx.x / TPR;
+  if (idx >= (uint32_t)(p.units * M)) return;
+  const MergeRow r = merge_row(p, idx);
+  float2 ml[kFewParts];
+  float4 o[kFewParts];
+#pragma unroll
+  for (int k = 0; k < kFewParts; ++k) {
+    if (k < p.nsplit) {                                  // (of a query that is not there: read, not used)
+      const int64_t at = r.first + (int64_t)k * M;
+      ml[k] = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
+      o[k] = *reinterpret_cast<const float4*>(p.part_o + at * D + 4 * d4);
+    } else {
+      ml[k] = make_float2(-INFINITY, 0.0f);
+      o[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+  }
+  float top = -INFINITY, total = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kFewParts; ++k) top = fmaxf(top, ml[k].x);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int k = 0; k < kFewParts; ++k) {
+    const float f = __builtin_amdgcn_exp2f(ml[k].x - ref);
+    total += f * ml[k].y;
+    sum.x += f * o[k].x; sum.y += f * o[k].y; sum.z += f * o[k].z; sum.w += f * o[k].w;
+  }
+  if (!r.live) {
+    total = 0.0f;
+    sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  }
+  store_row4(p.out, r.at * D + 4 * d4, sum, total, p.a.io_bf16);
+  if (d4 == 0 && p.lse) p.lse[r.at] = total != 0.0f ? ref * 0.6931471805599453f + logf(total) : -INFINITY;
+}
+
+// A row of more parts by kMergeGroups groups of D / 4 threads: group g takes the
+// parts g, g + 4, ... (their loads in flight together), and the groups' sums meet
+// in LDS in group order.  Few rows, bound by the chain of loads.
+constexpr int kMergeGroups = 4;
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeParams p) {
   constexpr int TPR = D / 4, RPB = kMergeThreads / (TPR * kMergeGroups), U = 8;
   __shared__ float4 s_sum[RPB][kMergeGroups][TPR];
   __shared__ float s_total[RPB][kMergeGroups];
-  const AttendParams& a = p.a;
-  const int M = a.N * a.G;
+  const int M = p.a.N * p.a.G;
   const int rb = threadIdx.x / (TPR * kMergeGroups), g = threadIdx.x / TPR % kMergeGroups, d4 = threadIdx.x % TPR;
-  const int64_t idx = (int64_t)blockIdx.x * RPB + rb;
-  const bool here = idx < (int64_t)p.units * M;
-  const int unit = here ? (int)(idx / M) : 0, row = here ? (int)(idx % M) : 0, b = unit / a.hkv, h = unit % a.hkv;
-  const int i = row / a.G;
-  const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
-  const int C = clamp_len(a.seq_lens[b], a.tmax);
-  const int nq = a.mask ? clamp_len(a.draft_lens[b], min(a.N, a.tmax - C)) : a.N;
-  const int64_t first = (int64_t)unit * p.nsplit * M + row;
-  const int n = here && i < nq ? p.nsplit : 0;
-  // the splits' maxima: each thread of a group loads its share
+  const uint32_t idx = blockIdx.x * RPB + rb;
+  const bool here = idx < (uint32_t)(p.units * M);
+  const MergeRow r = merge_row(p, here ? idx : 0);
+  const int n = here && r.live ? p.nsplit : 0;
+  // the parts' maxima: each thread of a group loads its share
   float top = -INFINITY;
-  for (int k = d4; k < n; k += TPR) top = fmaxf(top, p.part_ml[2 * (first + (int64_t)k * M)]);
+  for (int k = d4; k < n; k += TPR) top = fmaxf(top, p.part_ml[2 * (r.first + (int64_t)k * M)]);
 #pragma unroll
   for (int o = TPR / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   const float ref = top == -INFINITY ? 0.0f : top;
@@ -40,9 +90,9 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeParams p)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = k0 + u * kMergeGroups;
-      const int64_t r = first + (int64_t)(k < n ? k : g) * M;
-      ml[u] = *reinterpret_cast<const float2*>(p.part_ml + 2 * r);
-      o[u] = *reinterpret_cast<const float4*>(p.part_o + r * D + 4 * d4);
+      const int64_t at = r.first + (int64_t)(k < n ? k : g) * M;
+      ml[u] = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
+      o[u] = *reinterpret_cast<const float4*>(p.part_o + at * D + 4 * d4);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -63,8 +113,18 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeParams p)
     sum.x += o.x; sum.y += o.y; sum.z += o.z; sum.w += o.w;
     total += s_total[rb][k];
   }
-  store_row4(p.out, at * D + 4 * d4, sum, total, a.io_bf16);
-  if (d4 == 0 && p.lse) p.lse[at] = total != 0.0f ? ref * 0.6931471805599453f + logf(total) : -INFINITY;
+  store_row4(p.out, r.at * D + 4 * d4, sum, total, p.a.io_bf16);
+  if (d4 == 0 && p.lse) p.lse[r.at] = total != 0.0f ? ref * 0.6931471805599453f + logf(total) : -INFINITY;
+}
+
+template <int D>
+static hipError_t launch_merge(const TreeParams& p, hipStream_t st) {
+  const bool few = p.nsplit <= kFewParts;
+  const uint32_t rows = (uint32_t)(p.units * p.a.N * p.a.G), per = kMergeThreads / (D / 4 * (few ? 1 : kMergeGroups));
+  const dim3 g((rows + per - 1) / per), t(kMergeThreads);
+  if (few) hipLaunchKernelGGL(tree_merge_few_kernel<D>, g, t, 0, st, p);
+  else hipLaunchKernelGGL(tree_merge_kernel<D>, g, t, 0, st, p);
+  return hipGetLastError();
 }
 
 hipError_t launch_tree_bf16_d64(const TreeParams& p, int wq, int grid, hipStream_t st);
@@ -112,11 +172,7 @@ hipError_t launch_tree(const TreeParams& q, hipStream_t st) {
   if (p.a.kv_f32) e = p.a.d == 64 ? launch_tree_f32_d64(p, wq, g, st) : launch_tree_f32_d128(p, wq, g, st);
   else e = p.a.d == 64 ? launch_tree_bf16_d64(p, wq, g, st) : launch_tree_bf16_d128(p, wq, g, st);
   if (e != hipSuccess || p.nsplit == 1) return e;
-  const int64_t rows_out = (int64_t)p.units * p.a.N * p.a.G, per = kMergeThreads / (p.a.d / 4 * kMergeGroups);
-  const dim3 mg((unsigned)((rows_out + per - 1) / per));
-  if (p.a.d == 64) hipLaunchKernelGGL(tree_merge_kernel<64>, mg, dim3(kMergeThreads), 0, st, p);
-  else hipLaunchKernelGGL(tree_merge_kernel<128>, mg, dim3(kMergeThreads), 0, st, p);
-  return hipGetLastError();
+  return p.a.d == 64 ? launch_merge<64>(p, st) : launch_merge<128>(p, st);
 }
 
 }  // namespace cobs
