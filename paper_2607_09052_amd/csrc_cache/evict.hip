@@ -8,22 +8,25 @@
 // of the equal ones.
 //
 // A workgroup of 16 waves holds a chunk of up to 32768 keys in registers (wave w a
-// run of 64 KPT positions, so ranks come from ballots and one sum over waves).  (With 8
-// waves and chunks of 16384 the four launches of 64 rows of 131072 took 9 % longer.)
-// Rows of one chunk are done by one launch.  Longer ones take four: each writes the
-// chunks' histograms of one digit (16-bit counts, 4 KB a chunk), and the next sums
-// them anew in every workgroup, which costs less than a wait between workgroups,
-// needs no atomics across them and no cleared memory.  The sums over the chunks
-// before a workgroup's own are its ranks in the last launch.
+// run of 64 KPT positions, so ranks come from ballots and one sum over waves).
+// Rows of up to 32768 positions are done by one launch.  Longer ones take four: each
+// writes the chunks' histograms of one digit (16-bit counts, 4 KB a chunk), and the
+// next sums them in every workgroup, which costs less than a wait between
+// workgroups, needs no atomics across them and no cleared memory; what it found
+// goes on to the launch after it in a state per chunk.  The last one's sums over
+// the chunks before a workgroup's own are its ranks.
 //
-// Bound by HBM for many long rows (four reads of the weights, the later ones mostly
-// from the last-level cache), by the launches for few.
+// Bound by what one CU does with its chunk (loads, atomics in LDS, barriers): 9 to 16
+// us a launch with chunks of 32768, whatever the rows; so few rows take smaller
+// chunks, as long as there is a CU for each (evict_keys).  64 rows of 131072:
+// 47.6 us, the four reads at 2.8 TB/s; 8 rows: 23 us (38 with chunks of 32768).
+// Many long rows: 256 of 131072 in 166 us, 3.2 TB/s.
 #include "cache_device.h"
 
 namespace cobs {
 
 constexpr int kEvictThreads = 1024, kEvictWaves = 16;
-constexpr int kEvictChunk = 32768;
+constexpr int kEvictRow = 32768;                             // the longest row of one launch
 constexpr int kBins = 2048;                                  // of a digit; the last has 1024
 constexpr int kChunkHist = (2 * kBins + kBins / 2);          // 16-bit counts of a chunk: three digits
 __device__ __forceinline__ int digit_shift(int lv) { return lv == 0 ? 21 : (lv == 1 ? 10 : 0); }
@@ -112,9 +115,10 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
       for (int j = chunk * kEvictThreads + tid; j < p.keep; j += gridDim.x * kEvictThreads) out[j] = j < T ? j : -1;
     return;
   }
-  const int t_first = chunk * kEvictChunk;
+  constexpr int CHUNK = KPT * kEvictThreads;
+  const int t_first = chunk * CHUNK;
   if (t_first >= T) return;
-  const int nch = (T + kEvictChunk - 1) / kEvictChunk;
+  const int nch = (T + CHUNK - 1) / CHUNK;
   const int lo = p.sinks, hi = T - p.recent;                 // the tokens to choose from
   int need = p.keep - p.sinks - p.recent;                    // fewer than those: T > keep
   const bool choose = need > 0;
@@ -268,30 +272,53 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictParams p) {
   }
 }
 
-static int evict_chunks(int tmax) { return (tmax + kEvictChunk - 1) / kEvictChunk; }
+// Keys of a thread: the smallest chunks that are one a CU and at most 32 a row, whose histograms
+// every workgroup of the row sums.  (us with chunks of 8192, 16384, 32768: 8 rows of 131072 23, 26, 38;
+// 64 of 65000 32, 29, 40, and of 131072 62, 53, 48; 1 of 500000 38, 33, 37; 256 of 131072 200, 164, 166.)
+static int evict_keys(int B, int hkv, int tmax) {
+  if (tmax <= kEvictRow) return tmax <= 4 * kEvictThreads ? 4 : (tmax <= 16 * kEvictThreads ? 16 : 32);
+  for (int keys = 8; keys < 32; keys *= 2) {
+    const int64_t n = (tmax + keys * kEvictThreads - 1) / (keys * kEvictThreads);
+    if (n <= 32 && n * B * hkv <= 256) return keys;
+  }
+  return 32;
+}
+
+static int evict_chunks(int B, int hkv, int tmax) {
+  const int chunk = evict_keys(B, hkv, tmax) * kEvictThreads;
+  return (tmax + chunk - 1) / chunk;
+}
 
 size_t evict_workspace(int B, int hkv, int tmax) {
-  const int n = evict_chunks(tmax);
+  const int n = evict_chunks(B, hkv, tmax);
   return n == 1 ? 0 : ((size_t)B * hkv * n * (kChunkHist * sizeof(uint16_t) + sizeof(EvictState)) + 255) / 256 * 256;
+}
+
+template <int KPT>
+static hipError_t launch_long_rows(const EvictParams& p, dim3 grid, hipStream_t st) {
+  const dim3 t(kEvictThreads);
+  hipLaunchKernelGGL((evict_kernel<KPT, 0>), grid, t, 0, st, p);
+  hipLaunchKernelGGL((evict_kernel<KPT, 1>), grid, t, 0, st, p);
+  hipLaunchKernelGGL((evict_kernel<KPT, 2>), grid, t, 0, st, p);
+  hipLaunchKernelGGL((evict_kernel<KPT, 3>), grid, t, 0, st, p);
+  return hipGetLastError();
 }
 
 hipError_t launch_evict(const EvictParams& q, hipStream_t st) {
   EvictParams p = q;
-  p.chunks = evict_chunks(p.tmax);
+  const int keys = evict_keys(p.B, p.hkv, p.tmax);
+  p.chunks = evict_chunks(p.B, p.hkv, p.tmax);
   const dim3 grid(p.chunks, p.hkv, p.B), t(kEvictThreads);
   if (p.chunks == 1) {
-    // keys of a thread: as few as hold the longest row
-    if (p.tmax <= 4 * kEvictThreads) hipLaunchKernelGGL((evict_kernel<4, 4>), grid, t, 0, st, p);
-    else if (p.tmax <= 16 * kEvictThreads) hipLaunchKernelGGL((evict_kernel<16, 4>), grid, t, 0, st, p);
+    if (keys == 4) hipLaunchKernelGGL((evict_kernel<4, 4>), grid, t, 0, st, p);
+    else if (keys == 16) hipLaunchKernelGGL((evict_kernel<16, 4>), grid, t, 0, st, p);
     else hipLaunchKernelGGL((evict_kernel<32, 4>), grid, t, 0, st, p);
     return hipGetLastError();
   }
   p.state = reinterpret_cast<EvictState*>(p.hist + (size_t)p.B * p.hkv * p.chunks * kChunkHist);
-  hipLaunchKernelGGL((evict_kernel<32, 0>), grid, t, 0, st, p);
-  hipLaunchKernelGGL((evict_kernel<32, 1>), grid, t, 0, st, p);
-  hipLaunchKernelGGL((evict_kernel<32, 2>), grid, t, 0, st, p);
-  hipLaunchKernelGGL((evict_kernel<32, 3>), grid, t, 0, st, p);
-  return hipGetLastError();
+  if (keys == 8) return launch_long_rows<8>(p, grid, st);
+  if (keys == 16) return launch_long_rows<16>(p, grid, st);
+  return launch_long_rows<32>(p, grid, st);
 }
 
 }  // namespace cobs

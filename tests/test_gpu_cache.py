@@ -176,6 +176,8 @@ EVICT = [
     dict(T=(4093,), keep=1024, sinks=0, recent=0), dict(T=(4096, 1), keep=4095, sinks=8, recent=8),
     dict(T=(3000, 2999), keep=100, sinks=60, recent=40), dict(T=(70000, 30011), keep=5000, sinks=4, recent=64),
     dict(T=(131072,), keep=32768, sinks=4, recent=1024), dict(T=(50000,), keep=1), dict(T=(20000,), keep=19999, recent=19998),
+    # (chunks of 8192 so far; of 16384 and of 32768: more rows)
+    dict(T=(39990, 17, 33000, 40001) * 8, keep=700, sinks=3, recent=20), dict(T=(33001, 32769, 5) * 24, keep=900, sinks=3, recent=20),
 ]
 
 
