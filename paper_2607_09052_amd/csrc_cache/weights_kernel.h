@@ -36,6 +36,7 @@ struct WeightsShape {
   static constexpr int TILE = KS * 1024 * PARTS;        // bytes of a staged row tile
   static constexpr int ST = PARTS == 3 ? 2 : 4;         // row tiles of 16 in a buffer (two workgroups' fit a CU)
   static constexpr int STEP = ST * TILE;
+  static constexpr int BUFS = PARTS == 1 && !F32 ? 65536 / STEP : 2;   // buffers: 64 KB at most
   static constexpr int PER = ST * KS * 64 / kWeightsThreads;   // staged pieces of a thread
   static constexpr int LPP = PARTS == 1 ? 1 : 2;        // 16-byte loads of a piece
 };
@@ -75,10 +76,10 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   using S = WeightsShape<D, F32, PARTS>;
   constexpr int TF = S::TF, TG = S::TG, KS = S::KS, PER = S::PER, kStepTiles = S::ST;
   constexpr int ES = F32 ? 4 : 2;
-  __shared__ __align__(16) char tiles[2 * S::STEP];
-  __shared__ __align__(16) float s_lse[2][kStepTiles * 16];          // log2 units; +inf: adds nothing
-  __shared__ __align__(16) unsigned long long s_bits[2][kStepTiles * 16];
-  __shared__ unsigned long long s_live[2];                           // rows that add something
+  __shared__ __align__(16) char tiles[S::BUFS * S::STEP];
+  __shared__ __align__(16) float s_lse[S::BUFS][kStepTiles * 16];          // log2 units; +inf: adds nothing
+  __shared__ __align__(16) unsigned long long s_bits[S::BUFS][kStepTiles * 16];
+  __shared__ unsigned long long s_live[S::BUFS];                           // rows that add something
   __shared__ int red[4];
   const AttendParams& a = p.a;
   const int h = blockIdx.x, b = blockIdx.y;
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
       const float z = qz == -INFINITY ? INFINITY : qz * 1.4426950408889634f;
       if (lane < 16 * kStepTiles) {
         s_lse[buf][lane] = z;
-        s_bits[buf][lane] = qbits;
+        s_bits[buf][lane] = z != INFINITY ? qbits : 0;    // (a row that adds nothing sees no draft)
       }
       const unsigned long long live = __ballot(z != INFINITY);
       if (lane == 0) s_live[buf] = live;
@@ -206,13 +207,12 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   static_assert(kStepTiles * 16 <= 64, "one wave holds a step's normalisers");
 
   const int steps = (M + kStepTiles * 16 - 1) / (kStepTiles * 16);
-  const bool resident = steps <= 2;
+  const bool resident = steps <= S::BUFS;               // the first pass stages them all
   if (steps > 0) {
     fetch(0);
     load(0);
     put(0);
     if (steps > 1) fetch(1);
-    if (steps == 2) put(1);
     __syncthreads();
   }
   int n = 0;                                                                 // steps done
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     }
     for (int st = 0; st < steps; ++st, ++n) {
       const int buf = resident ? st : (n & 1);
-      const bool more = !resident && (st + 1 < steps || ps + 1 < passes);
+      const bool more = resident ? ps == 0 && st + 1 < steps : st + 1 < steps || ps + 1 < passes;
       // A step whose rows all add nothing is left out, so that it adds no NaN either (in a live one every token
       // of the context is attended to by some row).
       if (any && s_live[buf] != 0) {
@@ -311,29 +311,34 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
 #pragma unroll 1
           for (int tl = 0; tl < nt; ++tl) {
             f32x4w_t sc[TG];
-            scores(tl, sc);
             float z[4];
-            normalisers(tl, z);
-            // drafted tokens: the rows that see them
             unsigned long long bits[4];
+            normalisers(tl, z);
 #pragma unroll
             for (int i = 0; i < 4; ++i) bits[i] = s_bits[buf][tl * 16 + 4 * quad + i];
+            scores(tl, sc);
+            // bit t of a row's word for a frame: whether the row sees token t of it (the context's: all rows)
 #pragma unroll
-            for (int g = 0; g < TG; ++g) {
-              const int j = __builtin_amdgcn_readlane(my_a, ps * TF + g / 2) + 16 * (g % 2) + (lane & 15) - x.C;
+            for (int f = 0; f < TF; ++f) {
+              const int to_c = x.C - __builtin_amdgcn_readlane(my_a, ps * TF + f);
+              const int left = min(max(to_c, 0), kFrame), right = min(max(-to_c, 0), 63);
+              const uint32_t context = (uint32_t)((1ull << left) - 1);
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const bool see = (j < 0) | (((uint32_t)(bits[i] >> (j & 63)) & 1u) != 0);
-                const float e = __builtin_amdgcn_exp2f(fmaf(sc[g][i], c2, -z[i]));
-                sum[g] += (see & (z[i] != INFINITY)) ? e : 0.0f;
+                const uint32_t see = ((uint32_t)((bits[i] << left) >> right) | context) >> (lane & 15);
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                  const float e = __builtin_amdgcn_exp2f(fmaf(sc[2 * f + g][i], c2, -z[i]));
+                  sum[2 * f + g] += (see >> (16 * g)) & 1u ? e : 0.0f;
+                }
               }
             }
           }
         }
       }
       if (more) {
-        put((n + 1) & 1);
-        fetch((st + 2) % steps);
+        put(resident ? st + 1 : (n + 1) & 1);
+        if (!resident || st + 2 < steps) fetch((st + 2) % steps);
         __syncthreads();
       }
     }
