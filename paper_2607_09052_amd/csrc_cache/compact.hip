@@ -19,10 +19,9 @@ __device__ __forceinline__ int kept_at(const CompactParams& p, int b, int h, int
   return p.kept[(p.per_head ? ((int64_t)b * p.hkv + h) : (int64_t)b) * p.num_kept + j];
 }
 
-// Destination of entry j and its source; false when the entry moves nothing.
-__device__ __forceinline__ bool move_of(const CompactParams& p, int b, int h, int T, int first, int j, int64_t& from,
-                                        int64_t& to) {
-  const int t = kept_at(p, b, h, j);
+// Destination of entry j, position t, and its source; false when the entry moves nothing.
+__device__ __forceinline__ bool move_of(const CompactParams& p, int b, int h, int T, int first, int j, int t,
+                                        int64_t& from, int64_t& to) {
   if (t < 0 || t >= T || j >= p.dst_max - first) return false;
   from = kv_offset(p.src, b, h, t);
   to = kv_offset(p.dst, b, h, first + j);
@@ -48,7 +47,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_copy_kernel(CompactPa
   const int row = ((int)blockIdx.x * kCompactThreads + threadIdx.x) / CPR, ch = threadIdx.x % CPR;
   if (row >= p.num_kept) return;
   int64_t from, to;
-  const bool ok = move_of(p, b, h, T, first, row, from, to);
+  const bool ok = move_of(p, b, h, T, first, row, kept_at(p, b, h, row), from, to);
   if (ok) {
     const uint4 k = reinterpret_cast<const uint4*>(static_cast<const char*>(p.src.k) + from * es)[ch];
     const uint4 v = reinterpret_cast<const uint4*>(static_cast<const char*>(p.src.v) + from * es)[ch];
@@ -62,7 +61,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_copy_kernel(CompactPa
 // in place: blockIdx.x = slice of a row's 16-byte chunks (SC of them, K then V),
 // and one more for the weights
 template <int CPR, int SC>
-__global__ __launch_bounds__(kCompactThreads) void compact_in_place_kernel(CompactParams p) {
+__global__ __launch_bounds__(kCompactThreads, 4) void compact_in_place_kernel(CompactParams p) {
   constexpr int NS = CPR / SC, RPP = kCompactThreads / SC, U = 8;
   const int h = blockIdx.y, b = blockIdx.z, es = p.kv_f32 ? 4 : 2, tid = threadIdx.x;
   const int T = clamp_len(p.seq_lens[b], p.tmax);
@@ -78,7 +77,7 @@ __global__ __launch_bounds__(kCompactThreads) void compact_in_place_kernel(Compa
         const int j = j0 + i * kCompactThreads + tid;
         int64_t from, to;
         w[i] = 0.0f;
-        if (j < p.num_kept && move_of(p, b, h, T, first, j, from, to)) w[i] = p.weights[u + kept_at(p, b, h, j)];
+        if (j < p.num_kept && move_of(p, b, h, T, first, j, kept_at(p, b, h, j), from, to)) w[i] = p.weights[u + kept_at(p, b, h, j)];
       }
       __syncthreads();
 #pragma unroll
@@ -90,24 +89,45 @@ __global__ __launch_bounds__(kCompactThreads) void compact_in_place_kernel(Compa
     }
     return;
   }
+  // A batch's rows are in registers before the workgroup's barrier; then the next batch's, which
+  // no write of this one meets, are under way while this one is written.
   char* base = static_cast<char*>(const_cast<void*>(slice < NS ? p.src.k : p.src.v));
-  const int ch = (slice % NS) * SC + tid % SC;
-  for (int j0 = 0; j0 < p.num_kept; j0 += RPP * U) {
-    uint4 x[U];
-    int64_t to[U];
+  const int ch = (slice % NS) * SC + tid % SC, jt = tid / SC;
+  int t[U];
+  uint4 x[U] = {}, y[U] = {};
+  int64_t to[U], to_y[U];
+  auto entries = [&](int j0) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int j = j0 + i * RPP + tid / SC;
-      int64_t from;
-      if (j < p.num_kept && move_of(p, b, h, T, first, j, from, to[i]))
-        x[i] = reinterpret_cast<const uint4*>(base + from * es)[ch];
-      else to[i] = -1;
+      const int j = j0 + i * RPP + jt;
+      t[i] = j < p.num_kept ? kept_at(p, b, h, j) : -1;
     }
+  };
+  auto read = [&](int j0, uint4 (&r)[U], int64_t (&at)[U]) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      int64_t from;
+      if (move_of(p, b, h, T, first, j0 + i * RPP + jt, t[i], from, at[i])) r[i] = reinterpret_cast<const uint4*>(base + from * es)[ch];
+      else at[i] = -1;
+    }
+  };
+  entries(0);
+  read(0, x, to);
+  entries(RPP * U);
+  for (int j0 = 0; j0 < p.num_kept; j0 += RPP * U) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) asm volatile("" : "+v"(x[i].x), "+v"(x[i].y), "+v"(x[i].z), "+v"(x[i].w));   // arrived
     __syncthreads();
+    read(j0 + RPP * U, y, to_y);
+    entries(j0 + 2 * RPP * U);
 #pragma unroll
     for (int i = 0; i < U; ++i)
       if (to[i] >= 0) reinterpret_cast<uint4*>(base + to[i] * es)[ch] = x[i];
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      x[i] = y[i];
+      to[i] = to_y[i];
+    }
   }
 }
 
