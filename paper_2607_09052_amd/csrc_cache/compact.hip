@@ -6,7 +6,13 @@
 // that ascend strictly and kept[j] >= first + j, a position below first + j1 is the
 // source of no entry from j1 on, so a workgroup that owns a column slice of one
 // (batch row, KV head) walks the entries in order, reads a batch of rows into
-// registers, waits, and writes it: no write meets a later read.
+// registers, waits, and writes it while the next batch is read: no write meets a
+// later read.
+//
+// Measured with weights, bf16, d 128: to another cache 32 units of up to 8192 rows, 271 MB
+// read and written, in 47 us from the last-level cache and 55 from memory (4.9 TB/s, the rate
+// of a large copy); in place 32 units of 8192 rows in 76 us (3.5 TB/s), 8 units in 36, bound
+// by a batch's chain of loads (entry, row, barrier).
 #include <algorithm>
 
 #include "cache_device.h"
@@ -134,8 +140,13 @@ __global__ __launch_bounds__(kCompactThreads, 4) void compact_in_place_kernel(Co
 template <int CPR>
 static hipError_t launch_compact_rows(const CompactParams& p, hipStream_t st) {
   if (p.in_place) {
-    const int slices = 2 * CPR / 4 + (p.weights ? 1 : 0);
-    hipLaunchKernelGGL((compact_in_place_kernel<CPR, 4>), dim3(slices, p.hkv, p.B), dim3(kCompactThreads), 0, st, p);
+    // Slices of a 128-byte line where they are 128 workgroups, else of half a line (which two XCDs
+    // then read): 32 units of 8192 rows 76 and 91 us, 128 of 2048 49 and 71, but 8 of 8192 66 and 36.
+    const int more = p.weights ? 1 : 0;
+    if ((int64_t)p.B * p.hkv * (2 * CPR / 8) >= 128)
+      hipLaunchKernelGGL((compact_in_place_kernel<CPR, 8>), dim3(2 * CPR / 8 + more, p.hkv, p.B), dim3(kCompactThreads), 0, st, p);
+    else
+      hipLaunchKernelGGL((compact_in_place_kernel<CPR, 4>), dim3(2 * CPR / 4 + more, p.hkv, p.B), dim3(kCompactThreads), 0, st, p);
     return hipGetLastError();
   }
   const int rpw = kCompactThreads / CPR;

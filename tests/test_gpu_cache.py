@@ -297,6 +297,13 @@ def test_compaction_moves_rows_and_weights(kv, d, src, dst, T, num, per_head, fi
     assert torch.equal(wback.cpu(), e_w)
 
 
+@pytest.mark.parametrize("kv,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("src", ["contiguous", "pages", "strided"])
+def test_compaction_in_place_of_many_rows(kv, d, src):
+    """Enough (row, KV head) pairs for the wider slices, and entries for several of their batches."""
+    test_compaction_moves_rows_and_weights(kv, d, src, None, (2300, 200) * 16, 1700, True, None)
+
+
 def test_compaction_leaves_pages_out_of_range_alone():
     B, Hkv, L, d, cap = 1, 1, 64, 64, 256
     cfg = cobs.Config(batch=B, num_q_heads=1, num_kv_heads=1, head_dim=d, max_seq_len=cap, rank=0, budget=0, window=0)
