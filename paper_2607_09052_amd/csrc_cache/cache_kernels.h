@@ -31,19 +31,19 @@ inline int max_frames(const AttendParams& a) {
 }
 
 // Workgroups that each of `units` pieces of work of `passes` passes is split over: at most `parts`, with
-// at most `most` passes each, on 512 slots (256 CUs, two workgroups each).  The split with the least
+// at most `most` passes each, on `slots` (256 CUs, two workgroups each).  The split with the least
 // time of its rounds: a pass takes `pass_us`, and a workgroup 4 us more (measured: 3 to 5 us of
 // dependent loads before the first product).  The longest parts go first, so that only with one round
 // does a part's last, uneven pass show.  `taken`: workgroups besides that the launch has.
-inline int parts_of(int64_t passes, int64_t units, double pass_us, int64_t most, int64_t parts, int64_t taken = 0) {
+inline int parts_of(int64_t passes, int64_t units, double pass_us, int64_t most, int64_t parts, int64_t taken = 0, int64_t slots = 512) {
   int64_t best = 0;
   double cost = 0.0;
   for (int64_t rounds = 1; rounds <= 64; ++rounds) {
-    int64_t n = (512 * rounds - taken) / units;
+    int64_t n = (slots * rounds - taken) / units;
     n = n < 1 ? 1 : n;
     n = n < parts ? n : parts;
     n = n < passes ? n : passes;
-    const int64_t per = (passes + n - 1) / n, r = (units * n + taken + 511) / 512;
+    const int64_t per = (passes + n - 1) / n, r = (units * n + taken + slots - 1) / slots;
     const double mean = (double)passes / (double)n;
     const double c = r * (mean * pass_us + 4.0) + (r == 1 ? (per - mean) * pass_us : 0.0);
     if (per <= most && (best == 0 || c < cost)) { best = n; cost = c; }

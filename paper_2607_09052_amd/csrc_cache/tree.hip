@@ -137,19 +137,25 @@ hipError_t launch_tree_f32_d128(const TreeParams& p, int wq, int grid, hipStream
 void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit) {
   const int M = a.N * a.G;
   *wq = M <= 32 ? 1 : (M <= 64 ? 2 : 4);
+  // Tiles of 256 rows (tree_wide.h) where they pad no more than tiles of 128 and a workgroup has some 64 frames
+  // or more (us with tiles of 128 and of 256: 512 rows over 8 x 32k tokens 675, 617; 256 rows over 32 x 4k 198, 187,
+  // over 32k 64, 66, over 16 x 2k 67, 68; 64-element heads 412, 414).
+  const int64_t units = (int64_t)a.B * a.hkv, tiles = (M + 255) / 256;
+  if (a.io_bf16 && !a.kv_f32 && a.d == 128 && (M + 127) / 128 == 2 * tiles && max_frames(a) * units * tiles >= 64 * 256) *wq = 8;
   *mtiles = (M + *wq * 32 - 1) / (*wq * 32);
   // the longest row's frames, by a pass of a workgroup's waves at a time
   const int step = *wq == 1 ? 4 : (*wq == 2 || !a.kv_f32 ? 2 : 1);
   const int64_t passes = (max_frames(a) + step - 1) / step;
-  *nsplit = parts_of(passes, (int64_t)a.B * a.hkv * *mtiles, 2.0, 1 << 30, 128);
+  *nsplit = parts_of(passes, units * *mtiles, *wq == 8 ? 1.0 : 2.0, 1 << 30, 128, 0, *wq == 8 ? 256 : 512);
 }
 
-// Enough for both attended sets.
+// Enough for both attended sets and types of q.
 size_t tree_workspace(const AttendParams& a) {
   int wq, mtiles, nsplit = 1;
-  for (int sparse = 0; sparse < 2; ++sparse) {
+  for (int form = 0; form < 4; ++form) {
     AttendParams x = a;
-    x.sparse = sparse;
+    x.sparse = form & 1;
+    x.io_bf16 = form >> 1;
     int n;
     tree_plan(x, &wq, &mtiles, &n);
     nsplit = n > nsplit ? n : nsplit;

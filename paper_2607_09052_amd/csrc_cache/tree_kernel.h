@@ -18,10 +18,10 @@
 // Measured (d 128, bf16 cache): 16 rows of a batch of 32 over 85 selected blocks and a window of
 // 512, fp32 queries: 800 MB in 168 us, 4.8 TB/s, with three products for one (150 TFLOP in them)
 // near the matrix cores' bound too; 128 rows over 32k tokens, on pages: 4.0 TB/s; 512 rows over 32k
-// tokens: 0.55 TFLOP in 690 us, 800 TFLOP/s, the matrix cores busy 40 % of the
+// tokens: 0.55 TFLOP in 675 us, 815 TFLOP/s, the matrix cores busy 40 % of the
 // time and the exponentials' pipe as long, which overlap little with two waves a
-// SIMD.  64 rows a wave, one wave a SIMD, halve the reads from LDS and lose that
-// overlap: 910 us.  One short context: 9 us of dependent loads, barriers and one pass.
+// SIMD (tree_wide.h has the form for such calls).  One short context: 9 us of
+// dependent loads, barriers and one pass.
 //
 // Frames travel HBM -> registers (two passes ahead; WQ = 1: one) -> LDS, in 16-byte
 // chunks that are swizzled by row against bank conflicts:

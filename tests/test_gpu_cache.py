@@ -49,6 +49,77 @@ def test_tree_decode_matches_fp64(shape, kv, io):
     say(f"worst error / tolerance {p.check_tree(out, lse):.3f}")
 
 
+# Many rows over a long cache (of which little may be filled): tiles of 256 rows
+MANY_ROWS = [
+    dict(B=2, Hkv=8, G=16, T=(300, 77), N=64, extra=8192),
+    dict(B=2, Hkv=8, G=16, T=(1100, 0), N=64, drafts=(64, 40), extra=7200, layout="pages"),
+    dict(B=2, Hkv=8, G=16, T=(500, 33), N=44, drafts=(31, 44), extra=11000, layout="strided"),   # 704 rows, 31 of 44 queries
+    dict(B=2, Hkv=8, G=16, T=(1900, 700), N=64, s=128, w=100, extra=6400),
+    dict(B=2, Hkv=8, G=16, T=(129, 96), N=64, draft=False, L=32, extra=8192, c=0.3),
+    dict(B=1, Hkv=8, G=16, T=0, N=64, drafts=(0,), extra=16448),
+]
+
+
+@pytest.mark.parametrize("shape", MANY_ROWS, ids=_ids)
+def test_tree_decode_of_many_rows_matches_fp64(shape):
+    say(f"tree, many rows {shape}")
+    p = Problem(DEV, io="bf16", **shape).upload()
+    out, lse = run_tree(p)
+    sync()
+    say(f"worst error / tolerance {p.check_tree(out, lse):.3f}")
+
+
+def test_many_rows_over_one_long_context():
+    """64 (row, KV head) pairs that share one cache of 17024 tokens by strides of 0: one part of 532 frames each."""
+    p = Problem(DEV, B=1, Hkv=1, G=16, T=16960, N=64, io="bf16", seed=8).upload()
+    B, H = 4, 16
+    cfg = cobs.Config(batch=B, num_q_heads=H * 16, num_kv_heads=H, head_dim=128, max_seq_len=p.cap, rank=0, budget=0, window=0)
+    q = torch.randn((B, 64, H, 16, 128), generator=torch.Generator().manual_seed(9)).to(torch.bfloat16).to(DEV)
+    q[3, :, 15] = p.qd[0]
+    out, lse = torch.empty((B, 64, H * 16, 128), dtype=torch.bfloat16, device=DEV), torch.empty((B, 64, H * 16), device=DEV)
+    cache.cobs_tree_decode(cfg, q.view(B, 64, H * 16, 128), p.kd.expand(B, H, p.cap, 128), p.vd.expand(B, H, p.cap, 128),
+                           p.seq.expand(B).contiguous(), p.drafts.expand(B).contiguous(), p.mask.expand(B, 64).contiguous(),
+                           out, cache.new_tree_workspace(cfg, 64, DEV), lse=lse)
+    sync()
+    p.check_tree(out[3:, :, 240:].contiguous(), lse[3:, :, 240:].contiguous())
+
+
+def test_many_rows_do_not_see_what_others_see():
+    """As below, with tiles of 256 rows: values of drafted tokens that are not finite, NaN where no query looks."""
+    N, drafts, T = 64, (64, 50), (90, 0)
+    bits = [[1 << i for i in range(N)] for _ in range(2)]
+    a = dict(B=2, Hkv=8, G=16, T=T, N=N, drafts=drafts, bits=bits, io="bf16", extra=8192)
+    p, clean = Problem(DEV, **a), Problem(DEV, **a)
+    for b in range(2):
+        p.k[b, :, T[b] + drafts[b]:] = float("nan")
+        p.v[b, :, T[b] + drafts[b]:] = float("inf")
+        p.v[b, :, T[b] + 5, 3:6] = torch.tensor([float("inf"), float("nan"), -float("inf")], dtype=p.v.dtype)
+    p.upload(), clean.upload()
+    (out, lse), (want, wl) = run_tree(p), run_tree(clean)
+    sync()
+    got5 = out[:, 5].float()
+    for e, f in ((3, torch.isposinf), (4, torch.isnan), (5, torch.isneginf)):
+        assert bool(f(got5[..., e]).all()), (e, got5[..., e])
+    out[:, 5, :, 3:6] = want[:, 5, :, 3:6]
+    assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+def test_many_rows_on_pages_out_of_range():
+    """A page id out of range leaves its tokens out, as if another selection had (both by tiles of 256 rows)."""
+    p = Problem(DEV, B=1, Hkv=16, G=16, T=300, N=64, io="bf16", layout="pages", extra=8192).upload()
+    gone = Problem(DEV, B=1, Hkv=16, G=16, T=300, N=64, io="bf16", layout="pages", extra=8192, s=160, w=0)
+    for h in range(16):                                                    # blocks 0, 2, 3, 4 of 0 .. 4
+        gone.sel[0, h, :] = -1
+        gone.sel[0, h, :4] = (0, 2, 3, 4)
+    gone.upload()
+    gone.check_tree(*run_tree(gone))
+    for bad in (-1, p.pages["num_pages"]):
+        p.pages["block_table"][0, 1] = bad
+        out, lse = run_tree(p)
+        sync()
+        gone.check_tree(out, lse)
+
+
 @pytest.mark.parametrize("layout", ["pages", "strided"])
 @pytest.mark.parametrize("kv", ["bf16", "f32"])
 @pytest.mark.parametrize("shape", [SHAPES[i] for i in (2, 5, 8, 9, 10, 14)], ids=_ids)
