@@ -74,6 +74,53 @@ __device__ __forceinline__ Attended attended(const AttendParams& p, int b, int h
   return x;
 }
 
+// Parts that a tree's context is split into, where the batch's nsplit B parts of a KV head go to the rows
+// by their frames: lane b has those of row b and of the rows before it.  (Alike in every kernel of a call; all
+// lanes active.)
+__device__ __forceinline__ void row_parts(const TreeParams& p, int& n, int& before) {
+  const AttendParams& a = p.a;
+  const int b = threadIdx.x & 63;
+  uint32_t frames = 0;
+  if (b < a.B) {
+    const int C = clamp_len(a.seq_lens[b], a.tmax);
+    const int drafted = a.mask ? clamp_len(a.draft_lens[b], min(a.N, a.tmax - C)) : 0;
+    frames = (uint32_t)(C + drafted + kFrame - 1) / kFrame;
+  }
+  const uint32_t all = (uint32_t)__builtin_amdgcn_readlane(wave_incl_scan((int)frames), 63);
+  // (at most 64 rows of 128 parts and 2^15 frames: below 2^32)
+  n = b < a.B ? 1 + (int)((uint32_t)(a.B * (p.nsplit - 1)) * frames / max(all, 1u)) : 0;
+  before = wave_incl_scan(n) - n;
+}
+
+// What a workgroup does: part `split` of the `n` of (row b, KV head h), whose first is number `first` of all.
+struct TreePart {
+  int b, h, split, n;
+  int64_t first;
+};
+
+// The part of workgroup `group` of units nsplit; false if it has none.  Of equal splits, the draft's frames
+// and the longer parts first.
+__device__ __forceinline__ bool tree_part(const TreeParams& p, int group, TreePart& t) {
+  const int hkv = p.a.hkv;
+  if (!p.even) {
+    const int unit = group % p.units;
+    t = {unit / hkv, unit % hkv, p.nsplit - 1 - group / p.units, p.nsplit, (int64_t)unit * p.nsplit};
+    return true;
+  }
+  int n, before;
+  row_parts(p, n, before);
+  t.h = group % hkv;
+  const int j = group / hkv;
+  const unsigned long long mine = __ballot(j >= before && j < before + n);
+  if (mine == 0) return false;
+  t.b = __builtin_ctzll(mine);
+  const int skip = __builtin_amdgcn_readlane(before, t.b);
+  t.split = j - skip;
+  t.n = __builtin_amdgcn_readlane(n, t.b);
+  t.first = (int64_t)t.h * p.a.B * p.nsplit + skip;
+  return true;
+}
+
 // Position of the first selected block >= blk among the nsel valid ones.
 __device__ __forceinline__ int sel_lower_bound(const Attended& x, int blk) {
   int lo = 0, hi = x.nsel;

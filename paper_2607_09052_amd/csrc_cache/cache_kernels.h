@@ -64,6 +64,7 @@ struct TreeParams {
   float* part_ml;
   float* part_o;
   int units, mtiles, nsplit;    // (row, KV head) pairs, query row tiles, splits
+  int even;                     // whether rows get parts by their length (row_parts)
 };
 
 struct WeightsParams {

@@ -8,15 +8,25 @@ constexpr int kMergeThreads = 256;
 
 struct MergeRow {
   int64_t first, at;   // its first part; its row of out and lse
+  int n;               // parts
   bool live;           // of a query that is there
 };
+// (every lane of the wave calls it)
 __device__ __forceinline__ MergeRow merge_row(const TreeParams& p, uint32_t idx) {
   const AttendParams& a = p.a;
   const uint32_t M = a.N * a.G;
   const int unit = idx / M, row = idx % M, b = unit / a.hkv, h = unit % a.hkv, i = row / a.G;
   const int C = clamp_len(a.seq_lens[b], a.tmax);
   const int nq = a.mask ? clamp_len(a.draft_lens[b], min(a.N, a.tmax - C)) : a.N;
-  return {(int64_t)unit * p.nsplit * M + row, ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G), i < nq};
+  int n = p.nsplit;
+  int64_t first = (int64_t)unit * p.nsplit;
+  if (p.even) {
+    int parts, before;
+    row_parts(p, parts, before);
+    n = __shfl(parts, b, 64);
+    first = (int64_t)h * a.B * p.nsplit + __shfl(before, b, 64);
+  }
+  return {first * M + row, ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G), n, i < nq};
 }
 
 // Parts joined with the weights 2^(m_k - max m).  A row of up to kFewParts parts by D / 4 threads,
@@ -28,13 +38,14 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_few_kernel(TreeParam
   constexpr int TPR = D / 4, RPB = kMergeThreads / TPR;
   const int M = p.a.N * p.a.G, d4 = threadIdx.x % TPR;
   const uint32_t idx = blockIdx.x * RPB + threadIdx.x / TPR;
-  if (idx >= (uint32_t)(p.units * M)) return;
-  const MergeRow r = merge_row(p, idx);
+  const bool here = idx < (uint32_t)(p.units * M);
+  const MergeRow r = merge_row(p, here ? idx : 0);
+  if (!here) return;
   float2 ml[kFewParts];
   float4 o[kFewParts];
 #pragma unroll
   for (int k = 0; k < kFewParts; ++k) {
-    if (k < p.nsplit) {                                  // (of a query that is not there: read, not used)
+    if (k < r.n) {                                       // (of a query that is not there: read, not used)
       const int64_t at = r.first + (int64_t)k * M;
       ml[k] = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
       o[k] = *reinterpret_cast<const float4*>(p.part_o + at * D + 4 * d4);
@@ -77,7 +88,7 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeParams p)
   const uint32_t idx = blockIdx.x * RPB + rb;
   const bool here = idx < (uint32_t)(p.units * M);
   const MergeRow r = merge_row(p, here ? idx : 0);
-  const int n = here && r.live ? p.nsplit : 0;
+  const int n = here && r.live ? r.n : 0;
   // the parts' maxima: each thread of a group loads its share
   float top = -INFINITY;
   for (int k = d4; k < n; k += TPR) top = fmaxf(top, p.part_ml[2 * (r.first + (int64_t)k * M)]);
@@ -121,7 +132,7 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeParams p)
 
 template <int D>
 static hipError_t launch_merge(const TreeParams& p, hipStream_t st) {
-  const bool few = p.nsplit <= kFewParts;
+  const bool few = p.nsplit <= kFewParts && !p.even;
   const uint32_t rows = (uint32_t)(p.units * p.a.N * p.a.G), per = kMergeThreads / (D / 4 * (few ? 1 : kMergeGroups));
   const dim3 g((rows + per - 1) / per), t(kMergeThreads);
   if (few) hipLaunchKernelGGL(tree_merge_few_kernel<D>, g, t, 0, st, p);
@@ -170,6 +181,11 @@ hipError_t launch_tree(const TreeParams& q, hipStream_t st) {
   int wq;
   tree_plan(p.a, &wq, &p.mtiles, &p.nsplit);
   p.units = p.a.B * p.a.hkv;
+  // Parts by the rows' lengths, which a wave's lanes hold: 128 rows over 4 contexts of 8k to 32k tokens, on pages,
+  // 110 us (120 with as many parts a row), 32 rows over 16 contexts 283 (302).  Contexts of one length pay 1 to 2 us
+  // for finding their part, so not for short ones, nor where few parts a row are dealt too coarsely (512 rows over
+  // 8 contexts of 2 parts: 599 us, 541 with 2 for each).
+  p.even = !p.a.sparse && p.a.B > 1 && p.a.B <= 64 && p.nsplit >= 4 && p.nsplit <= 128 && max_frames(p.a) >= 32 * p.nsplit;
   const size_t rows = (size_t)p.units * p.nsplit * p.a.N * p.a.G;
   p.part_o = p.part_ml + (rows * 2 * sizeof(float) + 255) / 256 * 256 / sizeof(float);
   // eight XCDs: a multiple of 8 workgroup slots (see tree_kernel)

@@ -49,7 +49,6 @@ namespace cobs {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kTreeThreads = 256;
 constexpr int kTable = 256;            // frame descriptors held in LDS at a time
@@ -147,8 +146,8 @@ __device__ __forceinline__ void add_nonfinite(const AttendParams& a, const Atten
 }
 
 // Partial of a split, per query row: (log2-domain maximum, sum) and D unnormalised outputs.
-__device__ __forceinline__ int64_t part_row(const TreeParams& p, int unit, int split, int r) {
-  return ((int64_t)unit * p.nsplit + split) * (p.a.N * p.a.G) + r;
+__device__ __forceinline__ int64_t part_row(const TreeParams& p, const TreePart& t, int r) {
+  return (t.first + t.split) * (p.a.N * p.a.G) + r;
 }
 
 // Outputs 0 and lse -inf for the rows of a tile that belong to no live query.
@@ -186,8 +185,9 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
   // context, which read the same keys and values, follow each other on one.
   const int slot = blockIdx.x >> 3, group = (slot / p.mtiles) * 8 + (blockIdx.x & 7), mt = slot % p.mtiles;
   if (group >= p.units * p.nsplit) return;
-  const int unit = group % p.units, split = p.nsplit - 1 - group / p.units;    // the draft's frames and the longer parts first
-  const int b = unit / a.hkv, h = unit % a.hkv;
+  TreePart part;
+  if (!tree_part(p, group, part)) return;
+  const int b = part.b, h = part.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tg = wave / WQ, wq = wave % WQ, half = lane >> 5, gt = tid % NT;
   const int row0 = (mt * WQ + wq) * 32;                         // the wave's query rows
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
 
   constexpr int STEP = WT * FPI;                                // frames of a pass of the workgroup
   const int nf = x.frames(), all = (nf + STEP - 1) / STEP;
-  const int f_lo = first_pass(all, split, p.nsplit) * STEP, f_hi = min(first_pass(all, split + 1, p.nsplit) * STEP, nf);
+  const int f_lo = first_pass(all, part.split, part.n) * STEP, f_hi = min(first_pass(all, part.split + 1, part.n) * STEP, nf);
   const uint32_t rsb = (uint32_t)((a.kv.table ? a.kv.d : a.kv.st) * S::ES);     // 32 rows: below 2^32 bytes
   char* const mine = pool + tg * S::NBUF * S::STAGE;
 
@@ -524,7 +524,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
       store_row4(p.out, at * D + 4 * d4, sum, ll, a.io_bf16);
       if (d4 == 0 && p.lse) p.lse[at] = ll != 0.0f ? rm * a.c + logf(ll) : -INFINITY;
     } else {
-      const int64_t at = part_row(p, unit, split, row);
+      const int64_t at = part_row(p, part, row);
       *reinterpret_cast<float4*>(p.part_o + at * D + 4 * d4) = sum;
       if (d4 == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(mm * c2, ll);
     }

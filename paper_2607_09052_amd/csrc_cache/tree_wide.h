@@ -37,8 +37,9 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
   const AttendParams& a = p.a;
   const int slot = blockIdx.x >> 3, group = (slot / p.mtiles) * 8 + (blockIdx.x & 7), mt = slot % p.mtiles;
   if (group >= p.units * p.nsplit) return;
-  const int unit = group % p.units, split = p.nsplit - 1 - group / p.units;
-  const int b = unit / a.hkv, h = unit % a.hkv;
+  TreePart part;
+  if (!tree_part(p, group, part)) return;
+  const int b = part.b, h = part.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   QueryRow q[QG];
 #pragma unroll
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
       for (int i = 0; i < 16; ++i) o[g][dt][i] = 0.0f;
   }
   const int nf = x.frames(), all = (nf + FPI - 1) / FPI;
-  const int f_lo = first_pass(all, split, p.nsplit) * FPI, f_hi = min(first_pass(all, split + 1, p.nsplit) * FPI, nf);
+  const int f_lo = first_pass(all, part.split, part.n) * FPI, f_hi = min(first_pass(all, part.split + 1, part.n) * FPI, nf);
   const uint32_t rsb = (uint32_t)((a.kv.table ? a.kv.d : a.kv.st) * 2);
 
   struct Frame {
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
         store_row4(p.out, at * D + 4 * d4, y, ll, a.io_bf16);
         if (d4 == 0 && p.lse) p.lse[at] = ll != 0.0f ? rm * a.c + logf(ll) : -INFINITY;
       } else {
-        const int64_t at = part_row(p, unit, split, row);
+        const int64_t at = part_row(p, part, row);
         *reinterpret_cast<float4*>(p.part_o + at * D + 4 * d4) = y;
         if (d4 == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(mm * c2, ll);
       }

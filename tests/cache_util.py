@@ -99,7 +99,7 @@ class Problem:
         """fp64 q [N, G, d], K, V [T + n, d] and the flags of one (row, KV head)."""
         E = self.T[b] + self.n[b]
         q = f64(self.q)[b].reshape(self.N, self.Hkv, self.G, self.d)[:, h]
-        return q, f64(self.k)[b, h, :E], f64(self.v)[b, h, :E], self.see(b, h)
+        return q, f64(self.k[b, h, :E]), f64(self.v[b, h, :E]), self.see(b, h)
 
     def score_error(self, q, K, see):
         """Largest error [N, G] that the score arithmetic allows in a score c q.k of a query: the roundings of the

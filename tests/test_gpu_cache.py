@@ -69,6 +69,21 @@ def test_tree_decode_of_many_rows_matches_fp64(shape):
     say(f"worst error / tolerance {p.check_tree(out, lse):.3f}")
 
 
+@pytest.mark.parametrize("kv,io", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("shape", [
+    dict(B=8, Hkv=8, G=4, T=(8100, 0, 33, 700, 2500, 1, 64, 4000), N=5, drafts=(5, 2, 0, 5, 3, 5, 1, 4)),      # 8 parts a row on average
+    dict(B=16, Hkv=8, G=2, T=(31, 4000, 0, 5) + (0,) * 11 + (100,), N=3, layout="pages", extra=128),           # 4 parts each
+    dict(B=5, Hkv=2, G=8, T=(13000, 12000, 300, 12500, 5), N=12, draft=False, extra=40000),                    # 51 on average
+], ids=_ids)
+def test_parts_by_the_rows_lengths(shape, kv, io):
+    """Contexts of very different lengths, which share the parts of the longest by their lengths."""
+    say(f"tree, uneven rows {shape} {kv} {io}")
+    p = Problem(DEV, kv=kv, io=io, d=64, **shape).upload()
+    out, lse = run_tree(p)
+    sync()
+    say(f"worst error / tolerance {p.check_tree(out, lse):.3f}")
+
+
 def test_many_rows_over_one_long_context():
     """64 (row, KV head) pairs that share one cache of 17024 tokens by strides of 0: one part of 532 frames each."""
     p = Problem(DEV, B=1, Hkv=1, G=16, T=16960, N=64, io="bf16", seed=8).upload()
