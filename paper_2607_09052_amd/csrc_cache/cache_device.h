@@ -74,11 +74,10 @@ __device__ __forceinline__ Attended attended(const AttendParams& p, int b, int h
   return x;
 }
 
-// Parts that a tree's context is split into, where the batch's nsplit B parts of a KV head go to the rows
-// by their frames: lane b has those of row b and of the rows before it.  (Alike in every kernel of a call; all
+// Parts that the rows' contexts are split into, where the `parts` B parts of a KV head go to the rows by
+// their frames: lane b has those of row b and of the rows before it.  (Alike in every kernel of a call; all
 // lanes active.)
-__device__ __forceinline__ void row_parts(const TreeParams& p, int& n, int& before) {
-  const AttendParams& a = p.a;
+__device__ __forceinline__ void row_parts(const AttendParams& a, int parts, int& n, int& before) {
   const int b = threadIdx.x & 63;
   uint32_t frames = 0;
   if (b < a.B) {
@@ -88,7 +87,7 @@ __device__ __forceinline__ void row_parts(const TreeParams& p, int& n, int& befo
   }
   const uint32_t all = (uint32_t)__builtin_amdgcn_readlane(wave_incl_scan((int)frames), 63);
   // (at most 64 rows of 128 parts and 2^15 frames: below 2^32)
-  n = b < a.B ? 1 + (int)((uint32_t)(a.B * (p.nsplit - 1)) * frames / max(all, 1u)) : 0;
+  n = b < a.B ? 1 + (int)((uint32_t)(a.B * (parts - 1)) * frames / max(all, 1u)) : 0;
   before = wave_incl_scan(n) - n;
 }
 
@@ -108,7 +107,7 @@ __device__ __forceinline__ bool tree_part(const TreeParams& p, int group, TreePa
     return true;
   }
   int n, before;
-  row_parts(p, n, before);
+  row_parts(p.a, p.nsplit, n, before);
   t.h = group % hkv;
   const int j = group / hkv;
   const unsigned long long mine = __ballot(j >= before && j < before + n);

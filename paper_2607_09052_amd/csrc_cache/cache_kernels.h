@@ -52,6 +52,11 @@ inline int parts_of(int64_t passes, int64_t units, double pass_us, int64_t most,
   return (int)(best > 0 ? best : (passes + most - 1) / most);
 }
 
+// Whether a batch's parts go to its rows by their lengths (row_parts) rather than `parts` to each.
+inline bool parts_by_length(const AttendParams& a, int parts) {
+  return !a.sparse && a.B > 1 && a.B <= 64 && parts >= 4 && parts <= 128 && max_frames(a) >= 32 * parts;
+}
+
 // Pass that part `i` of `n` begins with when `passes` are dealt evenly.
 __host__ __device__ inline int first_pass(int passes, int i, int n) { return (int)((int64_t)passes * i / n); }
 
@@ -72,7 +77,8 @@ struct WeightsParams {
   const float* lse;
   const float* prev;
   float* weights;
-  int parts, lg;                // workgroups of a (row, KV head), log2 of G (set by the launcher)
+  // set by the launcher: workgroups of a (row, KV head), on average if `even` (row_parts); log2 of G
+  int parts, lg, even;
 };
 
 // What a launch of an eviction leaves for the next, per chunk: the digits found and the keys still

@@ -22,7 +22,7 @@ __device__ __forceinline__ MergeRow merge_row(const TreeParams& p, uint32_t idx)
   int64_t first = (int64_t)unit * p.nsplit;
   if (p.even) {
     int parts, before;
-    row_parts(p, parts, before);
+    row_parts(a, p.nsplit, parts, before);
     n = __shfl(parts, b, 64);
     first = (int64_t)h * a.B * p.nsplit + __shfl(before, b, 64);
   }
@@ -185,7 +185,7 @@ hipError_t launch_tree(const TreeParams& q, hipStream_t st) {
   // 110 us (120 with as many parts a row), 32 rows over 16 contexts 283 (302).  Contexts of one length pay 1 to 2 us
   // for finding their part, so not for short ones, nor where few parts a row are dealt too coarsely (512 rows over
   // 8 contexts of 2 parts: 599 us, 541 with 2 for each).
-  p.even = !p.a.sparse && p.a.B > 1 && p.a.B <= 64 && p.nsplit >= 4 && p.nsplit <= 128 && max_frames(p.a) >= 32 * p.nsplit;
+  p.even = parts_by_length(p.a, p.nsplit);
   const size_t rows = (size_t)p.units * p.nsplit * p.a.N * p.a.G;
   p.part_o = p.part_ml + (rows * 2 * sizeof(float) + 255) / 256 * 256 / sizeof(float);
   // eight XCDs: a multiple of 8 workgroup slots (see tree_kernel)

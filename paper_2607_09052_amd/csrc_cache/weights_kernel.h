@@ -87,9 +87,20 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   __shared__ unsigned long long s_live[S::BUFS];                           // rows that add something
   __shared__ int red[4];
   const AttendParams& a = p.a;
-  const int h = blockIdx.x, b = blockIdx.y;
-  const int part = p.parts - 1 - (int)blockIdx.z;       // the draft's frames and the longer parts first
+  const int h = blockIdx.x;
+  int b = blockIdx.y, n_parts = p.parts;
+  int part = p.parts - 1 - (int)blockIdx.z;             // the draft's frames and the longer parts first
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), quad = lane >> 4;
+  if (p.even) {
+    int n, before;
+    row_parts(a, p.parts, n, before);
+    const int j = (int)blockIdx.y * p.parts + part;
+    const unsigned long long mine = __ballot(j >= before && j < before + n);
+    if (mine == 0) return;
+    b = __builtin_ctzll(mine);
+    part = j - __builtin_amdgcn_readlane(before, b);
+    n_parts = __builtin_amdgcn_readlane(n, b);
+  }
   const Attended x = attended<kWeightsThreads>(a, b, h, red);
   if (part < 0) {
     static_assert(kCopySpan / kFrame / 64 <= 2 * kStepTiles * 16, "the span's block bits fit s_bits");
@@ -97,7 +108,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     return;
   }
   const int nf = x.frames(), all = (nf + 4 * TF - 1) / (4 * TF);
-  const int pass0 = first_pass(all, part, p.parts), passes = first_pass(all, part + 1, p.parts) - pass0;
+  const int pass0 = first_pass(all, part, n_parts), passes = first_pass(all, part + 1, n_parts) - pass0;
   if (passes == 0) return;
   const int F0 = pass0 * 4 * TF;
   const int M = x.nq * a.G;
@@ -372,6 +383,9 @@ hipError_t launch_weights_kernels(WeightsParams p, hipStream_t st) {
   const int copies = p.a.sparse && p.prev != p.weights ? (p.a.tmax + kCopySpan - 1) / kCopySpan : 0;
   p.parts = parts_of((frames + PASS - 1) / PASS, units, steps == 1 ? 2.0 : steps * (F32 || !p.a.io_bf16 ? 6.0 : 3.0), 64 / TF, 32768,
                      units * copies / 2);
+  // (the longest row gets p.parts at least, another at least (p.parts - 1) / frames of them per frame: parts of some
+  // 28 passes stay below the 64 frames of a wave with the rounding of both)
+  p.even = parts_by_length(p.a, p.parts) && frames <= (int64_t)(TF == 2 ? 28 : 56) * PASS * (p.parts - 1);
   p.lg = p.a.G == 1 ? 0 : (p.a.G == 2 ? 1 : (p.a.G == 4 ? 2 : (p.a.G == 8 ? 3 : 4)));
   const dim3 grid(p.a.hkv, p.a.B, p.parts + copies), t(kWeightsThreads);
   if constexpr (F32) {
