@@ -55,8 +55,8 @@ size_t cobs_tree_workspace_bytes(const cobs_config_t* cfg, int32_t num_queries);
  *   ws:   cobs_tree_workspace_bytes(cfg, num_queries), 256-byte aligned.
  * Scores, softmax and sums are fp32.  With bf16 keys and values the matrix cores
  * take bf16 operands: an fp32 query and its probabilities enter as three bf16
- * parts, which hold all their bits; with io_dtype COBS_BF16 the probabilities are
- * rounded to bf16 once (2^-8), like the outputs.                                 */
+ * parts, which hold all their bits; with io_dtype COBS_BF16 the probabilities enter as
+ * two (2^-17) and the outputs are rounded once.                                   */
 cobs_status_t cobs_tree_decode(const cobs_config_t* cfg, const void* q, cobs_dtype_t io_dtype, int32_t num_queries,
                                const cobs_kv_t* kv, const int32_t* seq_lens, const int32_t* draft_lens,
                                const uint64_t* tree_mask, int32_t sparse, const int32_t* sel, void* out, float* lse,

@@ -149,8 +149,8 @@ void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit) {
   const int M = a.N * a.G;
   *wq = M <= 32 ? 1 : (M <= 64 ? 2 : 4);
   // Tiles of 256 rows (tree_wide.h) where they pad no more than tiles of 128 and a workgroup has some 64 frames
-  // or more (us with tiles of 128 and of 256: 512 rows over 8 x 32k tokens 675, 617; 256 rows over 32 x 4k 198, 187,
-  // over 32k 64, 66, over 16 x 2k 67, 68; 64-element heads 412, 414).
+  // or more (us with tiles of 128 and of 256: 512 rows over 8 x 32k tokens 873, 804; 256 rows over 32 x 4k 245, 233,
+  // over 32k 77, 77, over 16 x 2k 79, 80).
   const int64_t units = (int64_t)a.B * a.hkv, tiles = (M + 255) / 256;
   if (a.io_bf16 && !a.kv_f32 && a.d == 128 && (M + 127) / 128 == 2 * tiles && max_frames(a) * units * tiles >= 64 * 256) *wq = 8;
   *mtiles = (M + *wq * 32 - 1) / (*wq * 32);

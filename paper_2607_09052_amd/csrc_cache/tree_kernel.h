@@ -17,9 +17,9 @@
 //
 // Measured (d 128, bf16 cache): 16 rows of a batch of 32 over 85 selected blocks and a window of
 // 512, fp32 queries: 800 MB in 168 us, 4.8 TB/s, with three products for one (150 TFLOP in them)
-// near the matrix cores' bound too; 128 rows over 32k tokens, on pages: 4.0 TB/s; 512 rows over 32k
-// tokens: 0.55 TFLOP in 675 us, 815 TFLOP/s, the matrix cores busy 40 % of the
-// time and the exponentials' pipe as long, which overlap little with two waves a
+// near the matrix cores' bound too; 128 rows over 8k to 32k tokens, on pages: 411 MB in 129 us, 3.2 TB/s;
+// 512 rows over 8 x 32k tokens: 0.55 TFLOP (0.82 with the second part of the probabilities)
+// in 873 us, matrix instructions and softmax overlapping little with two waves a
 // SIMD (tree_wide.h has the form for such calls).  One short context: 9 us of
 // dependent loads, barriers and one pass.
 //
@@ -35,7 +35,10 @@
 // fp32 products run on 32x32x2 fp32 operands.  bf16 products take an fp32 query and
 // its probabilities as three bf16 parts, which hold all 24 bits (two leave 2^-17:
 // outputs 3.6e-6 off instead of 1e-6 at 32k tokens, and 4 to 20 % faster at up to
-// 64 rows); with bf16 outputs, whose rounding is 2^-8, one part.
+// 64 rows).  bf16 queries are one part, their probabilities two (2^-17, far below the outputs'
+// rounding of 2^-8; one, which rounds them by 2^-8 as well, left outputs 2.0e-3 to 2.4e-3 off in
+// relative norm instead of 1.7e-3, and took 610 us instead of 800 at 512 rows over 8 x 32k tokens,
+// 108 instead of 129 at 128 rows on pages, and the same time for few rows).
 //
 // Drafted tokens stand in the frames behind the context; what a query's mask
 // leaves out gets score -inf.  A value that is not finite would still reach every
@@ -168,6 +171,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
   using S = TreeShape<D, WQ, F32>;
   constexpr int WT = S::WT, CPR = S::CPR, LD = S::LD, NT = S::NT, FPI = S::FPI;
   constexpr int NDT = D / 32;
+  constexpr int PP = PARTS == 3 ? 3 : 2;                  // bf16 parts of a probability
   constexpr bool JOINT = FPI == 2 && PARTS == 1;          // a pass's frames at one maximum (three parts leave no registers for it)
   constexpr int NF = JOINT ? 2 : 1;
   __shared__ __align__(16) char pool[S::LDS];
@@ -400,11 +404,13 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
       } else {
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-          sbf16x8_t pb[PARTS];
+          sbf16x8_t pb[PP];
           float pv[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) pv[j] = s[fr][8 * ks + j];
-          split_bf16x8<PARTS>(pv, pb);
+          split_bf16x8<PP>(pv, pb);
+          // (not all of the frame's operands at once: four registers would spill)
+          if constexpr (D == 128 && WQ == 1 && PARTS == 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
             // tokens 16 ks + 4 half + 0..3 and 8 more on, columns 32 dt + lane % 32
@@ -415,7 +421,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
             typedef short s16x8_t __attribute__((ext_vector_type(8)));
             const s16x8_t vv = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-            for (int k = PARTS - 1; k >= 0; --k)
+            for (int k = PP - 1; k >= 0; --k)
               o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(sbf16x8_t, vv), pb[k], o[dt], 0, 0, 0);
           }
         }

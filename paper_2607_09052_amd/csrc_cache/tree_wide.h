@@ -8,10 +8,9 @@
 // next pass's keys and values go from registers to one of three LDS slots, and the
 // loads of the pass after it start, among the scores.
 //
-// Measured: 512 rows over 8 rows of 32k tokens (0.55 TFLOP) in 617 us, 890 TFLOP/s
-// (tree_kernel 675; the same 64 rows a wave without that order 914).  Without loads
-// and stores of the frames it takes 500 us: the writes to LDS, the barrier and the
-// loads' issue are what is left, 460 us are the product rate of a large plain product.
+// Measured: 512 rows over 8 rows of 32k tokens (0.55 TFLOP, 0.82 with the second part of the
+// probabilities) in 804 us (tree_kernel 873); 690 us are those products at the rate of a
+// large plain one.
 #pragma once
 
 #include "tree_kernel.h"
@@ -133,7 +132,7 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
   };
 
   f32x16_t s[QG];
-  sbf16x8_t pb[QG][2];
+  sbf16x8_t pb[QG][2][2];                                // operand of a step of 16 tokens, its two parts
   auto scores = [&](const char* fb, f32x16_t (&y)[QG]) {
     const char* const kf = fb + half * S::KSTEP + (lane & 31) * 16;
 #pragma unroll
@@ -163,7 +162,10 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
     for (int c = 0; c < 2 * NDT; ++c) {
       const sbf16x8_t v = value(fb, c);
 #pragma unroll
-      for (int g = 0; g < QG; ++g) o[g][c % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[g][c / NDT], o[g][c % NDT], 0, 0, 0);
+      for (int k = 1; k >= 0; --k)
+#pragma unroll
+        for (int g = 0; g < QG; ++g)
+          o[g][c % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pb[g][c / NDT][k], o[g][c % NDT], 0, 0, 0);
     }
   };
   // One frame: the values of the frame before (`vb`), the softmax of this one, the scores of the next (`kb`).
@@ -190,8 +192,10 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
         const sbf16x8_t cur = vv;
         if (c + 1 < NC) vv = value(vb, c + 1);
 #pragma unroll
-        for (int g = 0; g < QG; ++g)
-          o[g][c % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cur, pb[g][c / NDT], o[g][c % NDT], 0, 0, 0);
+        for (int k = 1; k >= 0; --k)
+#pragma unroll
+          for (int g = 0; g < QG; ++g)
+            o[g][c % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cur, pb[g][c / NDT][k], o[g][c % NDT], 0, 0, 0);
 #pragma unroll
         for (int i = c * PER; i < (c + 1) * PER; ++i) top[i / 16] = i % 16 == 0 ? s[i / 16][0] : fmaxf(top[i / 16], s[i / 16][i % 16]);
       }
@@ -241,11 +245,14 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
           e[i % 8] = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], c2, -mc[i / 16]));
           if (i % 4 == 3) l[i / 16] += (e[i % 8 - 3] + e[i % 8 - 2]) + (e[i % 8 - 1] + e[i % 8]);
           if (i % 8 == 7) {
-            sbf16x8_t w[1];
-            split_bf16x8<1>(e, w);
-            uint4 u = __builtin_bit_cast(uint4, w[0]);
-            asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));      // kept beside the products
-            pb[i / 16][i % 16 / 8] = __builtin_bit_cast(sbf16x8_t, u);
+            sbf16x8_t w[2];
+            split_bf16x8<2>(e, w);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              uint4 u = __builtin_bit_cast(uint4, w[k]);
+              asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));    // kept beside the products
+              pb[i / 16][i % 16 / 8][k] = __builtin_bit_cast(sbf16x8_t, u);
+            }
           }
         }
         if (ks == 0) {
@@ -295,7 +302,7 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
 #pragma unroll
     for (int g = 0; g < QG; ++g)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) pb[g][ks] = __builtin_bit_cast(sbf16x8_t, make_uint4(0, 0, 0, 0));
+      for (int ks = 0; ks < 2; ++ks) pb[g][ks][0] = pb[g][ks][1] = __builtin_bit_cast(sbf16x8_t, make_uint4(0, 0, 0, 0));
     int s0 = at_slot(0), s1 = at_slot(1), s2 = at_slot(2);              // this pass, the next, the one before
     for (int it = 0; it < passes; ++it) {
       frames_of(it + 2, after);
