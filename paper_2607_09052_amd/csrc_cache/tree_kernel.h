@@ -44,6 +44,9 @@
 // leaves out gets score -inf.  A value that is not finite would still reach every
 // row of the product as 0 times it, so such elements of drafted tokens enter LDS
 // as 0 and are added afterwards to the rows that see them (add_nonfinite).
+// In several parts an operand gives NaN with an infinite key or value (inf - inf, 0 inf)
+// where the operand itself gives an infinity: rows with NaN of a part that holds
+// infinities are computed once more, without parts (plain_rows).
 #pragma once
 
 #include "cache_device.h"
@@ -151,6 +154,117 @@ __device__ __forceinline__ void add_nonfinite(const AttendParams& a, const Atten
 // Partial of a split, per query row: (log2-domain maximum, sum) and D unnormalised outputs.
 __device__ __forceinline__ int64_t part_row(const TreeParams& p, const TreePart& t, int r) {
   return (t.first + t.split) * (p.a.N * p.a.G) + r;
+}
+
+// Whether one of the five is NaN (or there are infinities of both signs).
+__device__ __forceinline__ bool has_nan(float4 y, float total) {
+  const float z = ((y.x + y.y) + (y.z + y.w)) + total;
+  return z != z;
+}
+
+// Whether one of 8 bf16 values is an infinity.
+__device__ __forceinline__ bool has_infinity(uint4 x) {
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = i == 0 ? x.x : (i == 1 ? x.y : (i == 2 ? x.z : x.w));
+    found |= (w & 0x7fffu) == 0x7f80u || (w & 0x7fff0000u) == 0x7f800000u;
+  }
+  return found;
+}
+
+// Query rows of the wave's outputs again (bit k of a lane's `nan`: its outputs of the pass k have NaN), if the
+// frames f_lo .. f_hi - 1 of the part (bf16) hold an infinity: scores, softmax and sums element by
+// element in fp32, from memory, a row at a time.  row_of(k, thread) is the row of a thread's outputs.
+// Rare, so only right: one infinite value in one of 32 contexts of 32k tokens, 32 rows each: 4.9 ms for 0.11.
+template <int D, typename RowOf>
+__device__ __forceinline__ void plain_rows(const TreeParams& p, const Attended& x, const TreePart& part, int f_lo, int f_hi,
+                                           uint32_t nan, RowOf row_of) {
+  constexpr int CPR = D / 8, COLS = D / 64, TPR = D / 4;
+  const AttendParams& a = p.a;
+  const int b = part.b, h = part.h, lane = threadIdx.x & 63, half = lane >> 5;
+  const int64_t rs = a.kv.table ? a.kv.d : a.kv.st;
+  const uint16_t* const kp = static_cast<const uint16_t*>(a.kv.k);
+  const uint16_t* const vp = static_cast<const uint16_t*>(a.kv.v);
+  bool found = false;
+  for (int f = f_lo; f < f_hi; ++f) {
+    int fa, lo, hi;
+    x.frame(f, fa, lo, hi);
+    const int64_t base = lo < hi ? kv_offset(a.kv, b, h, fa) : -1;
+    if (base < 0) continue;
+#pragma unroll 4
+    for (int i = lane; i < (hi - lo) * CPR; i += 64) {
+      const int64_t at = base + (lo - fa + i / CPR) * rs + 8 * (i % CPR);
+      const uint4 k = *reinterpret_cast<const uint4*>(kp + at), v = *reinterpret_cast<const uint4*>(vp + at);
+      found |= has_infinity(k);
+      found |= has_infinity(v);
+    }
+  }
+  if (!__ballot(found)) return;
+  __threadfence_block();                                     // what is read back below is written
+  const float c2 = a.c * 1.4426950408889634f;
+  for (int w = 0; w < 32 * 64 / TPR; ++w) {                    // passes, and rows of the wave in a pass
+    const int k = w / (64 / TPR), first = w % (64 / TPR) * TPR;
+    if (!((__ballot((nan >> k) & 1) >> first) & (TPR == 32 ? 0xffffffffull : 0xffffull))) continue;
+    const int row = wave_uniform32(row_of(k, (threadIdx.x & ~63) + first));
+    const QueryRow q = query_row(a, b, h, row);
+    float m = -INFINITY, l = 0.0f, o[COLS] = {};
+    for (int f = f_lo; f < f_hi; ++f) {
+      int fa, lo, hi;
+      x.frame(f, fa, lo, hi);
+      const int64_t base = lo < hi ? kv_offset(a.kv, b, h, fa) : -1;
+      if (base < 0) continue;
+      // lane l: token l % 32, half the elements
+      const int t = fa + (lane & 31);
+      const bool see = t >= lo && t < hi && (t < x.C || ((q.bits >> (t - x.C)) & 1));
+      float s = 0.0f;
+      if (see)
+        for (int e = half * (D / 2); e < (half + 1) * (D / 2); ++e)
+          s = fmaf(load_elem(a.q, q.at * D + e, !a.io_bf16), load_elem(kp, base + (lane & 31) * rs + e, false), s);
+      s += other_half(s);
+      float top = see ? s : -INFINITY;
+#pragma unroll
+      for (int k = 16; k >= 1; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
+      const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn, alpha = __builtin_amdgcn_exp2f((m - ref) * c2);
+      const float pr = see ? __builtin_amdgcn_exp2f((s - ref) * c2) : 0.0f;
+      m = mn;
+      float sum = pr;
+#pragma unroll
+      for (int k = 16; k >= 1; k >>= 1) sum += __shfl_xor(sum, k, 64);
+      l = fmaf(l, alpha, sum);
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) o[j] *= alpha;
+      uint32_t seen = (uint32_t)__ballot(see);               // (both halves alike)
+      while (seen) {
+        const int k = __builtin_ctz(seen);
+        seen &= seen - 1;
+        const float pk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pr), k));
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) o[j] = fmaf(pk, load_elem(vp, base + k * rs + COLS * lane + j, false), o[j]);
+      }
+    }
+    // in the place of what is NaN (a score: all of the row; a value: its column, at the maximum that the others have)
+    if (p.nsplit > 1) {
+      const int64_t at = part_row(p, part, row);
+      float2* const ml = reinterpret_cast<float2*>(p.part_ml + 2 * at);
+      const bool all = ml->y != ml->y;
+      const float f = all ? 1.0f : __builtin_amdgcn_exp2f(m * c2 - ml->x);
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) {
+        float& y = p.part_o[at * D + COLS * lane + j];
+        if (all || y != y) y = o[j] * f;
+      }
+      if (all && lane == 0) *ml = make_float2(m * c2, l);
+    } else {
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) {
+        const int64_t at = q.at * D + COLS * lane + j;
+        const float y = load_elem(p.out, at, !a.io_bf16);
+        if (y != y) store_elem(p.out, at, l != 0.0f ? o[j] / l : 0.0f, !a.io_bf16);
+      }
+      if (lane == 0 && p.lse && p.lse[q.at] != p.lse[q.at]) p.lse[q.at] = l != 0.0f ? m * a.c + logf(l) : -INFINITY;
+    }
+  }
 }
 
 // Outputs 0 and lse -inf for the rows of a tile that belong to no live query.
@@ -508,6 +622,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
           make_float4(o[dt][i] * scale, o[dt][i + 1] * scale, o[dt][i + 2] * scale, o[dt][i + 3] * scale);
     }
   __syncthreads();
+  uint32_t nan = 0;                                     // (a bit a pass)
   for (int idx = tid; idx < WQ * 32 * (D / 4); idx += kTreeThreads) {
     const int rr = idx / (D / 4), d4 = idx % (D / 4), w = rr / 32, r = rr % 32;
     const int row = mt * WQ * 32 + rr;
@@ -524,6 +639,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
                                                         4 * (d4 ^ (r & (D / 4 - 1))));
       sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
     }
+    if (!F32 && has_nan(sum, ll)) nan |= 1u << (idx / kTreeThreads);
     if (p.nsplit == 1) {
       const int i = row / a.G;
       const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
@@ -534,6 +650,10 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
       *reinterpret_cast<float4*>(p.part_o + at * D + 4 * d4) = sum;
       if (d4 == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(mm * c2, ll);
     }
+  }
+  if constexpr (!F32) {
+    if (__builtin_expect(__ballot(nan != 0) != 0, 0))
+      plain_rows<D>(p, x, part, f_lo, f_hi, nan, [&](int k, int t) { return mt * WQ * 32 + (k * kTreeThreads + t) / (D / 4); });
   }
 }
 

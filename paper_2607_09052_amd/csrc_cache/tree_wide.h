@@ -326,6 +326,9 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
 #pragma unroll
     for (int g = 0; g < QG; ++g) add_nonfinite<D, false>(a, x, b, h, q[g], s_bad, m[g] == -INFINITY ? 0.0f : m[g], c2, o[g]);
   }
+  constexpr int PASSES = 4 * 32 * (D / 4) / kTreeThreads;
+  static_assert(QG * PASSES <= 32, "a bit a pass");
+  uint32_t nan = 0;
 #pragma unroll
   for (int g = 0; g < QG; ++g) {
     if (g > 0) __syncthreads();
@@ -347,6 +350,7 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
       if (row >= x.nq * a.G) continue;
       const float mm = s_m[w][r], ll = s_l[w][r], rm = mm == -INFINITY ? 0.0f : mm;
       const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<float*>(pool) + (w * 32 + r) * D + 4 * (d4 ^ (r & (D / 4 - 1))));
+      if (has_nan(y, ll)) nan |= 1u << (g * PASSES + idx / kTreeThreads);
       if (p.nsplit == 1) {
         const int i = row / a.G;
         const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
@@ -359,6 +363,11 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
       }
     }
   }
+  if (__builtin_expect(__ballot(nan != 0) != 0, 0))
+    plain_rows<D>(p, x, part, f_lo, f_hi, nan, [&](int k, int t) {
+      const int rr = (k % PASSES * kTreeThreads + t) / (D / 4);
+      return mt * kWideRows + (rr / 32 * QG + k / PASSES) * 32 + rr % 32;
+    });
 }
 
 }  // namespace cobs

@@ -55,3 +55,71 @@ def test_bf16_outputs_are_rounded_once(shape):
                 worst = max(worst, float((off / tol).max()))
     say(f"worst error / tolerance {worst:.3f}")
     assert worst <= 1.0
+
+
+def _check_any(p, out, lse):
+    """Outputs and normalisers that need not be finite: the same infinities and NaN as the definition, and finite ones
+    within check_tree's tolerance (its errors over the finite keys, as an infinite one's score is exact, and bf16 queries'
+    probabilities as above)."""
+    got, gl = f64(out), f64(lse)
+    for b in range(p.B):
+        for h in range(p.Hkv):
+            q, K, V, see = p.unit(b, h)
+            with np.errstate(all="ignore"):
+                want, wl = O.tree_attention(q, K, V, see, p.cfg.scale)
+            finite = np.isfinite(K).all(1)
+            e = p.score_error(q, np.where(finite[:, None], K, 0.0), see & finite)
+            for i in range(p.N):
+                t = np.nonzero(see[i] & finite)[0]
+                g, z = got[b, i, h * p.G:(h + 1) * p.G], gl[b, i, h * p.G:(h + 1) * p.G]
+                assert np.array_equal(np.isnan(g), np.isnan(want[i])), (b, h, i)
+                assert np.array_equal(np.isnan(z), np.isnan(wl[i])), (b, h, i, z, wl[i])
+                big = np.isinf(want[i])
+                assert np.array_equal(g[big], want[i][big]), (b, h, i)
+                with np.errstate(all="ignore"):
+                    prob = np.exp(p.cfg.scale * (q[i] @ K[t].T) - wl[i][:, None])
+                    mass = prob @ np.where(np.isfinite(V[t]), np.abs(V[t]), 0.0)
+                    sums = (8 + 4 * np.sqrt(len(t))) * U32
+                    rnd = 2.0 ** -16 if p.kv == "bf16" and p.io == "bf16" else 0.0
+                    tol = mass * (2 * e[i][:, None] + rnd + 2 * sums) + HALF[p.io] * np.abs(want[i]) * 1.01 + 1e-30
+                    off, zoff = np.abs(g - want[i]), np.abs(z - wl[i])
+                    ok = np.isfinite(want[i])
+                    assert np.all(off[ok] <= tol[ok]), (b, h, i, float((off[ok] / tol[ok]).max()))
+                    fin = np.isfinite(wl[i])
+                    ltol = e[i] + sums + np.abs(wl[i]) * 2 * U32
+                    assert np.all(zoff[fin] <= ltol[fin]), (b, h, i, zoff, ltol)
+
+
+@pytest.mark.parametrize("kv,io", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("shape", FORMS, ids=_ids)
+def test_infinite_keys_and_values_where_queries_look(shape, kv, io):
+    """Element 0 of every query is positive.  A key with -inf there has score -inf: its token is as if it were not
+    attended to.  One with +inf makes every output of its head NaN.  A value reaches the outputs as probability times value."""
+    if shape.get("extra") and io != "bf16":
+        shape = dict(shape, Hkv=1, extra=0)
+    say(f"infinities {shape} {kv} {io}")
+    p = Problem(DEV, kv=kv, io=io, seed=5, **shape)
+    p.q[..., 0] = p.q[..., 0].abs() + 0.25
+    last = p.T[0] - 1                                         # (in the window, where there is one)
+    p.k[0, :, last - 20, 0] = -INF
+    p.v[0, :, last - 33, 3], p.v[0, :, last - 1, 4] = INF, -INF
+    p.v[0, :, last - 33, 5], p.v[0, :, last - 1, 5] = INF, -INF
+    p.v[0, :, last - 7, 6] = NAN
+    p.k[0, :, p.T[0] + 1, 0] = -INF                           # drafted token 1
+    p.v[0, :, p.T[0], 7] = INF
+    p.k[1, 0, p.T[1] - 2, 0] = INF
+    out, lse = run_tree(p.upload())
+    sync()
+    _check_any(p, out, lse)
+
+
+def test_a_query_that_is_not_a_number_stays_by_itself():
+    """NaN and infinities in one query's elements reach its own outputs alone."""
+    for io in ("f32", "bf16"):
+        p, clean = (Problem(DEV, T=(300, 90), N=5, io=io).upload() for _ in range(2))
+        p.qd[0, 2, 3, 7], p.qd[1, 4, 6, 0] = NAN, INF
+        (out, lse), (want, wl) = run_tree(p), run_tree(clean)
+        for b, i, head in ((0, 2, 3), (1, 4, 6)):
+            assert bool(out[b, i, head].isnan().all()) and bool(lse[b, i, head].isnan())
+            out[b, i, head], lse[b, i, head] = want[b, i, head], wl[b, i, head]
+        assert torch.equal(out, want) and torch.equal(lse, wl)
