@@ -31,8 +31,8 @@
  *     attend to the context alone.  One query is then cobs_sparse_decode.
  * A token that a query does not attend to has no effect on it, whatever its key
  * and value hold; one that it attends to acts as in plain arithmetic (with a score of
- * -inf its probability is 0, an infinite value is one in the output).  A context with
- * infinities may take a hundred times as long.  Tokens on a page whose id is out of range are left out.
+ * -inf its probability is 0, an infinite value is one in the output).  Infinities there
+ * may make a call take a hundred times as long.  Tokens on a page whose id is out of range are left out.
  */
 #ifndef COBS_CACHE_H
 #define COBS_CACHE_H
@@ -71,7 +71,7 @@ cobs_status_t cobs_tree_decode(const cobs_config_t* cfg, const void* q, cobs_dty
  *   q, num_queries, io_dtype, kv, ..., sel: as for cobs_tree_decode (V is not read).
  *   lse:     device fp32 [B, num_queries, Hq]: the queries' normalisers, as cobs_tree_decode
  *            or a decode step returns them.  A query head with lse -inf or +inf adds nothing
- *            (+inf leaves a rejected drafted token out).
+ *            (+inf leaves a rejected drafted token out), whatever its query holds.
  *   prev:    optional device fp32 [B, Hkv, max_seq_len], NULL for zeros; `weights` itself, or apart.
  *   weights: device fp32 [B, Hkv, max_seq_len].                                     */
 cobs_status_t cobs_attention_weights(const cobs_config_t* cfg, const void* q, cobs_dtype_t io_dtype,

@@ -53,8 +53,8 @@ def tree_attention(q, K, V, see, c):
 def attention_weights(q, K, see, lse, c):
     """Sum over queries and heads of exp(c q.k - lse) per token [tokens]; a head whose lse is infinite adds nothing."""
     s = _scores(q, K, see, c)
-    z = np.where(np.isinf(lse), np.inf, lse)
-    return np.where(see[:, None, :], np.exp(s - z[:, :, None]), 0.0).sum((0, 1))
+    adds = see[:, None, :] & ~np.isinf(lse)[:, :, None]      # (inf - inf of a key's infinity is no term either)
+    return np.exp(np.where(adds, s - np.where(np.isinf(lse), 0.0, lse)[:, :, None], -np.inf)).sum((0, 1))
 
 
 def evict(weights, T, keep, sinks, recent):

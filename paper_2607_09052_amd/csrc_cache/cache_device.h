@@ -160,6 +160,15 @@ __device__ __forceinline__ void store_row4(void* out, int64_t i, float4 sum, flo
   }
 }
 
+// The kernel's parameter block (its only argument) as it stands in memory: what a rare path at a kernel's end reads from
+// there takes no scalar registers before.
+template <typename P>
+__device__ __forceinline__ const P& kernel_params() {
+  uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return *reinterpret_cast<const P*>(at);
+}
+
 __device__ __forceinline__ float load_elem(const void* p, int64_t i, bool f32) {
   if (f32) return static_cast<const float*>(p)[i];
   return bf16_lo((uint32_t) static_cast<const uint16_t*>(p)[i]);

@@ -76,6 +76,53 @@ __device__ __forceinline__ void copy_weights(const WeightsParams& p, const Atten
   }
 }
 
+// The tokens whose sums came out NaN (bit k of a lane's `again`: its token of pass k, in the frame that lane k TF of the wave
+// holds), from memory and element by element.  NaN is right of a key with NaN, or of a query that adds.  But rows
+// that add nothing take part in the products, with terms exp2(c2 s - inf) that are NaN where s is: with an infinity in the
+// key (a row that fills a tile up is zeros) or in such a row's query; and with an infinite key the lower bf16
+// parts of a query make NaN.  Rare, so only right; what it needs of the workgroup comes from memory and LDS, as
+// scalar registers kept for it through the kernel cost 64 rows of fp32 queries over 8 x 32k tokens 131 us instead of 126.
+struct WeightsUnit {
+  int b, h, C, nq, passes;
+};
+template <int D, bool F32, int TF>
+__device__ __forceinline__ void weigh_again(unsigned long long again, int my_a, int64_t my_base, const WeightsUnit& unit) {
+  const WeightsParams& p = kernel_params<WeightsParams>();
+  const AttendParams& a = p.a;
+  const int b = unit.b, h = unit.h, C = unit.C, nq = unit.nq, passes = unit.passes;
+  const int lane = threadIdx.x & 63;
+  const float c2 = a.c * 1.4426950408889634f;
+  auto row_of = [&](int r) { return ((int64_t)b * a.N + r / a.G) * a.hq + h * a.G + r % a.G; };
+  bool odd = false;                                      // whether a row that adds nothing has a query that is not finite
+  for (int r = lane; r < nq * a.G; r += 64)
+    if (fabsf(p.lse[row_of(r)]) == INFINITY)
+      for (int e = 0; e < D; ++e) odd |= !(fabsf(load_elem(a.q, row_of(r) * D + e, !a.io_bf16)) < INFINITY);
+  odd = __ballot(odd) != 0;
+  for (int ps = 0; ps < passes; ++ps) {
+    const int mine = ps * TF + (TF == 2 ? lane >> 5 : 0);
+    const int t = __shfl(my_a, mine, 64) + (lane & 31);
+    const int64_t at = __shfl(my_base, mine, 64) + (lane & 31) * (a.kv.table ? (int64_t)a.kv.d : a.kv.st);
+    if (!((again >> ps) & 1)) continue;
+    bool infinite = false, nan = false;
+    for (int e = 0; e < D; ++e) {
+      const float k = load_elem(a.kv.k, at + e, F32);
+      infinite |= fabsf(k) == INFINITY;
+      nan |= k != k;
+    }
+    float sum = nan || !(infinite || odd) ? NAN : 0.0f;
+    for (int r = 0; r < nq * a.G && sum == sum; ++r) {
+      const int64_t row = row_of(r);
+      const float z = p.lse[row];
+      if (fabsf(z) == INFINITY || (t >= C && !((a.mask[(int64_t)b * a.N + r / a.G] >> (t - C)) & 1))) continue;
+      float s = 0.0f;
+      for (int e = 0; e < D; ++e) s = fmaf(load_elem(a.q, row * D + e, !a.io_bf16), load_elem(a.kv.k, at + e, F32), s);
+      sum += __builtin_amdgcn_exp2f(fmaf(s, c2, -z * 1.4426950408889634f));
+    }
+    const int64_t w = ((int64_t)b * a.hkv + h) * a.tmax + t;
+    p.weights[w] = (p.prev ? p.prev[w] : 0.0f) + sum;
+  }
+}
+
 template <int D, bool F32, int PARTS>
 __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsParams p) {
   using S = WeightsShape<D, F32, PARTS>;
@@ -86,6 +133,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   __shared__ __align__(16) unsigned long long s_bits[S::BUFS][kStepTiles * 16];
   __shared__ unsigned long long s_live[S::BUFS];                           // rows that add something
   __shared__ int red[4];
+  __shared__ WeightsUnit s_unit;
   const AttendParams& a = p.a;
   const int h = blockIdx.x;
   int b = blockIdx.y, n_parts = p.parts;
@@ -110,6 +158,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   const int nf = x.frames(), all = (nf + 4 * TF - 1) / (4 * TF);
   const int pass0 = first_pass(all, part, n_parts), passes = first_pass(all, part + 1, n_parts) - pass0;
   if (passes == 0) return;
+  if (tid == 0) s_unit = {b, h, x.C, x.nq, passes};          // (read behind the barrier of the first rows)
   const int F0 = pass0 * 4 * TF;
   const int M = x.nq * a.G;
   const float c2 = a.c * 1.4426950408889634f;
@@ -231,6 +280,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     if (steps > 1) fetch(1);
     __syncthreads();
   }
+  unsigned long long again = 0;                                              // passes in which the lane's sum is NaN
   int n = 0;                                                                 // steps done
   for (int ps = 0; ps < passes; ++ps) {
     uint4 kc[TG][KS];
@@ -258,8 +308,6 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
     for (int st = 0; st < steps; ++st, ++n) {
       const int buf = resident ? st : (n & 1);
       const bool more = resident ? ps == 0 && st + 1 < steps : st + 1 < steps || ps + 1 < passes;
-      // A step whose rows all add nothing is left out, so that it adds no NaN either (in a live one every token
-      // of the context is attended to by some row).
       if (any && s_live[buf] != 0) {
         auto scores = [&](int tl, f32x4w_t (&sc)[TG]) {
           const char* qt = tiles + buf * S::STEP + tl * S::TILE;
@@ -366,8 +414,14 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
       v += other_half(v);
       if (quad == g) total = good[g / 2] ? v : 0.0f;
     }
-    if (writes) p.weights[wrow + fa + r32] = prev + total;
+    if (total == total) {
+      if (writes) p.weights[wrow + fa + r32] = prev + total;
+    } else if (writes) {
+      again |= 1ull << ps;
+    }
   }
+  if (__builtin_expect(__ballot(again != 0) != 0, 0))
+    weigh_again<D, F32, TF>(again, my_a, my_base, s_unit);
 }
 
 template <int D, bool F32>

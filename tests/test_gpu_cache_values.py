@@ -123,3 +123,63 @@ def test_a_query_that_is_not_a_number_stays_by_itself():
             assert bool(out[b, i, head].isnan().all()) and bool(lse[b, i, head].isnan())
             out[b, i, head], lse[b, i, head] = want[b, i, head], wl[b, i, head]
         assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+WEIGHT_ROWS = [
+    dict(T=(300, 77), N=1, G=4), dict(T=(300, 77), N=5, G=4), dict(T=(200, 64), N=16, G=4), dict(T=(200, 90), N=3, G=1, d=64),
+    dict(T=(700, 130), N=64, G=4), dict(T=(150, 90), N=9, G=16), dict(T=(150, 90), N=40, G=8), dict(T=(900, 333), N=7, G=2, s=3, w=100),
+    dict(T=(300, 77), N=1, G=4, draft=False), dict(T=(500, 250), N=20, G=2, layout="pages", d=64),
+]
+
+
+@pytest.mark.parametrize("dead", ["some", "none", "all"])
+@pytest.mark.parametrize("kv,io", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("shape", WEIGHT_ROWS, ids=_ids)
+def test_weights_of_infinite_keys_and_of_heads_that_add_nothing(shape, kv, io, dead):
+    """Keys of score -inf add 0, of +inf infinity, NaN ones NaN; a head with an infinite lse adds nothing to any of
+    them, whatever its query holds."""
+    say(f"weights, infinities {shape} {kv} {io} {dead}")
+    p = Problem(DEV, kv=kv, io=io, seed=6, **shape)
+    g = torch.Generator().manual_seed(7)
+    p.q[..., 0] = p.q[..., 0].abs() + 0.25
+    lse = 5.0 + torch.rand((p.B, p.N, p.Hkv * p.G), generator=g)
+    if dead == "some":
+        gone = torch.rand(lse.shape, generator=g) < 0.3
+        gone[:, 0, 0], gone[:, 0, -1] = True, True
+        lse[gone] = torch.where(torch.rand(lse.shape, generator=g) < 0.5, INF, -INF)[gone]
+        p.q[0, 0, 0], p.q[1, 0, -1, 3] = NAN, INF                 # queries of heads that add nothing
+    elif dead == "all":
+        lse[:] = INF
+        lse[:, ::2] = -INF
+        p.q[1, 0, 0] = NAN
+    for b in range(2):
+        last = p.T[b] - 1
+        p.k[b, :, last - 20, 0], p.k[b, :, last - 30, 0], p.k[b, :, last - 40, 5] = -INF, INF, NAN
+        if p.n[b] > 1:
+            p.k[b, :, p.T[b] + 1, 0] = -INF
+    prev = torch.rand((p.B, p.Hkv, p.cap), generator=g).to(DEV)
+    z = lse.to(DEV)
+    got = f64(run_weights(p.upload(), z, torch.zeros_like(prev), prev))
+    sync()
+    lse = f64(lse).reshape(p.B, p.N, p.Hkv, p.G)
+    for b in range(p.B):
+        E = p.T[b] + p.n[b]
+        for h in range(p.Hkv):
+            q, K, _, see = p.unit(b, h)
+            live = np.isfinite(lse[b, :, h])
+            add = np.zeros(E)
+            with np.errstate(all="ignore"):
+                for i in range(p.N):
+                    for j in range(p.G):
+                        if live[i, j]:
+                            s = p.cfg.scale * (K @ q[i, j])
+                            add += np.where(see[i], np.exp(np.where(see[i], s, 0.0) - lse[b, i, h, j]), 0.0)
+            finite, sure = np.isfinite(K).all(1), np.where(np.isfinite(q).all(-1, keepdims=True), q, 0.0)
+            e = p.score_error(sure, np.where(finite[:, None], K, 0.0), see & finite).max() + 2.0 ** -17
+            want = f64(prev)[b, h, :E] + add
+            assert np.array_equal(np.isnan(got[b, h, :E]), np.isnan(want)), (b, h, np.nonzero(np.isnan(got[b, h, :E]) != np.isnan(want)))
+            big = np.isinf(want)
+            assert np.array_equal(got[b, h, :E][big], want[big])
+            ok = np.isfinite(want)
+            tol = add[ok] * (e + (8 + 4 * np.sqrt(p.N * p.G)) * U32) + np.abs(want[ok]) * 2 * U32 + 1e-37
+            assert np.all(np.abs(got[b, h, :E][ok] - want[ok]) <= tol), (b, h)
