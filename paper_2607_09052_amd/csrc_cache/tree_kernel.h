@@ -108,6 +108,10 @@ __device__ __forceinline__ uint4 finite_only(uint4 x, bool& found) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// By how much a score may pass the running maximum: 2^8 in the probabilities.  (Finite at the smallest scales,
+// where 8 / c2 overflows, as -inf + inf would let no score become the maximum.)
+__device__ __forceinline__ float max_slack(float c2) { return fminf(8.0f / c2, 3.4028234e38f); }
+
 // The rows of a wave: query row `r` of the M = N G of a (row, KV head), or none.  The
 // rows of padded queries are read like the others, which needs no row length (their
 // columns of the products are computed and left).
@@ -310,7 +314,7 @@ __global__ __launch_bounds__(kTreeThreads, F32 || (PARTS == 3 && D == 128 && WQ 
   const int tg = wave / WQ, wq = wave % WQ, half = lane >> 5, gt = tid % NT;
   const int row0 = (mt * WQ + wq) * 32;                         // the wave's query rows
   const QueryRow q = query_row(a, b, h, row0 + (lane & 31));
-  const float c2 = a.c * 1.4426950408889634f, slack = 8.0f / c2;
+  const float c2 = a.c * 1.4426950408889634f, slack = max_slack(c2);
   if (tid < WT) s_bad[tid] = 0;
 
   // ---- the query rows as the B operand: column lane % 32, k = 8 half + j of every step

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kTreeThreads, 1) void tree_wide_kernel(TreeParams p
   QueryRow q[QG];
 #pragma unroll
   for (int g = 0; g < QG; ++g) q[g] = query_row(a, b, h, mt * kWideRows + (wave * QG + g) * 32 + (lane & 31));
-  const float c2 = a.c * 1.4426950408889634f, slack = 8.0f / c2;
+  const float c2 = a.c * 1.4426950408889634f, slack = max_slack(c2);
   if (tid == 0) s_bad = 0;
   sbf16x8_t qb[QG][QK];
 #pragma unroll

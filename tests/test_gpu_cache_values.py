@@ -183,3 +183,14 @@ def test_weights_of_infinite_keys_and_of_heads_that_add_nothing(shape, kv, io, d
             ok = np.isfinite(want)
             tol = add[ok] * (e + (8 + 4 * np.sqrt(p.N * p.G)) * U32) + np.abs(want[ok]) * 2 * U32 + 1e-37
             assert np.all(np.abs(got[b, h, :E][ok] - want[ok]) <= tol), (b, h)
+
+
+@pytest.mark.parametrize("c", [1e-30, 1.6e-38, 1e-38, 1e-44])
+@pytest.mark.parametrize("shape", [FORMS[i] for i in (0, 1, 3, 4, 7)], ids=_ids)
+def test_the_smallest_scales_average(shape, c):
+    """Any positive scale is taken: at these every token has the same weight."""
+    for io in ("bf16", "f32") if not shape.get("extra") else ("bf16",):
+        p = Problem(DEV, io=io, c=c, **shape).upload()
+        out, lse = run_tree(p)
+        sync()
+        p.check_tree(out, lse)
