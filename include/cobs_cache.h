@@ -7,7 +7,9 @@
  *
  * The conventions of cobs.h hold: device pointers that the caller owns, host
  * validation before any launch, asynchronous work on `stream` (of the current
- * device), no allocation, no state between calls, deterministic results.  Of
+ * device), no allocation, no state between calls, deterministic results (the
+ * same call gives the same bits; the order in which a row's attention is summed
+ * may go by the lengths of the batch's other rows).  Of
  * cobs_config_t these calls read batch, num_q_heads, num_kv_heads, head_dim,
  * max_seq_len, block_size, budget, window, kv_dtype and softmax_scale, with the
  * same limits as there; the record fields are ignored.

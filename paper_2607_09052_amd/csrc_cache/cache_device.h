@@ -75,9 +75,10 @@ __device__ __forceinline__ Attended attended(const AttendParams& p, int b, int h
 }
 
 // Parts that the rows' contexts are split into, where the `parts` B parts of a KV head go to the rows by
-// their frames: lane b has those of row b and of the rows before it.  (Alike in every kernel of a call; all
-// lanes active.)
-__device__ __forceinline__ void row_parts(const AttendParams& a, int parts, int& n, int& before) {
+// their frames, at most one for each `step` frames of a row (its passes: a part without one would write and be joined
+// for nothing): lane b has those of row b and of the rows before it.  So a row's parts, and the order
+// of its sums, go by the other rows' lengths too.  (Alike in every kernel of a call; all lanes active.)
+__device__ __forceinline__ void row_parts(const AttendParams& a, int parts, int step, int& n, int& before) {
   const int b = threadIdx.x & 63;
   uint32_t frames = 0;
   if (b < a.B) {
@@ -87,7 +88,8 @@ __device__ __forceinline__ void row_parts(const AttendParams& a, int parts, int&
   }
   const uint32_t all = (uint32_t)__builtin_amdgcn_readlane(wave_incl_scan((int)frames), 63);
   // (at most 64 rows of 128 parts and 2^15 frames: below 2^32)
-  n = b < a.B ? 1 + (int)((uint32_t)(a.B * (parts - 1)) * frames / max(all, 1u)) : 0;
+  n = 1 + (int)((uint32_t)(a.B * (parts - 1)) * frames / max(all, 1u));
+  n = b < a.B ? min(n, max(1, (int)(frames + step - 1) / step)) : 0;
   before = wave_incl_scan(n) - n;
 }
 
@@ -107,7 +109,7 @@ __device__ __forceinline__ bool tree_part(const TreeParams& p, int group, TreePa
     return true;
   }
   int n, before;
-  row_parts(p.a, p.nsplit, n, before);
+  row_parts(p.a, p.nsplit, p.step, n, before);
   t.h = group % hkv;
   const int j = group / hkv;
   const unsigned long long mine = __ballot(j >= before && j < before + n);

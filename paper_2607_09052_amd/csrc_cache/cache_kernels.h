@@ -69,7 +69,7 @@ struct TreeParams {
   float* part_ml;
   float* part_o;
   int units, mtiles, nsplit;    // (row, KV head) pairs, query row tiles, splits
-  int even;                     // whether rows get parts by their length (row_parts)
+  int even, step;               // whether rows get parts by their length (row_parts); frames of a workgroup's pass
 };
 
 struct WeightsParams {
@@ -109,8 +109,7 @@ struct CompactParams {
   int per_head, num_kept, B, hkv, d, tmax, dst_max, kv_f32, in_place;
 };
 
-// Row tiles and splits of a call, from its shape alone (so that a workspace's size
-// and a result's bits depend on nothing else).
+// Row tiles and splits of a call, from its shape alone (so that a workspace's size depends on nothing else).
 void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit);
 size_t tree_workspace(const AttendParams& a);
 hipError_t launch_tree(const TreeParams& p, hipStream_t st);

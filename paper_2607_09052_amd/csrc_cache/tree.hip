@@ -22,7 +22,7 @@ __device__ __forceinline__ MergeRow merge_row(const TreeParams& p, uint32_t idx)
   int64_t first = (int64_t)unit * p.nsplit;
   if (p.even) {
     int parts, before;
-    row_parts(a, p.nsplit, parts, before);
+    row_parts(a, p.nsplit, p.step, parts, before);
     n = __shfl(parts, b, 64);
     first = (int64_t)h * a.B * p.nsplit + __shfl(before, b, 64);
   }
@@ -145,6 +145,9 @@ hipError_t launch_tree_bf16_d128(const TreeParams& p, int wq, int grid, hipStrea
 hipError_t launch_tree_f32_d64(const TreeParams& p, int wq, int grid, hipStream_t st);
 hipError_t launch_tree_f32_d128(const TreeParams& p, int wq, int grid, hipStream_t st);
 
+// Frames of a pass of a workgroup's waves (STEP of the kernels).
+static int pass_frames(const AttendParams& a, int wq) { return wq == 1 ? 4 : (wq == 2 || !a.kv_f32 ? 2 : 1); }
+
 void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit) {
   const int M = a.N * a.G;
   *wq = M <= 32 ? 1 : (M <= 64 ? 2 : 4);
@@ -155,7 +158,7 @@ void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit) {
   if (a.io_bf16 && !a.kv_f32 && a.d == 128 && (M + 127) / 128 == 2 * tiles && max_frames(a) * units * tiles >= 64 * 256) *wq = 8;
   *mtiles = (M + *wq * 32 - 1) / (*wq * 32);
   // the longest row's frames, by a pass of a workgroup's waves at a time
-  const int step = *wq == 1 ? 4 : (*wq == 2 || !a.kv_f32 ? 2 : 1);
+  const int step = pass_frames(a, *wq);
   const int64_t passes = (max_frames(a) + step - 1) / step;
   *nsplit = parts_of(passes, units * *mtiles, *wq == 8 ? 1.0 : 2.0, 1 << 30, 128, 0, *wq == 8 ? 256 : 512);
 }
@@ -186,6 +189,7 @@ hipError_t launch_tree(const TreeParams& q, hipStream_t st) {
   // for finding their part, so not for short ones, nor where few parts a row are dealt too coarsely (512 rows over
   // 8 contexts of 2 parts: 599 us, 541 with 2 for each).
   p.even = parts_by_length(p.a, p.nsplit);
+  p.step = pass_frames(p.a, wq);
   const size_t rows = (size_t)p.units * p.nsplit * p.a.N * p.a.G;
   p.part_o = p.part_ml + (rows * 2 * sizeof(float) + 255) / 256 * 256 / sizeof(float);
   // eight XCDs: a multiple of 8 workgroup slots (see tree_kernel)

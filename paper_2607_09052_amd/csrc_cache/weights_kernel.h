@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kWeightsThreads, 2) void weights_kernel(WeightsPara
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_uniform32(tid >> 6), quad = lane >> 4;
   if (p.even) {
     int n, before;
-    row_parts(a, p.parts, n, before);
+    row_parts(a, p.parts, 4 * TF, n, before);
     const int j = (int)blockIdx.y * p.parts + part;
     const unsigned long long mine = __ballot(j >= before && j < before + n);
     if (mine == 0) return;

@@ -194,3 +194,27 @@ def test_the_smallest_scales_average(shape, c):
         out, lse = run_tree(p)
         sync()
         p.check_tree(out, lse)
+
+
+@pytest.mark.parametrize("io,N", [("bf16", 1), ("f32", 3), ("bf16", 64)])
+def test_a_short_row_takes_no_more_parts_than_it_has_passes(io, N):
+    """One row of 300 tokens among empty ones, in a capacity of 131072: its 10 frames are at most 10 parts, and an empty
+    row is one, each of N rows of 64 outputs, a maximum and a sum in the workspace; nothing else is written there."""
+    B, d, cap = 64, 64, 131072
+    p = Problem(DEV, B=1, Hkv=1, G=1, d=d, T=300, N=N, io=io, draft=False)
+    cfg = cobs.Config(batch=B, num_q_heads=1, num_kv_heads=1, head_dim=d, max_seq_len=cap, rank=0, budget=0, window=0)
+    k, v = (torch.zeros((1, 1, cap, d), dtype=torch.bfloat16) for _ in range(2))
+    k[:, :, :p.cap], v[:, :, :p.cap] = p.k, p.v
+    k, v, q = k.to(DEV).expand(B, 1, cap, d), v.to(DEV).expand(B, 1, cap, d), p.q.to(DEV).expand(B, N, 1, d).contiguous()
+    for at in (0, 37):
+        seq = torch.zeros(B, dtype=torch.int32, device=DEV)
+        seq[at] = 300
+        ws = torch.full((cache.tree_workspace_bytes(cfg, N),), 0x7b, dtype=torch.uint8, device=DEV)
+        out, lse = torch.empty_like(q), torch.empty((B, N, 1), device=DEV)
+        cache.cobs_tree_decode(cfg, q, k, v, seq, None, None, out, ws, lse=lse)
+        sync()
+        p.check_tree(out[at:at + 1], lse[at:at + 1])
+        rest = torch.arange(B, device=DEV) != at
+        assert bool((out[rest] == 0).all()) and bool((lse[rest] == -INF).all())
+        written = int((ws.view(torch.int32) != 0x7b7b7b7b).sum())
+        assert written <= (10 + B - 1) * N * (d + 2), written
