@@ -14,7 +14,7 @@ import torch
 from . import cobs
 from .cobs import CobsError, _KV, _check, _fits, _gpu, _kv, _kv_fits, _need, _opt, _ptr, _same_gpu, _stream, _units, _ws
 
-MAX_QUERIES = 64
+MAX_QUERIES = 64           # per row and call (the bits of a tree mask word)
 
 _P, _I, _Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
 _SIGS = {
@@ -77,7 +77,7 @@ def _queries_fit(cfg, dtype, q, k, v, seq_lens, draft_lens, tree_mask, sel, bloc
         return None
     dev, shape = _gpu(q), q.shape
     if (len(shape) != 4 or shape[0] != cfg.batch or shape[2] != cfg.num_q_heads or shape[3] != cfg.head_dim or
-            q.dtype not in _IO or (tree_mask is not None and tree_mask.shape != shape[:2])):
+            not 1 <= shape[1] <= MAX_QUERIES or q.dtype not in _IO or (tree_mask is not None and tree_mask.shape != shape[:2])):
         return None
     if not _fits(dev, (q, q.dtype, 0), (seq_lens, torch.int32, cfg.batch), (draft_lens, torch.int32, cfg.batch),
                  (tree_mask, torch.int64, 0), (sel, torch.int32, _units(cfg) * cfg.budget), *more):
@@ -108,6 +108,8 @@ def _queries(cfg, q, seq_lens, draft_lens, tree_mask, sel):
     if q.dim() != 4 or q.shape[0] != cfg.batch or tuple(q.shape[2:]) != (cfg.num_q_heads, cfg.head_dim):
         raise CobsError(f"q must have shape [{cfg.batch}, N, {cfg.num_q_heads}, {cfg.head_dim}], got {list(q.shape)}")
     n = q.shape[1]
+    if not 1 <= n <= MAX_QUERIES:
+        raise CobsError(f"q must hold 1 to {MAX_QUERIES} queries a row, got {n}")
     _need("q", q, q.dtype, q.numel())
     _need("seq_lens", seq_lens, torch.int32, cfg.batch)
     if (draft_lens is None) != (tree_mask is None):

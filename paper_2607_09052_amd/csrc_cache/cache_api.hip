@@ -10,6 +10,8 @@ using namespace cobs;
 
 namespace {
 
+static_assert(kMaxQueries == COBS_MAX_QUERIES, "the header's bound");
+
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 cobs_status_t hip_status(hipError_t e) { return e == hipSuccess ? COBS_OK : COBS_ERR_HIP; }

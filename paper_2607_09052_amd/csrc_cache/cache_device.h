@@ -122,16 +122,6 @@ __device__ __forceinline__ bool tree_part(const TreeParams& p, int group, TreePa
   return true;
 }
 
-// Position of the first selected block >= blk among the nsel valid ones.
-__device__ __forceinline__ int sel_lower_bound(const Attended& x, int blk) {
-  int lo = 0, hi = x.nsel;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (x.sel[mid] < blk) lo = mid + 1; else hi = mid;
-  }
-  return lo;
-}
-
 __device__ __forceinline__ int wave_uniform32(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // The value that the lane of the other half of the wave (l ^ 32) holds.
