@@ -31,7 +31,9 @@ inline int max_frames(const AttendParams& a) {
 }
 
 // Workgroups that each of `units` pieces of work of `passes` passes is split over: at most `parts`, with
-// at most `most` passes each, on `slots` (256 CUs, two workgroups each).  The split with the least
+// at most `most` passes each, on `slots` (256 CUs, two workgroups each, as most of the kernels fit: tree_kernel
+// for fp32 caches of 128-element heads, and for up to 32 rows of fp32 queries over bf16 ones, fits one; for 64-element
+// bf16 caches three).  The split with the least
 // time of its rounds: a pass takes `pass_us`, and a workgroup 4 us more (measured: 3 to 5 us of
 // dependent loads before the first product).  The longest parts go first, so that only with one round
 // does a part's last, uneven pass show.  `taken`: workgroups besides that the launch has.

@@ -185,9 +185,9 @@ hipError_t launch_tree(const TreeParams& q, hipStream_t st) {
   tree_plan(p.a, &wq, &p.mtiles, &p.nsplit);
   p.units = p.a.B * p.a.hkv;
   // Parts by the rows' lengths, which a wave's lanes hold: 128 rows over 4 contexts of 8k to 32k tokens, on pages,
-  // 110 us (120 with as many parts a row), 32 rows over 16 contexts 283 (302).  Contexts of one length pay 1 to 2 us
+  // 133 us (139 with as many parts a row), 32 rows over 16 contexts 284 (301).  Contexts of one length pay 1 to 2 us
   // for finding their part, so not for short ones, nor where few parts a row are dealt too coarsely (512 rows over
-  // 8 contexts of 2 parts: 599 us, 541 with 2 for each).
+  // 8 contexts of 2 parts: 800 us, 722 with 2 for each).
   p.even = parts_by_length(p.a, p.nsplit);
   p.step = pass_frames(p.a, wq);
   const size_t rows = (size_t)p.units * p.nsplit * p.a.N * p.a.G;

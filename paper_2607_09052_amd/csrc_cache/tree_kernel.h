@@ -17,11 +17,11 @@
 //
 // Measured (d 128, bf16 cache): 16 rows of a batch of 32 over 85 selected blocks and a window of
 // 512, fp32 queries: 800 MB in 168 us, 4.8 TB/s, with three products for one (150 TFLOP in them)
-// near the matrix cores' bound too; 128 rows over 8k to 32k tokens, on pages: 411 MB in 129 us, 3.2 TB/s;
-// 512 rows over 8 x 32k tokens: 0.55 TFLOP (0.82 with the second part of the probabilities)
-// in 873 us, matrix instructions and softmax overlapping little with two waves a
-// SIMD (tree_wide.h has the form for such calls).  One short context: 9 us of
-// dependent loads, barriers and one pass.
+// near the matrix cores' bound too (busy 44 % of the time); 128 rows over 4 contexts of 8k to 32k tokens, on
+// pages: 411 MB in 110 us, 3.7 TB/s, the matrix cores busy 35 %; 512 rows over 8 x 32k tokens:
+// 0.55 TFLOP (0.82 with the second part of the probabilities) in 873 us, matrix instructions and
+// softmax overlapping little with two waves a SIMD (tree_wide.h has the form for such calls).
+// One short context: 9 us of dependent loads, barriers and one pass.
 //
 // Frames travel HBM -> registers (two passes ahead; WQ = 1: one) -> LDS, in 16-byte
 // chunks that are swizzled by row against bank conflicts:
