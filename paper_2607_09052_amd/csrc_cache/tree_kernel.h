@@ -180,7 +180,7 @@ __device__ __forceinline__ bool has_infinity(uint4 x) {
 // Query rows of the wave's outputs again (bit k of a lane's `nan`: its outputs of the pass k have NaN), if the
 // frames f_lo .. f_hi - 1 of the part (bf16) hold an infinity: scores, softmax and sums element by
 // element in fp32, from memory, a row at a time.  row_of(k, thread) is the row of a thread's outputs.
-// Rare, so only right: one infinite value in one of 32 contexts of 32k tokens, 32 rows each: 4.9 ms for 0.11.
+// Rare, so only right: one infinite value in one of 32 contexts of 32k tokens, 32 rows each: 2.5 ms for 0.11.
 template <int D, typename RowOf>
 __device__ __forceinline__ void plain_rows(const TreeParams& p, const Attended& x, const TreePart& part, int f_lo, int f_hi,
                                            uint32_t nan, RowOf row_of) {
@@ -212,7 +212,10 @@ __device__ __forceinline__ void plain_rows(const TreeParams& p, const Attended& 
     if (!((__ballot((nan >> k) & 1) >> first) & (TPR == 32 ? 0xffffffffull : 0xffffull))) continue;
     const int row = wave_uniform32(row_of(k, (threadIdx.x & ~63) + first));
     const QueryRow q = query_row(a, b, h, row);
-    float m = -INFINITY, l = 0.0f, o[COLS] = {};
+    float m = -INFINITY, l = 0.0f, o[COLS] = {}, qv[COLS];    // (element 64 j + lane of the query)
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) qv[j] = load_elem(a.q, q.at * D + 64 * j + lane, !a.io_bf16);
+    auto element = [&](int e) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(qv[COLS == 2 && e >= 64]), e % 64)); };
     for (int f = f_lo; f < f_hi; ++f) {
       int fa, lo, hi;
       x.frame(f, fa, lo, hi);
@@ -222,9 +225,17 @@ __device__ __forceinline__ void plain_rows(const TreeParams& p, const Attended& 
       const int t = fa + (lane & 31);
       const bool see = t >= lo && t < hi && (t < x.C || ((q.bits >> (t - x.C)) & 1));
       float s = 0.0f;
-      if (see)
-        for (int e = half * (D / 2); e < (half + 1) * (D / 2); ++e)
-          s = fmaf(load_elem(a.q, q.at * D + e, !a.io_bf16), load_elem(kp, base + (lane & 31) * rs + e, false), s);
+#pragma unroll
+      for (int e = 0; e < D / 2; e += 8) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (see) x = *reinterpret_cast<const uint4*>(kp + base + (lane & 31) * rs + half * (D / 2) + e);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float qe = half ? element(D / 2 + e + i) : element(e + i);
+          s = fmaf(qe, i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]), s);
+        }
+      }
       s += other_half(s);
       float top = see ? s : -INFINITY;
 #pragma unroll
@@ -238,13 +249,22 @@ __device__ __forceinline__ void plain_rows(const TreeParams& p, const Attended& 
       l = fmaf(l, alpha, sum);
 #pragma unroll
       for (int j = 0; j < COLS; ++j) o[j] *= alpha;
-      uint32_t seen = (uint32_t)__ballot(see);               // (both halves alike)
-      while (seen) {
-        const int k = __builtin_ctz(seen);
-        seen &= seen - 1;
-        const float pk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pr), k));
+      const uint32_t seen = (uint32_t)__ballot(see);         // (both halves alike; a value that is not seen enters as 0)
+      for (int k0 = 0; k0 < kFrame; k0 += 16) {
+        uint32_t v[16];
 #pragma unroll
-        for (int j = 0; j < COLS; ++j) o[j] = fmaf(pk, load_elem(vp, base + k * rs + COLS * lane + j, false), o[j]);
+        for (int k = 0; k < 16; ++k) {
+          const uint16_t* at = vp + base + (k0 + k) * rs + COLS * lane;
+          if constexpr (COLS == 2) v[k] = *reinterpret_cast<const uint32_t*>(at);
+          else v[k] = *at;
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float pk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pr), k0 + k));
+          const uint32_t x = (seen >> (k0 + k)) & 1 ? v[k] : 0;
+          o[0] = fmaf(pk, bf16_lo(x), o[0]);
+          if constexpr (COLS == 2) o[1] = fmaf(pk, bf16_hi(x), o[1]);
+        }
       }
     }
     // in the place of what is NaN (a score: all of the row; a value: its column, at the maximum that the others have)
