@@ -73,7 +73,8 @@ cobs_status_t cobs_tree_decode(const cobs_config_t* cfg, const void* q, cobs_dty
  *   q, num_queries, io_dtype, kv, ..., sel: as for cobs_tree_decode (V is not read).
  *   lse:     device fp32 [B, num_queries, Hq]: the queries' normalisers, as cobs_tree_decode
  *            or a decode step returns them.  A query head with lse -inf or +inf adds nothing
- *            (+inf leaves a rejected drafted token out), whatever its query holds.
+ *            (+inf leaves a rejected drafted token out), whatever its query holds
+ *            (one that is not finite makes the call some hundred times as long).
  *   prev:    optional device fp32 [B, Hkv, max_seq_len], NULL for zeros; `weights` itself, or apart.
  *   weights: device fp32 [B, Hkv, max_seq_len].                                     */
 cobs_status_t cobs_attention_weights(const cobs_config_t* cfg, const void* q, cobs_dtype_t io_dtype,
