@@ -33,8 +33,9 @@
  *     attend to the context alone.  One query is then cobs_sparse_decode.
  * A token that a query does not attend to has no effect on it, whatever its key
  * and value hold; one that it attends to acts as in plain arithmetic (with a score of
- * -inf its probability is 0, an infinite value is one in the output).  Infinities there
- * may make a call take a hundred times as long.  Tokens on a page whose id is out of range are left out.
+ * -inf its probability is 0, an infinite value is one in the output; a query with no
+ * other scores is like one that attends to nothing).  Infinities there may make a call
+ * take a hundred times as long.  Tokens on a page whose id is out of range are left out.
  */
 #ifndef COBS_CACHE_H
 #define COBS_CACHE_H
