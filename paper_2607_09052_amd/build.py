@@ -20,12 +20,13 @@ FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
+DIRS = ("csrc", "csrc_cache", "csrc_tokens")
 OBJ_DIR = os.path.join(HERE, "_build")
 
 
 def sources():
-    """The decode path's translation units, then the cache operators' (their names differ)."""
-    return [s for d in ("csrc", "csrc_cache") for s in sorted(glob.glob(os.path.join(HERE, d, "*.hip")))]
+    """The decode path's translation units, then those of the operators around it (their names differ)."""
+    return [s for d in DIRS for s in sorted(glob.glob(os.path.join(HERE, d, "*.hip")))]
 
 
 def _run(cmd):
@@ -39,7 +40,7 @@ def build(verbose=False, jobs=None):
     """Compile every translation unit (in parallel), then link libcobs.so."""
     from concurrent.futures import ThreadPoolExecutor
     os.makedirs(OBJ_DIR, exist_ok=True)
-    inc = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"), "-I", os.path.join(HERE, "csrc_cache")]
+    inc = ["-I", os.path.join(ROOT, "include")] + [x for d in DIRS for x in ("-I", os.path.join(HERE, d))]
     srcs = sources()
     objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-4] + ".o") for s in srcs]
     cmds = [[HIPCC, *FLAGS, *inc, "-c", s, "-o", o] for s, o in zip(srcs, objs)]

@@ -5,6 +5,8 @@
 
 namespace cobs {
 
+constexpr int kTreeThreads = 256;
+
 // The tokens of one (batch row, KV head) that queries attend to, as frames:
 // aligned runs of 32 positions a .. a + 31, of which lo .. hi - 1 take part.
 // First the frames of the valid selected blocks (tokens before the window start
@@ -149,6 +151,41 @@ __device__ __forceinline__ void store_row4(void* out, int64_t i, float4 sum, flo
         make_uint2(f32x2_to_bf16x2_rne(y.x, y.y), f32x2_to_bf16x2_rne(y.z, y.w));
   } else {
     *reinterpret_cast<float4*>(static_cast<float*>(out) + i) = y;
+  }
+}
+
+// The rows of a wave: query row `r` of the M = N G of a (row, KV head), or none.  The
+// rows of padded queries are read like the others, which needs no row length (their
+// columns of the products are computed and left).
+struct QueryRow {
+  int64_t at;        // (b N + i) Hq + head: row of q, out and lse
+  bool live;
+  uint64_t bits;     // drafted tokens that it sees
+};
+__device__ __forceinline__ QueryRow query_row(const AttendParams& a, int b, int h, int r) {
+  QueryRow q;
+  const int i = r / a.G, g = r - i * a.G;
+  q.live = i < a.N;
+  q.at = ((int64_t)b * a.N + i) * a.hq + h * a.G + g;
+  q.bits = (q.live && a.mask) ? a.mask[(int64_t)b * a.N + i] : 0;
+  return q;
+}
+
+// Partial of a split, per query row: (log2-domain maximum, sum) and D unnormalised outputs.
+__device__ __forceinline__ int64_t part_row(const TreeParams& p, const TreePart& t, int r) {
+  return (t.first + t.split) * (p.a.N * p.a.G) + r;
+}
+
+// Outputs 0 and lse -inf for the rows of a tile that belong to no live query.
+template <int D>
+__device__ __forceinline__ void clear_padding(const TreeParams& p, int b, int h, int first, int rows, int nq) {
+  const AttendParams& a = p.a;
+  const int end = min(first + rows, a.N * a.G);
+  for (int idx = max(first, nq * a.G) * (D / 4) + threadIdx.x; idx < end * (D / 4); idx += kTreeThreads) {
+    const int row = idx / (D / 4), d4 = idx % (D / 4), i = row / a.G;
+    const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
+    store_row4(p.out, at * D + 4 * d4, make_float4(0.0f, 0.0f, 0.0f, 0.0f), 0.0f, a.io_bf16);
+    if (d4 == 0 && p.lse) p.lse[at] = -INFINITY;
   }
 }
 

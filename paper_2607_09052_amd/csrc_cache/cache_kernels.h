@@ -115,6 +115,7 @@ struct CompactParams {
 void tree_plan(const AttendParams& a, int* wq, int* mtiles, int* nsplit);
 size_t tree_workspace(const AttendParams& a);
 hipError_t launch_tree(const TreeParams& p, hipStream_t st);
+hipError_t launch_tree_merge(const TreeParams& p, hipStream_t st);      // joins the parts of split contexts
 hipError_t launch_weights(const WeightsParams& p, hipStream_t st);
 size_t evict_workspace(int B, int hkv, int tmax);
 hipError_t launch_evict(const EvictParams& p, hipStream_t st);

@@ -140,6 +140,10 @@ static hipError_t launch_merge(const TreeParams& p, hipStream_t st) {
   return hipGetLastError();
 }
 
+hipError_t launch_tree_merge(const TreeParams& p, hipStream_t st) {
+  return p.a.d == 64 ? launch_merge<64>(p, st) : launch_merge<128>(p, st);
+}
+
 hipError_t launch_tree_bf16_d64(const TreeParams& p, int wq, int grid, hipStream_t st);
 hipError_t launch_tree_bf16_d128(const TreeParams& p, int wq, int grid, hipStream_t st);
 hipError_t launch_tree_f32_d64(const TreeParams& p, int wq, int grid, hipStream_t st);
@@ -200,7 +204,7 @@ hipError_t launch_tree(const TreeParams& q, hipStream_t st) {
   if (p.a.kv_f32) e = p.a.d == 64 ? launch_tree_f32_d64(p, wq, g, st) : launch_tree_f32_d128(p, wq, g, st);
   else e = p.a.d == 64 ? launch_tree_bf16_d64(p, wq, g, st) : launch_tree_bf16_d128(p, wq, g, st);
   if (e != hipSuccess || p.nsplit == 1) return e;
-  return p.a.d == 64 ? launch_merge<64>(p, st) : launch_merge<128>(p, st);
+  return launch_tree_merge(p, st);
 }
 
 }  // namespace cobs

@@ -56,7 +56,6 @@ namespace cobs {
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kTreeThreads = 256;
 constexpr int kTable = 256;            // frame descriptors held in LDS at a time
 
 template <int D, int WQ, bool F32>
@@ -112,23 +111,6 @@ __device__ __forceinline__ uint4 finite_only(uint4 x, bool& found) {
 // where 8 / c2 overflows, as -inf + inf would let no score become the maximum.)
 __device__ __forceinline__ float max_slack(float c2) { return fminf(8.0f / c2, 3.4028234e38f); }
 
-// The rows of a wave: query row `r` of the M = N G of a (row, KV head), or none.  The
-// rows of padded queries are read like the others, which needs no row length (their
-// columns of the products are computed and left).
-struct QueryRow {
-  int64_t at;        // (b N + i) Hq + head: row of q, out and lse
-  bool live;
-  uint64_t bits;     // drafted tokens that it sees
-};
-__device__ __forceinline__ QueryRow query_row(const AttendParams& a, int b, int h, int r) {
-  QueryRow q;
-  const int i = r / a.G, g = r - i * a.G;
-  q.live = i < a.N;
-  q.at = ((int64_t)b * a.N + i) * a.hq + h * a.G + g;
-  q.bits = (q.live && a.mask) ? a.mask[(int64_t)b * a.N + i] : 0;
-  return q;
-}
-
 // Sum over visible drafted tokens j in `bad` of p V[j][d] for the elements of V that are not finite,
 // added to the lane's outputs.  Rare (an overflowed value), so from memory and element by element.
 template <int D, bool F32>
@@ -153,11 +135,6 @@ __device__ __forceinline__ void add_nonfinite(const AttendParams& a, const Atten
         if (see && !(fabsf(v) < INFINITY)) o[dt][i] += p * v;
       }
   }
-}
-
-// Partial of a split, per query row: (log2-domain maximum, sum) and D unnormalised outputs.
-__device__ __forceinline__ int64_t part_row(const TreeParams& p, const TreePart& t, int r) {
-  return (t.first + t.split) * (p.a.N * p.a.G) + r;
 }
 
 // Whether one of the five is NaN (or there are infinities of both signs).
@@ -288,19 +265,6 @@ __device__ __forceinline__ void plain_rows(const TreeParams& p, const Attended& 
       }
       if (lane == 0 && p.lse && p.lse[q.at] != p.lse[q.at]) p.lse[q.at] = l != 0.0f ? m * a.c + logf(l) : -INFINITY;
     }
-  }
-}
-
-// Outputs 0 and lse -inf for the rows of a tile that belong to no live query.
-template <int D>
-__device__ __forceinline__ void clear_padding(const TreeParams& p, int b, int h, int first, int rows, int nq) {
-  const AttendParams& a = p.a;
-  const int end = min(first + rows, a.N * a.G);
-  for (int idx = max(first, nq * a.G) * (D / 4) + threadIdx.x; idx < end * (D / 4); idx += kTreeThreads) {
-    const int row = idx / (D / 4), d4 = idx % (D / 4), i = row / a.G;
-    const int64_t at = ((int64_t)b * a.N + i) * a.hq + h * a.G + (row - i * a.G);
-    store_row4(p.out, at * D + 4 * d4, make_float4(0.0f, 0.0f, 0.0f, 0.0f), 0.0f, a.io_bf16);
-    if (d4 == 0 && p.lse) p.lse[at] = -INFINITY;
   }
 }
 

@@ -1,0 +1,191 @@
+// cobs_append8: new tokens' keys (rotated) and values into a cache of 8-bit floats with one scale for
+// each block and KV head; their queries rotated beside (append_body.h).
+//
+// The unit of work is (row b, block, KV head, keys or values): the largest magnitude among the block's new tokens sets
+// its scale, so a unit holds its tokens in registers between that maximum and their encoding, and memory is
+// read once.  D / 16 lanes take a token's head, 16 elements each.  A unit is taken by
+//   a workgroup   (many new tokens; 256 lanes, PASSES times 16 elements each), which takes several heads in turn, so
+//                 that the cosines and sines of its tokens stay in registers;
+//   a wave        (up to 8 new tokens a row, 16 of 64-element heads);
+//   D / 16 lanes  (one new token a row: a decode step, 8 or 16 units a wave).
+// Scales are powers of two, so a grown scale changes the exponents of the block's earlier codes and nothing else
+// (but for the smallest ones, which are rounded again).
+#include "append_body.h"
+
+namespace cobs {
+
+// The smallest power of two s, 2^-100 at least, with top / s <= 448 = 1.75 * 2^8: a mantissa above 1.75 carries
+// into the exponent.
+__device__ __forceinline__ float scale_for(float top) {
+  const int e = (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8;
+  return __uint_as_float((uint32_t)max(e, 27) << 23);
+}
+
+// Four codes of x * inv (at most 448 in magnitude), the lowest byte first.  The hardware rounds to nearest even and
+// keeps denormals; what is not finite becomes NaN.
+__device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = fabsf(x[i]) < INFINITY ? x[i] * inv : __uint_as_float(0x7fc00000u);
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
+}
+
+__device__ __forceinline__ void values4(uint32_t w, float* x) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
+}
+
+template <int D, int LANES, int PASSES>
+__global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) {
+  constexpr int TPR = D / 16, RP = LANES / TPR, UNITS = kHeadThreads / LANES;
+  static_assert(LANES == kHeadThreads || LANES <= 64, "a workgroup, or lanes of a wave");
+  __shared__ HeadsShared hs;
+  __shared__ float s_top[2][kHeadThreads / 64], s_held[2];
+  if (blockIdx.x == 0) write_lens(p.t);
+  if ((int)blockIdx.x < p.q_groups) {
+    heads_body<D, false>(p.t, nullptr, false, blockIdx.x, p.per_wg, p.slots, p.slot_groups, hs);
+    return;
+  }
+  const int tid = threadIdx.x, H2 = 2 * p.t.hkv;
+  // items: (head, K or V), keys first, `items` of them a workgroup (LANES < 256: one a unit)
+  const int per = LANES == kHeadThreads ? p.items : 1, groups = (H2 + per - 1) / per;
+  const int64_t unit = (int64_t)((int)blockIdx.x - p.q_groups) * UNITS + tid / LANES;
+  const int64_t units = (int64_t)p.t.B * p.blocks * groups;
+  if (unit >= units) return;                           // (LANES == 256: the whole workgroup)
+  const int it0 = (int)(unit % groups) * per, it1 = min(H2, it0 + per);
+  const int bj = (int)(unit / groups), b = bj / p.blocks;
+  const NewRow r = new_row(p.t, b);
+  const int lsh = p.kv.lsh;
+  const int n = min(r.n, p.t.tmax - r.T);               // tokens that the cache has room for
+  const int j = (r.T >> lsh) + bj % p.blocks;           // the block
+  const int t0 = max(j << lsh, r.T), t1 = min((j + 1) << lsh, r.T + n);     // its new tokens
+  if (t0 >= t1) return;
+  const int earlier = t0 - (j << lsh);                  // tokens that it holds
+  const int64_t base = kv_offset(p.kv, b, 0, j << lsh);
+  if (base < 0) return;
+  const int64_t rs = p.kv.table ? D : p.kv.st, hs_step = p.kv.table ? ((int64_t)D << lsh) : p.kv.sh;
+  const int64_t srow = p.kv.table ? base / ((int64_t)p.t.hkv * D << lsh) * p.t.hkv : (int64_t)b * p.t.hkv * p.kv.nbmax + j;
+  const int64_t sstep = p.kv.table ? 1 : p.kv.nbmax;
+
+  const int lane = tid % LANES, row = lane / TPR, piece = lane % TPR;
+  const Piece e = piece_of(p.t.rope, piece), straight = {16 * piece, 16 * piece + 8, false};
+  float2 cs[PASSES][8];
+  if (e.turned && it0 < p.t.hkv) {
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+      const int t = t0 + row + k * RP;
+      if (t < t1) {
+        const int i = t - r.T, at = p.t.rope.positions ? p.t.rope.positions[(int64_t)b * p.t.N + i] : t;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) cs[k][x] = turn_of(p.t.rope, at, 8 * piece + x);
+      }
+    }
+  }
+  for (int it = it0; it < it1; ++it) {
+    const bool key = it < p.t.hkv;
+    const int h = key ? it : it - p.t.hkv;
+    const HeadsView& from = key ? p.t.k : p.t.v;
+    const Piece c = key ? e : straight;
+    float x[PASSES][16];
+    float top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+      const int t = t0 + row + k * RP;
+      if (t < t1) {
+        const int64_t at = b * from.sb + (t - r.T) * from.sn + h * from.sh;
+        const Raw8 r0 = load_raw8(from.p, at + c.e0, from.f32), r1 = load_raw8(from.p, at + c.e1, from.f32);
+        widen8(r0, from.f32, x[k]);
+        widen8(r1, from.f32, x[k] + 8);
+        if (c.turned) turn16(x[k], cs[k], p.t.rope.interleaved);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float a = fabsf(x[k][i]);
+          top = a < INFINITY ? fmaxf(top, a) : top;
+        }
+      }
+    }
+    float* const scale = (key ? p.k_scale : p.v_scale) + srow + h * sstep;
+    float held;
+    if constexpr (LANES == kHeadThreads) {
+      top = wave_max(top);
+      const int buf = (it - it0) & 1;                   // (a barrier lies between a buffer's use and its next writing)
+      if ((tid & 63) == 0) s_top[buf][tid >> 6] = top;
+      if (tid == 0) s_held[buf] = *scale;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kHeadThreads / 64; ++w) top = fmaxf(top, s_top[buf][w]);
+      held = s_held[buf];
+    } else {
+#pragma unroll
+      for (int o = LANES / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+      held = *scale;
+    }
+    const float need = scale_for(top);
+    const float now = earlier > 0 && held >= need ? held : need, inv = 1.0f / now;
+    uint8_t* const codes = static_cast<uint8_t*>(const_cast<void*>(key ? p.kv.k : p.kv.v)) + base + h * hs_step;
+    if (earlier > 0 && now != held) {
+      const float ratio = held * inv;
+      for (int t = row; t < earlier; t += RP) {
+        uint4* const at = reinterpret_cast<uint4*>(codes + t * rs + 16 * piece);
+        const uint4 w = *at;
+        float y[16];
+        values4(w.x, y); values4(w.y, y + 4); values4(w.z, y + 8); values4(w.w, y + 12);
+        *at = make_uint4(codes4(y, ratio), codes4(y + 4, ratio), codes4(y + 8, ratio), codes4(y + 12, ratio));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+      const int t = t0 + row + k * RP;
+      if (t < t1) {
+        uint8_t* const at = codes + (t - (j << lsh)) * rs;
+        *reinterpret_cast<uint2*>(at + c.e0) = make_uint2(codes4(x[k], inv), codes4(x[k] + 4, inv));
+        *reinterpret_cast<uint2*>(at + c.e1) = make_uint2(codes4(x[k] + 8, inv), codes4(x[k] + 12, inv));
+      }
+    }
+    if (lane == 0) *scale = now;
+  }
+}
+
+template <int D>
+static hipError_t launch_d(Append8Params p, hipStream_t st) {
+  constexpr int TPR = D / 16;
+  const int L = 1 << p.kv.lsh;
+  p.q_groups = p.per_wg = p.slots = p.slot_groups = 0;
+  if (p.t.hq > 0) {
+    const int64_t tokens = (int64_t)p.t.B * p.t.N;
+    plan_heads(tokens, p.t.hq, D, &p.per_wg, &p.slots, &p.slot_groups);
+    const int64_t g = (tokens + p.per_wg - 1) / p.per_wg * p.slot_groups;
+    if (g > 0x3fffffff) return hipErrorInvalidValue;
+    p.q_groups = (int)g;
+  }
+  const int most = p.t.N < L ? p.t.N : L;               // new tokens of a block
+  p.blocks = (p.t.N + L - 2) / L + 1;
+  // (with 64 lanes a unit: one unit a wave)
+  const int lanes = most == 1 ? TPR : (most <= 64 / TPR ? 64 : kHeadThreads);
+  p.items = 1;
+  if (lanes == kHeadThreads) {
+    // heads of a workgroup: as many as leave four workgroups a CU
+    const int64_t all = (int64_t)p.t.B * p.blocks * 2 * p.t.hkv;
+    p.items = (int)(all / 1024);
+    p.items = p.items < 1 ? 1 : (p.items > 2 * p.t.hkv ? 2 * p.t.hkv : p.items);
+  }
+  const int64_t units = (int64_t)p.t.B * p.blocks * ((2 * p.t.hkv + p.items - 1) / p.items);
+  const int per_group = kHeadThreads / lanes;
+  const int64_t grid = p.q_groups + (units + per_group - 1) / per_group;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 g((uint32_t)grid), t(kHeadThreads);
+  const int rows = kHeadThreads / TPR;                  // tokens of a workgroup's pass
+  if (lanes == TPR) hipLaunchKernelGGL((append8_kernel<D, TPR, 1>), g, t, 0, st, p);
+  else if (lanes == 64) hipLaunchKernelGGL((append8_kernel<D, 64, 1>), g, t, 0, st, p);
+  else if (most <= rows) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 1>), g, t, 0, st, p);
+  else if (most <= 2 * rows) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 2>), g, t, 0, st, p);
+  else if constexpr (D == 128) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 4>), g, t, 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_append8(const Append8Params& p, hipStream_t st) {
+  return p.t.d == 64 ? launch_d<64>(p, st) : launch_d<128>(p, st);
+}
+
+}  // namespace cobs

@@ -1,0 +1,596 @@
+"""The token operators against fp64: rotary positions, appends to bf16, fp32 and 8-bit caches, attention over
+8-bit caches, their blocks unpacked, and all of them in turn as a serving program runs them.  Tolerances are
+derived in tests/tokens_util.py."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as O
+from oracle import tokens as R
+from paper_2607_09052_amd import cobs, tokens
+from tests.cache_util import TORCH
+from tests.gpu_util import DEV, f64, say, sync
+from tests.tokens_util import E4M3, NAN_CODE, Appending, Problem8, rotation_tolerance, run_decode8
+
+pytestmark = pytest.mark.gpu
+
+
+def _ids(x):
+    return "-".join(f"{k}{v}" for k, v in x.items()) if isinstance(x, dict) else str(x)
+
+
+# ---------------------------------------------------------------- rotation --
+ROTATIONS = [
+    dict(B=1, N=1, H=1, d=64, r=16),
+    dict(B=1, N=1, H=7, d=128, r=128, inter=True),
+    dict(B=3, N=5, H=4, d=64, r=64),
+    dict(B=2, N=33, H=3, d=128, r=96, inter=True, scale=1.25),
+    dict(B=1, N=257, H=40, d=128, r=64, base=5e5),
+    dict(B=2, N=2500, H=2, d=64, r=32, inter=True),                   # more than 4096 tokens: four to a workgroup
+    dict(B=1, N=4099, H=5, d=128, r=112),
+]
+
+
+@pytest.mark.parametrize("io,out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("shape", ROTATIONS, ids=_ids)
+def test_rotation_matches_fp64(shape, io, out):
+    say(f"rotate {shape} {io} {out}")
+    B, N, H, d, r = (shape[x] for x in ("B", "N", "H", "d", "r"))
+    inter, scale = shape.get("inter", False), shape.get("scale", 1.0)
+    gen = torch.Generator().manual_seed(7)
+    x = torch.randn((B, N, H, d + 16), generator=gen).to(TORCH[io])
+    freq = tokens.rope_frequencies(r, base=shape.get("base", 1e4))
+    at = torch.randint(-(1 << 20), 1 << 20, (B, N), generator=gen).to(torch.int32)
+    at[0, 0] = 0
+    wide = torch.full((N, B, H, d + 8), 3.0, dtype=TORCH[out], device=DEV)
+    y = wide.permute(1, 0, 2, 3)[..., :d]                             # strides of its own
+    tokens.cobs_rotate(x.to(DEV)[..., :d], tokens.Rope(freq.to(DEV), inter, scale), at.to(DEV), y)
+    sync()
+    for b in range(B):
+        want = R.rotate(f64(x[b, ..., :d]), at[b].numpy(), freq.double().numpy(), inter, scale)
+        tol = rotation_tolerance(f64(x[b, ..., :d]), want, r // 2, inter, scale, out)
+        off = np.abs(f64(y[b]) - want)
+        assert np.all(off <= tol), float((off / tol).max())
+        assert np.array_equal(f64(y[b])[..., r:], f64(x[b, ..., r:d].to(TORCH[out])))
+    assert torch.all(wide[..., d:] == 3.0)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotation_in_place_of_one_projections_output(inter):
+    gen = torch.Generator().manual_seed(3)
+    rows = torch.randn((2, 9, 6, 128), generator=gen).bfloat16().to(DEV)
+    before = rows.clone()
+    freq = tokens.rope_frequencies(128).to(DEV)
+    at = torch.arange(18, dtype=torch.int32, device=DEV).view(2, 9)
+    apart = torch.empty((2, 9, 4, 128), dtype=torch.bfloat16, device=DEV)
+    tokens.cobs_rotate(before[:, :, :4], tokens.Rope(freq, inter), at, apart)
+    tokens.cobs_rotate(rows[:, :, :4], tokens.Rope(freq, inter), at, rows[:, :, :4])
+    sync()
+    assert torch.equal(rows[:, :, :4], apart) and torch.equal(rows[:, :, 4:], before[:, :, 4:])
+
+
+def test_a_turn_back_gives_the_queries_again():
+    gen = torch.Generator().manual_seed(4)
+    x = torch.randn((1, 64, 8, 128), generator=gen).to(DEV)
+    at = torch.randint(0, 1 << 30, (1, 64), generator=gen).to(torch.int32).to(DEV)
+    rope = tokens.Rope(tokens.rope_frequencies(128).to(DEV))
+    y = torch.empty_like(x)
+    tokens.cobs_rotate(x, rope, at, y)
+    tokens.cobs_rotate(y, rope, -at, y)
+    sync()
+    a = f64(x)
+    tol = 2.5 * rotation_tolerance(a, a, 64, False, 1.0, "f32")
+    # (the second turn's input is off by the first's error, and its pairs are up to sqrt(2) times as large)
+    pair = np.abs(a[..., :64]) + np.abs(a[..., 64:])
+    tol += 16 * 2.0 ** -24 * np.concatenate([pair, pair], -1)
+    assert np.all(np.abs(f64(y) - a) <= tol)
+
+
+# ----------------------------------------------------------------- appends --
+APPENDS = [
+    dict(B=1, Hkv=1, G=1, d=64, L=32, N=1, T=0),                                     # the first token
+    dict(B=1, Hkv=2, G=4, N=1, T=63),                                                # the last of a block
+    dict(B=5, Hkv=2, G=2, N=1, T=(0, 1, 64, 127, 200)),                              # a decode step
+    dict(B=3, Hkv=2, G=2, N=7, T=(60, 64, 3), new=(7, 0, 2)),                        # drafts; a row without one
+    dict(B=2, Hkv=3, G=1, d=64, N=13, T=(10, 121), L=128, r=32, inter=True),
+    dict(B=2, Hkv=2, G=8, N=20, T=(5, 100), L=32, shift=100000, scale=1.2),          # over three blocks; other positions
+    dict(B=2, Hkv=1, G=2, N=64, T=(64, 32), r=64),
+    dict(B=2, Hkv=2, G=1, N=300, T=(0, 77), new=(300, 211), inter=True),
+    dict(B=1, Hkv=2, G=2, N=5000, T=130, L=128),                                     # a prompt
+    dict(B=1, Hkv=4, G=1, d=64, N=4500, T=0, L=128, r=0),                            # no rotation
+    dict(B=3, Hkv=2, G=2, N=50, T=(100, 128, 80), cap=128),                          # the cache ends
+    dict(B=2, Hkv=2, G=2, N=9, T=(-5, 1000), cap=128, new=(100, -1)),                # lengths out of range
+    dict(B=40, Hkv=8, G=1, d=64, N=2, T=31, L=32, shift=50),
+]
+
+
+@pytest.mark.parametrize("layout", ["contiguous", "pages", "strided"])
+@pytest.mark.parametrize("io,kv,out", [("bf16", "bf16", "f32"), ("f32", "bf16", "bf16"), ("bf16", "f32", "bf16"), ("f32", "f32", "f32")])
+@pytest.mark.parametrize("shape", APPENDS, ids=_ids)
+def test_append_matches_fp64(shape, io, kv, out, layout):
+    say(f"append {shape} {io} {kv} {out} {layout}")
+    p = Appending(DEV, io=io, kv=kv, out=out, layout=layout, spread=False, **shape).fresh().call()
+    sync()
+    p.check_cache()
+    p.check_queries()
+
+
+@pytest.mark.parametrize("layout", ["contiguous", "pages", "strided"])
+@pytest.mark.parametrize("io,out", [("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("shape", APPENDS, ids=_ids)
+def test_append8_matches_the_definition(shape, io, out, layout):
+    say(f"append8 {shape} {io} {out} {layout}")
+    p = Appending(DEV, io=io, out=out, layout=layout, eight=True, **shape).fresh().call()
+    sync()
+    p.check_cache8()
+    p.check_queries()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_append_without_queries_lengths_or_a_count(eight):
+    p = Appending(DEV, B=2, N=6, T=(3, 60), eight=eight, q=False, fused=False).fresh()
+    p.after = None
+    p.call(new_lens=False)
+    sync()
+    p.after = torch.tensor([9, 66])
+    (p.check_cache8 if eight else p.check_cache)()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("N", [1, 40])
+def test_append_drops_tokens_on_pages_out_of_range(eight, N):
+    p = Appending(DEV, B=3, N=N, T=(70, 5, 64), layout="pages", eight=eight, spread=False)
+    p.table[0, 1], p.table[1, 0], p.table[2, 1] = -1, p.pages_in_use(), 1 << 30
+    p.fresh().call()
+    sync()
+    (p.check_cache8 if eight else p.check_cache)()
+    p.check_queries()
+
+
+def test_append8_of_what_is_not_finite_and_of_zeros():
+    p = Appending(DEV, B=1, Hkv=2, G=1, N=40, T=(50,), eight=True, r=0, io="f32", spread=False)
+    x = p.host[2]
+    x[0, 3, 0, 5], x[0, 4, 0, 6], x[0, 5, 1, 7] = np.inf, np.nan, -np.inf
+    x[0, 20:, 1] = 0.0
+    p.host[1][0, :, 0] = 0.0                          # a block of zeros and earlier tokens
+    p.host[1][0, 14:, 1] = 2.0 ** -120                # a block below the smallest scale
+    p.kn, p.vn = (torch.from_numpy(p.host[i]).float().to(DEV) for i in (1, 2))
+    p.qd = p.qd.contiguous()
+    p.fresh().call()
+    sync()
+    p.check_cache8()
+
+
+def test_every_code_is_the_nearest():
+    """All bf16 numbers up to 448 with scale 1 (a token's largest element is 448): the codes of an append, and back."""
+    bits = torch.arange(1 << 15, dtype=torch.int32)
+    x = bits.to(torch.int16).view(torch.bfloat16)
+    x = x[x.float() <= 448.0]                         # (NaN goes too)
+    x = torch.cat([x, -x])
+    rows = -(-x.numel() // 127)
+    x = torch.cat([x, torch.zeros(rows * 127 - x.numel(), dtype=x.dtype)]).view(rows, 127)
+    x = torch.cat([x, torch.full((rows, 1), 448.0, dtype=x.dtype)], 1)
+    cap = -(-rows // 64) * 64
+    cfg = cobs.Config(batch=1, num_q_heads=1, num_kv_heads=1, head_dim=128, max_seq_len=cap, rank=0, budget=0, window=0)
+    c8 = tokens.new_cache8(cfg, DEV)
+    new = x.view(1, rows, 1, 128).to(DEV)
+    lens, after = torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    tokens.cobs_append8(cfg, new, new, c8, lens, new_seq_lens=after)
+    k, v = (torch.zeros((1, 1, cap, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    tokens.cobs_unpack8(cfg, c8, after, k, v)
+    sync()
+    assert torch.all(c8.k_scale[..., :-(-rows // 64)] == 1.0)
+    want = R.e4m3_codes(x.double().numpy())
+    assert np.array_equal(c8.k[0, 0, :rows].view(torch.uint8).cpu().numpy(), want)
+    assert np.array_equal(f64(k)[0, 0, :rows], R.e4m3_values()[want]) and torch.equal(k, v)
+
+
+@pytest.mark.parametrize("N", [1, 3, 30])
+def test_tokens_one_after_the_other_keep_a_blocks_values(N):
+    """Appended in pieces, a block's elements are within half a step of what was given, or of two where a scale grew past
+    the smallest numbers' range: half a step of the code and 2^-10 of the last scale for each growth."""
+    gen = torch.Generator().manual_seed(11)
+    B, Hkv, d, L, total = 2, 2, 128, 32, 90
+    cfg = cobs.Config(batch=B, num_q_heads=Hkv, num_kv_heads=Hkv, head_dim=d, max_seq_len=96, rank=0, budget=0, window=0, block_size=L)
+    grow = 2.0 ** (torch.arange(total) / 6.0).view(1, total, 1, 1)
+    x = (torch.randn((B, total, Hkv, d), generator=gen) * grow).bfloat16()
+    c8 = tokens.new_cache8(cfg, DEV)
+    lens, after = torch.zeros(B, dtype=torch.int32, device=DEV), torch.zeros(B, dtype=torch.int32, device=DEV)
+    on = x.to(DEV)
+    for i in range(0, total, N):
+        tokens.cobs_append8(cfg, on[:, i:i + N], on[:, i:i + N], c8, lens, new_seq_lens=after)
+        lens.copy_(after)
+    k, v = (torch.zeros((B, Hkv, 96, d), device=DEV) for _ in range(2))
+    cfg.kv_dtype = "f32"
+    tokens.cobs_unpack8(cfg, c8, lens, k, v)
+    sync()
+    want = f64(x).transpose(0, 2, 1, 3)
+    scale = np.repeat(f64(c8.k_scale), L, -1)[:, :, :total, None]
+    grown = 7                                          # (2^(32 / 6) over a block: six doublings at most, and the first)
+    tol = np.abs(want) * 2.0 ** -4 + grown * scale * 2.0 ** -10
+    assert np.all(np.abs(f64(k)[:, :, :total] - want) <= tol) and torch.equal(k, v)
+
+
+# --------------------------------------------------------------- attention --
+SHAPES = [
+    dict(B=1, Hkv=1, G=1, d=64, L=32, T=1, N=1, draft=False),
+    dict(B=1, Hkv=1, G=1, d=64, L=32, T=0, N=1),
+    dict(B=2, Hkv=2, G=4, d=128, T=(300, 0), N=1, draft=False),
+    dict(B=2, Hkv=2, G=4, d=128, T=(300, 77), N=8),
+    dict(B=3, Hkv=1, G=16, d=128, T=(31, 32, 33), N=5, L=32),
+    dict(B=2, Hkv=3, G=2, d=64, T=(129, 1000), N=3, L=128),
+    dict(B=2, Hkv=2, G=8, d=128, T=(700, 0), N=64),
+    dict(B=2, Hkv=1, G=16, d=64, T=(1500, 64), N=64, L=64),
+    dict(B=1, Hkv=2, G=4, d=128, T=3001, N=17, c=0.25),
+    dict(B=4, Hkv=2, G=4, d=128, T=(200, 90, 0, 511), N=9, drafts=(9, 0, 4, 1)),
+    dict(B=2, Hkv=2, G=4, d=128, T=(900, 333), N=6, s=3, w=100),
+    dict(B=2, Hkv=2, G=8, d=128, T=(900, 20), N=33, s=5, w=70, L=32),
+    dict(B=2, Hkv=1, G=2, d=64, T=(2000, 640), N=12, s=40, w=0, L=128),
+    dict(B=1, Hkv=2, G=4, d=128, T=700, N=4, s=0, w=65),
+    dict(B=2, Hkv=2, G=1, d=128, T=(450, 7), N=40, s=2, w=5000),
+    dict(B=2, Hkv=2, G=4, d=128, T=(257, 64), N=7, draft=False),
+    dict(B=1, Hkv=2, G=8, d=64, T=1200, N=1, draft=False, s=4, w=33),
+    dict(B=1, Hkv=1, G=2, d=128, T=20011, N=4),                        # frames beyond one table
+    dict(B=5, Hkv=1, G=4, d=128, T=(9000, 17, 4100, 0, 700), N=6),     # parts by the rows' lengths
+    dict(B=3, Hkv=2, G=4, d=64, T=(8200, 31, 2500), N=1, draft=False),
+]
+
+
+@pytest.mark.parametrize("layout", ["contiguous", "pages", "strided"])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=_ids)
+def test_decode8_matches_fp64(shape, io, layout):
+    say(f"decode8 {shape} {io} {layout}")
+    p = Problem8(DEV, io=io, layout=layout, **shape).upload()
+    out, lse = run_decode8(p)
+    sync()
+    say(f"worst error / tolerance {p.check(out, lse):.3f}")
+
+
+def test_decode8_without_a_log_sum_gives_the_same():
+    p = Problem8(DEV, B=2, T=(500, 90), N=3).upload()
+    out, _ = run_decode8(p)
+    again = torch.empty_like(out)
+    tokens.cobs_decode8(p.cfg, p.qd, p.cache8, p.seq, p.drafts, p.mask, again, tokens.new_decode8_workspace(p.cfg, p.N, DEV))
+    sync()
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("d,N,G", [(128, 6, 2), (64, 6, 4), (128, 24, 8)])
+def test_what_a_query_does_not_see_does_not_reach_it(io, d, N, G):
+    """NaN codes in drafted tokens' keys and values: queries that see such a token get NaN where plain arithmetic gives it (a key:
+    everywhere; a value: its column), the others what they get without it."""
+    bits = [[1 << i | 1 for i in range(N)] for _ in range(2)]
+    clean = Problem8(DEV, B=2, Hkv=2, G=G, d=d, T=(100, 33), N=N, io=io, bits=bits, seed=5).upload()
+    want, wl = run_decode8(clean)
+    p = Problem8(DEV, B=2, Hkv=2, G=G, d=d, T=(100, 33), N=N, io=io, bits=bits, seed=5)
+    for b, T in enumerate((100, 33)):
+        p.codes[0][b, 0, T + 2, 7] = 0xff            # a key of head 0, seen by query 2
+        p.codes[1][b, 1, T + 4, 9] = NAN_CODE        # a value of head 1, seen by query 4
+    p.upload()
+    out, lse = run_decode8(p)
+    sync()
+    o, w, z = out.view(2, N, 2, G, d), want.view(2, N, 2, G, d), lse.view(2, N, 2, G)
+    nan = torch.zeros(o.shape, dtype=torch.bool, device=o.device)
+    nan[:, 2, 0] = True
+    nan[:, 4, 1, :, 9] = True
+    assert torch.equal(torch.isnan(o), nan)
+    assert torch.equal(o[~nan], w[~nan])
+    gone = torch.zeros(z.shape, dtype=torch.bool, device=o.device)
+    gone[:, 2, 0] = True
+    assert torch.equal(torch.isnan(z), gone) and torch.equal(z[~gone], wl.view(2, N, 2, G)[~gone])
+
+
+def test_a_nan_value_of_the_context_reaches_its_column():
+    p = Problem8(DEV, B=1, Hkv=1, G=4, T=(700,), N=2, seed=6)
+    p.codes[1][0, 0, 333, 50] = NAN_CODE
+    p.upload()
+    out, lse = run_decode8(p)
+    sync()
+    nan = torch.zeros((1, 2, 4, 128), dtype=torch.bool, device=DEV)
+    nan[..., 50] = True
+    assert torch.equal(torch.isnan(out), nan) and not torch.isnan(lse).any()
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_queries_that_are_not_finite(io):
+    """An infinite query element makes scores of +inf, -inf or NaN with the keys' signs; a query whose scores are all -inf is
+    like one that attends to nothing, one with +inf or NaN among them gives NaN, others are not touched."""
+    p = Problem8(DEV, B=1, Hkv=1, G=4, T=(150,), N=1, io=io, draft=False, seed=8)
+    p.codes[0][0, 0, :150, 3] = 0x38                  # keys of one sign in column 3
+    p.refresh()
+    p.q[0, 0, 0, 3], p.q[0, 0, 1, 3], p.q[0, 0, 2, 60] = float("-inf"), float("inf"), float("nan")
+    p.upload()
+    out, lse = run_decode8(p)
+    q = p.q.clone()
+    p.q = torch.nan_to_num(q, nan=0.0, posinf=0.0, neginf=0.0)
+    p.upload()
+    want, wl = run_decode8(p)
+    sync()
+    assert torch.all(out[0, 0, 0] == 0) and lse[0, 0, 0] == float("-inf")
+    assert torch.isnan(out[0, 0, 1]).all() and torch.isnan(out[0, 0, 2]).all()
+    assert torch.equal(out[0, 0, 3], want[0, 0, 3]) and lse[0, 0, 3] == wl[0, 0, 3]
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_decode8_leaves_out_pages_out_of_range(io):
+    p = Problem8(DEV, B=2, Hkv=2, T=(500, 130), N=3, io=io, layout="pages", seed=9).upload()
+    gone = {0: [1, 4], 1: [0]}
+    table = p.pages["block_table"]
+    for b, blocks in gone.items():
+        for j, bad in zip(blocks, (-1, 1 << 30)):
+            table[b, j] = bad
+    out, lse = run_decode8(p)
+    sync()
+    see = p.see
+
+    def without(b, h):
+        x = see(b, h)
+        for j in gone[b]:
+            x[:, j * p.L:(j + 1) * p.L] = False
+        return x
+    p.see = without
+    p.check(out, lse)
+
+
+def test_scales_far_apart():
+    """Blocks whose scales lie up to 2^60 apart, and one of scale 0."""
+    p = Problem8(DEV, B=1, Hkv=2, G=4, T=(640,), N=2, seed=10)
+    for s, (lo, hi) in zip(p.scales, ((-14, -6), (-50, 10))):
+        rng = np.random.default_rng(1)
+        s[:, :, :10] = 2.0 ** rng.integers(lo, hi, size=(1, 2, 10))
+    p.scales[0][0, 0, 3] = p.scales[1][0, 1, 4] = 0.0
+    p.refresh()
+    p.upload()
+    out, lse = run_decode8(p)
+    sync()
+    p.check(out, lse)
+
+
+def test_offsets_past_32_bits():
+    """A row stride that takes later tokens past 4 GiB."""
+    B, Hkv, d, cap, st = 1, 1, 128, 2048, (1 << 22)
+    need = cap * st
+    free, _ = torch.cuda.mem_get_info()
+    assert free > 3 * need
+    flat = torch.zeros(2 * need, dtype=torch.uint8, device=DEV)
+    k, v = (flat[i * need:(i + 1) * need].as_strided((B, Hkv, cap, d), (need, need, st, 1)) for i in range(2))
+    cfg = cobs.Config(batch=B, num_q_heads=2, num_kv_heads=Hkv, head_dim=d, max_seq_len=cap, rank=0, budget=0, window=0)
+    near = tokens.new_cache8(cfg, DEV)
+    far = tokens.Cache8(k, v, torch.zeros_like(near.k_scale), torch.zeros_like(near.v_scale))
+    gen = torch.Generator().manual_seed(2)
+    x = torch.randn((B, cap, 4, d), generator=gen).bfloat16().to(DEV)
+    lens = torch.zeros(1, dtype=torch.int32, device=DEV)
+    full = torch.full((1,), cap, dtype=torch.int32, device=DEV)
+    got = []
+    for c8 in (near, far):
+        tokens.cobs_append8(cfg, x[:, :, 2:3], x[:, :, 3:], c8, lens)
+        out, lse = torch.empty((B, 2, 2, d), dtype=torch.bfloat16, device=DEV), torch.empty((B, 2, 2), device=DEV)
+        tokens.cobs_decode8(cfg, x[:, :2, :2].contiguous(), c8, full, None, None, out, tokens.new_decode8_workspace(cfg, 2, DEV), lse=lse)
+        ko, vo = (torch.zeros((B, Hkv, cap, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        tokens.cobs_unpack8(cfg, c8, full, ko, vo)
+        got.append((out, lse, ko, vo, c8.k_scale))
+    sync()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- unpacked --
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("src,dst", [("contiguous", "contiguous"), ("pages", "pages"), ("strided", "pages"), ("pages", "contiguous")])
+@pytest.mark.parametrize("which", [dict(), dict(first_block=1, num_blocks=2), dict(last=1), dict(last=3), dict(first_block=2), dict(num_blocks=0)], ids=_ids)
+@pytest.mark.parametrize("d,L,T", [(128, 64, (300, 64, 0, 1)), (64, 32, (65, 127, 33, 200)), (128, 128, (129, 5, 400, 256))])
+def test_unpack8_matches_the_definition(d, L, T, which, src, dst, kv):
+    p = Problem8(DEV, B=4, Hkv=2, G=1, d=d, L=L, T=T, N=1, draft=False, layout=src, seed=3).upload()
+    p.cfg.kv_dtype = kv
+    nb = p.cap // L
+    pages = dict(p.pages)
+    if dst == "pages":
+        rng = np.random.default_rng(4)
+        table = torch.from_numpy(rng.permutation(4 * nb + 5)[:4 * nb].astype(np.int32)).view(4, nb)
+        table[0, 0] = -1                               # left out
+        shape = (4 * nb + 5, 2, L, d)
+        pages.update(out_block_table=table.to(DEV), out_num_pages=4 * nb + 5)
+    else:
+        shape = (4, 2, p.cap, d)
+    k, v = (torch.full(shape, 9.0, dtype=TORCH[kv], device=DEV) for _ in range(2))
+    tokens.cobs_unpack8(p.cfg, p.cache8, p.seq, k, v, **which, **pages)
+    sync()
+    for got, x in ((k, p.k), (v, p.v)):
+        want = torch.full(shape, 9.0, dtype=TORCH[kv])
+        for b in range(4):
+            blocks = -(-T[b] // L)
+            if "last" in which:
+                js = range(max(0, blocks - which["last"]), blocks)
+            else:
+                j0 = which.get("first_block", 0)
+                js = range(j0, min(blocks, j0 + which.get("num_blocks", nb - j0)))
+            for j in js:
+                n = min(L, T[b] - j * L)
+                rows = x[b, :, j * L:j * L + n].float().to(TORCH[kv])      # (one rounding: codes times scales fit fp32)
+                if dst == "pages":
+                    if table[b, j] >= 0:
+                        want[table[b, j].long(), :, :n] = rows
+                else:
+                    want[b, :, j * L:j * L + n] = rows
+        assert torch.equal(got.cpu(), want)
+
+
+# ------------------------------------------------------------------ in turn --
+def test_a_serving_loop_runs_them_in_turn():
+    """Prompts appended (rotated, 8 bits), records from unpacked blocks, then decode steps: the new token's append with its queries' rotation,
+    its block's record, selection, attention over the selection; a draft's attention at the end.  Checked against fp64
+    attention over the unpacked cache, step by step."""
+    say("serving loop over an 8-bit cache")
+    B, Hkv, G, d, L, cap, s, w = 2, 2, 4, 128, 64, 1024, 4, 96
+    cfg = cobs.Config(batch=B, num_q_heads=Hkv * G, num_kv_heads=Hkv, head_dim=d, max_seq_len=cap, rank=2, budget=s, window=w)
+    gen = torch.Generator().manual_seed(1)
+    nb = cap // L
+    perm = torch.randperm(B * nb, generator=gen).to(torch.int32).view(B, nb).to(DEV)
+    c8 = tokens.new_cache8(cfg, DEV, num_pages=B * nb)
+    on = dict(block_table=perm, num_pages=B * nb)
+    rope = tokens.Rope(tokens.rope_frequencies(d, base=5e5, factor=4.0, original_len=256).to(DEV), False, 1.1)
+    lens, after = torch.zeros(B, dtype=torch.int32, device=DEV), torch.zeros(B, dtype=torch.int32, device=DEV)
+    given = torch.tensor([700, 433], dtype=torch.int32, device=DEV)
+
+    def project(n):
+        x = torch.randn((B, n, Hkv * (G + 2), d), generator=gen).bfloat16().to(DEV)
+        return x[:, :, :Hkv * G], x[:, :, Hkv * G:Hkv * (G + 1)], x[:, :, Hkv * (G + 1):]
+
+    # the records' keys: pages of a bf16 pool, here one for every block
+    kb, vb = (torch.zeros((B * nb, Hkv, L, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    rec = cobs.new_summaries(cfg, DEV)
+    _, k, v = project(700)
+    tokens.cobs_append8(cfg, k, v, c8, lens, new_lens=given, rope=rope, new_seq_lens=after, **on)
+    lens.copy_(after)
+    tokens.cobs_unpack8(cfg, c8, lens, kb, vb, out_block_table=perm, out_num_pages=B * nb, **on)
+    cobs.cobs_build_block_stats(cfg, kb, vb, lens, rec, **on)
+    ws, dws = cobs.new_workspace(cfg, cobs.OP_SELECT, DEV), tokens.new_decode8_workspace(cfg, 4, DEV)
+    sel = torch.empty((B, Hkv, s), dtype=torch.int32, device=DEV)
+    table = R.e4m3_values()
+
+    def cached(b, h, T):
+        out = []
+        for codes, scale in ((c8.k, c8.k_scale), (c8.v, c8.v_scale)):
+            pages = perm[b].long()
+            c = codes.view(torch.uint8)[pages, h].cpu().numpy().reshape(cap, d)[:T]
+            out.append(table[c] * np.repeat(f64(scale[pages, h]), L)[:T, None])
+        return out
+
+    for step in range(3):
+        q, k, v = project(1)
+        qr = torch.empty((B, 1, Hkv * G, d), device=DEV)
+        tokens.cobs_append8(cfg, k, v, c8, lens, rope=rope, q=q, q_out=qr, new_seq_lens=after, **on)
+        lens.copy_(after)
+        tokens.cobs_unpack8(cfg, c8, lens, kb, vb, last=1, out_block_table=perm, out_num_pages=B * nb, **on)
+        for j in {int((t - 1) // L) for t in lens.tolist()}:
+            cobs.cobs_build_block_stats(cfg, kb, vb, lens, rec, first_block=j, num_blocks=1, **on)
+        cobs.cobs_select(cfg, qr, rec, lens, sel, ws)
+        out, lse = torch.empty_like(qr), torch.empty((B, 1, Hkv * G), device=DEV)
+        tokens.cobs_decode8(cfg, qr, c8, lens, None, None, out, dws, sel=sel, lse=lse, **on)
+        # the same attention over the unpacked cache
+        same, sl = torch.empty((B, Hkv * G, d), device=DEV), torch.empty((B, Hkv * G), device=DEV)
+        cobs.cobs_sparse_decode(cfg, qr, kb, vb, lens, sel, same, cobs.new_workspace(cfg, cobs.OP_DECODE, DEV), lse=sl, **on)
+        sync()
+        for b in range(B):
+            T = int(lens[b])
+            for h in range(Hkv):
+                K, V = cached(b, h, T)
+                picked = [x for x in sel[b, h].tolist() if x >= 0]
+                see = O.visible(T, 0, 1, L, w, picked)
+                qq = f64(qr)[b].reshape(1, Hkv, G, d)[:, h]
+                want, wl = O.tree_attention(qq, K, V, see, cfg.scale)
+                # fp32 arithmetic throughout: scores of magnitude below 64 are within (3 d + 6) half steps of it
+                e = 64 * (3 * d + 6) * 2.0 ** -24
+                t = np.nonzero(see[0])[0]
+                top = np.abs(V[t]).max()
+                assert (cfg.scale * (np.abs(qq[0]) @ np.abs(K[t]).T)).max() < 64
+                assert np.all(np.abs(f64(out)[b, 0, h * G:(h + 1) * G] - want[0]) <= 4 * e * top)
+                assert np.all(np.abs(f64(same)[b, h * G:(h + 1) * G] - want[0]) <= 4 * e * top + 2.0 ** -16 * top)
+                assert np.all(np.abs(f64(lse)[b, 0, h * G:(h + 1) * G] - wl[0]) <= 2 * e)
+    # a draft of four behind the context, of which two tokens are accepted (and two places are written again)
+    q, k, v = project(4)
+    at = lens.view(B, 1) + torch.tensor([0, 1, 1, 2], dtype=torch.int32, device=DEV)
+    qr = torch.empty((B, 4, Hkv * G, d), device=DEV)
+    tokens.cobs_append8(cfg, k, v, c8, lens, rope=rope, positions=at, q=q, q_out=qr, new_seq_lens=after, **on)
+    bits = [1, 3, 5, 11]
+    mask = torch.tensor([bits] * B, dtype=torch.int64, device=DEV)
+    out = torch.empty_like(qr)
+    tokens.cobs_decode8(cfg, qr, c8, lens, after - lens, mask, out, dws, **on)
+    sync()
+    for b in range(B):
+        T = int(lens[b])
+        for h in range(Hkv):
+            K, V = cached(b, h, T + 4)
+            want, _ = O.tree_attention(f64(qr)[b].reshape(4, Hkv, G, d)[:, h], K, V, O.visible(T, 4, 4, L, w, None, bits), cfg.scale)
+            e = 64 * (3 * d + 6) * 2.0 ** -24
+            assert np.all(np.abs(f64(out)[b].reshape(4, Hkv, G, d)[:, h] - want) <= 4 * e * np.abs(V).max())
+
+
+def test_streams_and_graphs():
+    """Two problems interleaved on two streams, and every operator captured and replayed with eager work between, give the bits of the
+    calls one after the other."""
+    ps = [Problem8(DEV, B=2, T=(700, 200), N=16, G=8, io="bf16", seed=1).upload(),
+          Problem8(DEV, B=1, T=(4000,), N=5, s=6, w=64, seed=2).upload()]
+    want = [run_decode8(p) for p in ps]
+    sync()
+    streams = [torch.cuda.Stream() for _ in ps]
+    wss = [tokens.new_decode8_workspace(p.cfg, p.N, DEV) for p in ps]
+    got = []
+    for _ in range(4):
+        for p, st, ws in zip(ps, streams, wss):
+            with torch.cuda.stream(st):
+                got.append(run_decode8(p, ws=ws))
+    sync()
+    for i, (o, z) in enumerate(got):
+        assert torch.equal(o, want[i % 2][0]) and torch.equal(z, want[i % 2][1])
+
+    a8 = Appending(DEV, B=2, N=40, T=(70, 3), eight=True, seed=4).fresh()
+    a = Appending(DEV, B=2, N=3, T=(70, 3), seed=5).fresh()
+    new = torch.tensor([40, 33], dtype=torch.int32, device=DEV)
+    ko, vo = (torch.zeros((2, 2, a8.cap, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    at = torch.arange(6, dtype=torch.int32, device=DEV).view(2, 3)
+    turned = torch.zeros((2, 3, 4, 128), device=DEV)
+    p = ps[0]
+    out, lse = torch.zeros_like(p.qd), torch.zeros((p.B, p.N, 16), device=DEV)
+    outs = (*a8.cache8[:2], *a8.cache8[2:], a8.q_out, a8.after, a.kd, a.vd, a.q_out, ko, vo, turned, out, lse)
+    before = [x.clone() for x in outs]
+
+    def calls():
+        tokens.cobs_append8(a8.cfg, a8.kn, a8.vn, a8.cache8, a8.lens, new_lens=new, rope=a8.rope, q=a8.qd, q_out=a8.q_out, new_seq_lens=a8.after)
+        tokens.cobs_append(a.cfg, a.kn, a.vn, a.kd, a.vd, a.lens, rope=a.rope, q=a.qd, q_out=a.q_out)
+        tokens.cobs_unpack8(a8.cfg, a8.cache8, a8.after, ko, vo)
+        tokens.cobs_rotate(a.qd, a.rope, at, turned)
+        tokens.cobs_decode8(p.cfg, p.qd, p.cache8, p.seq, p.drafts, p.mask, out, wss[0], lse=lse)
+
+    calls()
+    sync()
+    eager = [x.clone() for x in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        calls()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            calls()
+    for _ in range(3):
+        for x, y in zip(outs, before):
+            x.copy_(y)
+        run_decode8(ps[1])                       # eager work between the replays
+        sync()
+        graph.replay()
+        sync()
+        for x, e in zip(outs, eager):
+            assert torch.equal(x.view(torch.uint8), e.view(torch.uint8))      # (bits: the cache holds NaN codes too)
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_random_problems(seed):
+    rng = np.random.default_rng(seed + 40)
+    for _ in range(4):
+        d, L = int(rng.choice([64, 128])), int(rng.choice([32, 64, 128]))
+        B, Hkv, G = int(rng.integers(1, 5)), int(rng.integers(1, 4)), int(rng.choice([1, 2, 4, 8, 16]))
+        layout = str(rng.choice(["contiguous", "pages", "strided"]))
+        io = str(rng.choice(["f32", "bf16"]))
+        N = int(rng.integers(1, 100))
+        shape = dict(B=B, Hkv=Hkv, G=G, d=d, L=L, N=N, T=[int(x) for x in rng.integers(0, 300, B)], new=[int(x) for x in rng.integers(0, N + 1, B)],
+                     r=int(rng.choice([0, 16, d // 2, d])), inter=bool(rng.integers(2)), shift=[None, 1000][int(rng.integers(2))], seed=int(rng.integers(1 << 30)))
+        say(f"append {shape} {layout} {io}")
+        p = Appending(DEV, io=io, layout=layout, eight=True, **shape).fresh().call()
+        a = Appending(DEV, io=io, layout=layout, kv=str(rng.choice(["f32", "bf16"])), spread=False, **shape).fresh().call()
+        sync()
+        p.check_cache8()
+        p.check_queries()
+        a.check_cache()
+        n = int(rng.integers(1, 65))
+        s = int(rng.integers(-1, 6))
+        shape = dict(B=B, Hkv=Hkv, G=G, d=d, L=L, T=[int(x) for x in rng.integers(0, 1500, B)], N=n, drafts=[int(x) for x in rng.integers(0, n + 1, B)],
+                     draft=bool(rng.integers(2)), s=s, w=int(rng.integers(0, 200)), seed=int(rng.integers(1 << 30)))
+        say(f"decode8 {shape} {layout} {io}")
+        p = Problem8(DEV, io=io, layout=layout, **shape).upload()
+        out, lse = run_decode8(p)
+        sync()
+        p.check(out, lse)
