@@ -25,8 +25,9 @@ extern "C" {
 
 /* Heads of tokens as a projection leaves them: element (b, i, h, e) at
  *   p + b*stride_b + i*stride_n + h*stride_h + e   (strides in elements, e < d contiguous).
- * p: 16-byte aligned; strides >= 0 and multiples of 16 bytes' worth of elements.  Of what a
- * call writes no two elements may share memory (a stride below d, of a dimension longer than 1, is refused). */
+ * p: 16-byte aligned; strides >= 0 and multiples of 16 bytes' worth of elements (that of a dimension
+ * of 1 is not used).  Of what a call writes no two elements may share memory: sorted by stride, each
+ * dimension's stride has to span the ones before it, or the call is refused. */
 typedef struct {
   void* p;
   int64_t stride_b, stride_n, stride_h;

@@ -71,18 +71,25 @@ def _cache_fits(cfg, dtype, dev, k, v, block_table, num_pages):
     return _KV(k.data_ptr(), v.data_ptr(), 0, 0, 0, block_table.data_ptr(), num_pages)
 
 
-def _queries_fit(cfg, dtype, q, k, v, seq_lens, draft_lens, tree_mask, sel, block_table, num_pages, *more):
-    """The C view of the cache if every argument of a call with queries fits, else None; `more` as for _fits."""
-    if q is None or k is None or v is None or seq_lens is None or (draft_lens is None) != (tree_mask is None):
-        return None
+def _queries_alone_fit(cfg, q, seq_lens, draft_lens, tree_mask, sel, *more):
+    """Whether the arguments of a call with queries fit, but for the cache; `more` as for _fits."""
+    if (draft_lens is None) != (tree_mask is None):
+        return False
     dev, shape = _gpu(q), q.shape
     if (len(shape) != 4 or shape[0] != cfg.batch or shape[2] != cfg.num_q_heads or shape[3] != cfg.head_dim or
             not 1 <= shape[1] <= MAX_QUERIES or q.dtype not in _IO or (tree_mask is not None and tree_mask.shape != shape[:2])):
+        return False
+    return _fits(dev, (q, q.dtype, 0), (seq_lens, torch.int32, cfg.batch), (draft_lens, torch.int32, cfg.batch),
+                 (tree_mask, torch.int64, 0), (sel, torch.int32, _units(cfg) * cfg.budget), *more)
+
+
+def _queries_fit(cfg, dtype, q, k, v, seq_lens, draft_lens, tree_mask, sel, block_table, num_pages, *more):
+    """The C view of the cache if every argument of a call with queries fits, else None; `more` as for _fits."""
+    if q is None or k is None or v is None or seq_lens is None:
         return None
-    if not _fits(dev, (q, q.dtype, 0), (seq_lens, torch.int32, cfg.batch), (draft_lens, torch.int32, cfg.batch),
-                 (tree_mask, torch.int64, 0), (sel, torch.int32, _units(cfg) * cfg.budget), *more):
+    if not _queries_alone_fit(cfg, q, seq_lens, draft_lens, tree_mask, sel, *more):
         return None
-    return _cache_fits(cfg, dtype, dev, k, v, block_table, num_pages)
+    return _cache_fits(cfg, dtype, _gpu(q), k, v, block_table, num_pages)
 
 
 def tree_workspace_bytes(cfg, num_queries):

@@ -9,18 +9,19 @@ hipError_t launch_decode8_bf16_d128(const Decode8Params& p, int tiles, int grid,
 hipError_t launch_decode8_f32_d64(const Decode8Params& p, int tiles, int grid, hipStream_t st);
 hipError_t launch_decode8_f32_d128(const Decode8Params& p, int tiles, int grid, hipStream_t st);
 
-// Tiles of 16 query rows that a workgroup takes, a wave one of them or two; frames that its waves take at a time.
-static int wave_tiles(const AttendParams& a, int tiles) { return tiles == 1 || (a.d == 128 && !a.io_bf16) ? 1 : 2; }
+// Tiles of 16 query rows that a workgroup takes: 1 or 2 (decode8_kernel), 4 or 8 (decode8_many_kernel); frames that its
+// waves take at a time.
 static int row_tiles(const AttendParams& a) {
   const int M = a.N * a.G;
-  return M <= 16 ? 1 : (M <= 32 ? 2 : (M <= 64 || wave_tiles(a, 8) == 1 ? 4 : 8));
+  const bool two = a.d == 64 || a.io_bf16;              // tiles a wave
+  return M <= 16 ? 1 : (M <= 32 && two ? 2 : (M <= 64 || !two ? 4 : 8));
 }
-static int pass_frames(const AttendParams& a, int tiles) { return 4 * wave_tiles(a, tiles) / tiles; }
+static int pass_frames(int tiles) { return tiles <= 2 ? 4 : 2; }
 
 static void decode8_plan(const AttendParams& a, int* tiles, int* mtiles, int* nsplit) {
   *tiles = row_tiles(a);
   *mtiles = (a.N * a.G + *tiles * 16 - 1) / (*tiles * 16);
-  const int step = pass_frames(a, *tiles);
+  const int step = pass_frames(*tiles);
   const int64_t passes = (max_frames(a) + step - 1) / step;
   *nsplit = parts_of(passes, (int64_t)a.B * a.hkv * *mtiles, 2.0, 1 << 30, 128);
 }
@@ -49,7 +50,7 @@ hipError_t launch_decode8(const Decode8Params& q, hipStream_t st) {
   decode8_plan(t.a, &tiles, &t.mtiles, &t.nsplit);
   t.units = t.a.B * t.a.hkv;
   t.even = parts_by_length(t.a, t.nsplit);
-  t.step = pass_frames(t.a, tiles);
+  t.step = pass_frames(tiles);
   t.part_o = t.part_ml + ml_bytes((size_t)t.units * t.nsplit * t.a.N * t.a.G) / sizeof(float);
   // eight XCDs: a multiple of 8 workgroup slots (see decode8_kernel)
   const int64_t groups = ((int64_t)t.units * t.nsplit + 7) / 8 * 8, grid = groups * t.mtiles;

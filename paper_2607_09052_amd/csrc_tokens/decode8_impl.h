@@ -10,10 +10,12 @@ hipError_t launch_decode8_kernels(const Decode8Params& p, int tiles, int grid, h
   const dim3 g(grid), t(kTreeThreads);
   // (two tiles a wave with three parts of 128-element queries spill)
   constexpr int QT = D == 128 && PARTS == 3 ? 1 : 2;
-  if (tiles == 1) hipLaunchKernelGGL((decode8_kernel<D, PARTS, 1, 1>), g, t, 0, st, p);
-  else if (tiles == 2) hipLaunchKernelGGL((decode8_kernel<D, PARTS, QT, 2 / QT>), g, t, 0, st, p);
-  else if (tiles == 4) hipLaunchKernelGGL((decode8_kernel<D, PARTS, QT, 4 / QT>), g, t, 0, st, p);
-  else if constexpr (QT == 2) hipLaunchKernelGGL((decode8_kernel<D, PARTS, 2, 4>), g, t, 0, st, p);
+  if (tiles == 1) hipLaunchKernelGGL((decode8_kernel<D, PARTS, 1>), g, t, 0, st, p);
+  else if (tiles == 4) hipLaunchKernelGGL((decode8_many_kernel<D, PARTS, 1>), g, t, 0, st, p);
+  else if constexpr (QT == 2) {
+    if (tiles == 2) hipLaunchKernelGGL((decode8_kernel<D, PARTS, 2>), g, t, 0, st, p);
+    else hipLaunchKernelGGL((decode8_many_kernel<D, PARTS, 2>), g, t, 0, st, p);
+  }
   return hipGetLastError();
 }
 

@@ -12,18 +12,25 @@ namespace {
 
 bool io_type(cobs_dtype_t t) { return t == COBS_F32 || t == COBS_BF16; }
 
-cobs_status_t check_heads(const cobs_heads_t* x, cobs_dtype_t type) {
+// Heads [batch, tokens, heads, d]; the stride of a dimension of 1 is not used and may be anything.
+struct HeadsShape {
+  int64_t batch, tokens, heads, d;
+};
+
+cobs_status_t check_heads(const cobs_heads_t* x, cobs_dtype_t type, const HeadsShape& n) {
   if (!x || !x->p || !aligned(x->p, 16)) return COBS_ERR_INVALID_ARG;
   const int64_t vec = type == COBS_F32 ? 4 : 8;          // elements of 16 bytes
-  for (const int64_t s : {x->stride_b, x->stride_n, x->stride_h})
-    if (s < 0 || s % vec) return COBS_ERR_INVALID_ARG;
+  if (n.batch > 1 && (x->stride_b < 0 || x->stride_b % vec)) return COBS_ERR_INVALID_ARG;
+  if (n.tokens > 1 && (x->stride_n < 0 || x->stride_n % vec)) return COBS_ERR_INVALID_ARG;
+  if (n.heads > 1 && (x->stride_h < 0 || x->stride_h % vec)) return COBS_ERR_INVALID_ARG;
   return COBS_OK;
 }
 
-// Whether no two elements of [batch, tokens, heads, d] share memory: each stride spans the dimensions of smaller strides.
-bool apart(const cobs_heads_t* x, int64_t batch, int64_t tokens, int64_t heads, int64_t d) {
-  int64_t size[3] = {batch, tokens, heads}, stride[3] = {x->stride_b, x->stride_n, x->stride_h};
-  int64_t extent = d;
+// Whether no two elements share memory: each stride spans the dimensions of smaller strides.
+bool apart(const cobs_heads_t* x, const HeadsShape& n) {
+  int64_t size[3] = {n.batch, n.tokens, n.heads};
+  const int64_t stride[3] = {x->stride_b, x->stride_n, x->stride_h};
+  int64_t extent = n.d;
   for (int k = 0; k < 3; ++k) {
     int at = -1;
     for (int i = 0; i < 3; ++i)
@@ -51,14 +58,13 @@ RopeView view_rope(const cobs_rope_t* r, const int32_t* positions) {
 }
 
 // Queries and where they go: both checked, and the one itself or apart from the other.
-cobs_status_t check_out(const cobs_heads_t* x, cobs_dtype_t in, const cobs_heads_t* y, cobs_dtype_t out, int64_t batch,
-                        int64_t tokens, int64_t heads, int64_t d) {
+cobs_status_t check_out(const cobs_heads_t* x, cobs_dtype_t in, const cobs_heads_t* y, cobs_dtype_t out, const HeadsShape& n) {
   cobs_status_t s;
   if (!io_type(in) || !io_type(out)) return COBS_ERR_INVALID_ARG;
-  if ((s = check_heads(x, in)) != COBS_OK || (s = check_heads(y, out)) != COBS_OK) return s;
-  if (!apart(y, batch, tokens, heads, d)) return COBS_ERR_INVALID_ARG;
-  const bool same = (batch == 1 || x->stride_b == y->stride_b) && (tokens == 1 || x->stride_n == y->stride_n) &&
-                    (heads == 1 || x->stride_h == y->stride_h) && in == out;
+  if ((s = check_heads(x, in, n)) != COBS_OK || (s = check_heads(y, out, n)) != COBS_OK) return s;
+  if (!apart(y, n)) return COBS_ERR_INVALID_ARG;
+  const bool same = (n.batch == 1 || x->stride_b == y->stride_b) && (n.tokens == 1 || x->stride_n == y->stride_n) &&
+                    (n.heads == 1 || x->stride_h == y->stride_h) && in == out;
   return x->p == y->p && !same ? COBS_ERR_INVALID_ARG : COBS_OK;
 }
 
@@ -72,11 +78,12 @@ cobs_status_t new_tokens(const cobs_config_t* cfg, const cobs_heads_t* k_new, co
   if (!io_type(in_dtype) || num_new < 1 || !seq_lens) return COBS_ERR_INVALID_ARG;
   if (new_seq_lens && (new_seq_lens == seq_lens || new_seq_lens == new_lens || new_seq_lens == positions))
     return COBS_ERR_INVALID_ARG;
-  if ((s = check_heads(k_new, in_dtype)) != COBS_OK || (s = check_heads(v_new, in_dtype)) != COBS_OK) return s;
+  const HeadsShape kv_shape = {cfg->batch, num_new, cfg->num_kv_heads, d}, q_shape = {cfg->batch, num_new, cfg->num_q_heads, d};
+  if ((s = check_heads(k_new, in_dtype, kv_shape)) != COBS_OK || (s = check_heads(v_new, in_dtype, kv_shape)) != COBS_OK) return s;
   if (rope && (s = check_rope(rope, d)) != COBS_OK) return s;
   if ((q == nullptr) != (q_out == nullptr)) return COBS_ERR_INVALID_ARG;
   if (q) {
-    if ((s = check_out(q, in_dtype, q_out, q_dtype, cfg->batch, num_new, cfg->num_q_heads, d)) != COBS_OK) return s;
+    if ((s = check_out(q, in_dtype, q_out, q_dtype, q_shape)) != COBS_OK) return s;
     if (q_out->p == k_new->p || q_out->p == v_new->p) return COBS_ERR_INVALID_ARG;
     t->hq = cfg->num_q_heads;
     t->q = view_heads(q, in_dtype);
@@ -129,7 +136,7 @@ cobs_status_t cobs_rotate(const cobs_heads_t* x, cobs_dtype_t in_dtype, int32_t 
   if ((s = check_rope(rope, head_dim)) != COBS_OK) return s;
   const int64_t tokens = (int64_t)batch * num_tokens;
   if (tokens > ((int64_t)1 << 31) / num_heads) return COBS_ERR_UNSUPPORTED;
-  if ((s = check_out(x, in_dtype, out, out_dtype, batch, num_tokens, num_heads, head_dim)) != COBS_OK) return s;
+  if ((s = check_out(x, in_dtype, out, out_dtype, {batch, num_tokens, num_heads, head_dim})) != COBS_OK) return s;
   AppendParams p = {};
   p.t.rope = view_rope(rope, positions);
   p.t.q = view_heads(x, in_dtype);

@@ -8,32 +8,22 @@ projection's output go in as they are.
 
 import ctypes
 import math
+import struct
 from typing import NamedTuple
 
 import torch
 
 from . import cobs
-from .cache import _IO, _call, _queries, _struct
+from .cache import _IO, _cache_fits, _call, _queries, _queries_alone_fit, _struct
 from .cobs import CobsError, _fits, _gpu, _kv, _need, _opt, _ptr, _same_gpu, _stream, _ws
 
 E4M3 = torch.float8_e4m3fn
 
 
-class _Heads(ctypes.Structure):
-    _fields_ = [("p", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64),
-                ("stride_h", ctypes.c_int64)]
-
-
-class _Rope(ctypes.Structure):
-    _fields_ = [("inv_freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
-                ("scale", ctypes.c_float)]
-
-
-class _KV8(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
-                ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
-                ("block_table", ctypes.c_void_p), ("num_pages", ctypes.c_int64)]
-
+# The C structs cobs_heads_t, cobs_rope_t and cobs_kv8_t, packed (a third of the time of a ctypes.Structure's making).
+_pack_heads = struct.Struct("@Pqqq").pack
+_pack_rope = struct.Struct("@Piif4x").pack
+_pack_kv8 = struct.Struct("@PPPPqqqPq").pack
 
 _P, _I, _Z, _E = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_int
 _APPEND = [_P, _P, _P, _E, _I, _P, _P, _P, _P, _P, _P, _P, _E, _P, _P]
@@ -116,10 +106,8 @@ def _heads_fit(t, dtype, dev, shape):
     """The C view of heads [B, N, H, d] on GPU `dev`, or None if anything does not fit."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
         return None
-    s = t.stride()
-    if s[3] != 1:
-        return None
-    return _Heads(t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+    b, n, h, e = t.stride()
+    return _pack_heads(t.data_ptr(), b, n, h) if e == 1 else None
 
 
 def _heads(name, t, dtype, shape):
@@ -127,75 +115,142 @@ def _heads(name, t, dtype, shape):
         raise CobsError(f"{name} must be {dtype or 'torch.float32 or torch.bfloat16'}")
     if t.dim() != 4 or tuple(t.shape) != tuple(shape) or t.stride(-1) != 1:
         raise CobsError(f"{name} must have shape {list(shape)} with a dense head dimension, got {list(t.shape)}")
-    return _Heads(t.data_ptr(), *(s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape[:3])))
+    return _pack_heads(t.data_ptr(), *t.stride()[:3])
 
 
-def _rope(rope, positions, tokens):
-    """The C form of a rotation whose tensors fit, and its tensors."""
+def _rope_form(rope):
+    freq, interleaved, scale = rope
+    return _pack_rope(freq.data_ptr(), 2 * freq.numel(), bool(interleaved), float(scale))
+
+
+def _rope(rope, positions, shape):
+    """Checks of a rotation and its positions."""
     if not isinstance(rope, Rope):
         raise CobsError("rope must be a tokens.Rope")
     _need("inv_freq", rope.inv_freq, torch.float32, 1)
     if positions is not None:
-        _need("positions", positions, torch.int32, tokens)
-    return _Rope(rope.inv_freq.data_ptr(), 2 * rope.inv_freq.numel(), bool(rope.interleaved), float(rope.scale))
+        _need("positions", positions, torch.int32, shape[0] * shape[1])
+        if tuple(positions.shape) != tuple(shape):
+            raise CobsError(f"positions must have shape {list(shape)}, got {list(positions.shape)}")
 
 
 def cobs_rotate(x, rope, positions, out, stream=None):
     """out [B, N, H, d] = x with the rotary positions `positions` [B, N] applied; out may be x."""
-    if x is None or x.dim() != 4:
-        raise CobsError("x must have shape [B, N, H, d]")
-    shape = tuple(x.shape)
-    hx = _heads("x", x, None, shape)
-    hy = _heads("out", out, None, shape)
-    if positions is None:
-        raise CobsError("positions is required")
-    r = _rope(rope, positions, shape[0] * shape[1])
-    if tuple(positions.shape) != shape[:2]:
-        raise CobsError(f"positions must have shape {list(shape[:2])}, got {list(positions.shape)}")
-    _same_gpu(x=x, out=out, positions=positions, inv_freq=rope.inv_freq)
-    _call(lib().cobs_rotate, x, ctypes.byref(hx), _IO[x.dtype], *shape, ctypes.byref(r), positions.data_ptr(),
-          ctypes.byref(hy), _IO[out.dtype], _stream(stream, x))
+    hx = hy = None
+    if x is not None and out is not None and positions is not None and type(rope) is Rope and len(x.shape) == 4:
+        dev, shape = _gpu(x), x.shape
+        if (x.dtype in _IO and out.dtype in _IO and positions.shape == shape[:2] and
+                _fits(dev, (positions, torch.int32, 0), (rope[0], torch.float32, 1))):
+            hx, hy = _heads_fit(x, x.dtype, dev, shape), _heads_fit(out, out.dtype, dev, shape)
+    if hx is None or hy is None:
+        if x is None or x.dim() != 4:
+            raise CobsError("x must have shape [B, N, H, d]")
+        shape = tuple(x.shape)
+        hx, hy = _heads("x", x, None, shape), _heads("out", out, None, shape)
+        if positions is None:
+            raise CobsError("positions is required")
+        _rope(rope, positions, shape[:2])
+        _same_gpu(x=x, out=out, positions=positions, inv_freq=rope.inv_freq)
+    _call(lib().cobs_rotate, x, hx, _IO[x.dtype], *shape, _rope_form(rope), positions.data_ptr(), hy, _IO[out.dtype],
+          _stream(stream, x))
 
 
-def _append(fn, cfg, c, view, k_new, v_new, tensors, seq_lens, new_lens, rope, positions, q, q_out, new_seq_lens, stream):
-    """The call of cobs_append and cobs_append8 into the cache of C form `view` and of `tensors`."""
-    if k_new is None or v_new is None or k_new.dim() != 4:
+def _new_fit(cfg, dev, k_new, v_new, seq_lens, new_lens, rope, positions, q, q_out, new_seq_lens):
+    """The C views (k_new, v_new, q, q_out, rope) of an append's arguments, or None if anything does not fit."""
+    B, N, H, d = k_new.shape
+    t = k_new.dtype
+    if (t not in _IO or B != cfg.batch or H != cfg.num_kv_heads or d != cfg.head_dim or
+            not _fits(dev, (seq_lens, torch.int32, B), (new_lens, torch.int32, B), (new_seq_lens, torch.int32, B),
+                      (positions, torch.int32, 0))):
+        return None
+    r = hq = hy = None
+    if rope is not None:
+        if type(rope) is not Rope or not _fits(dev, (rope[0], torch.float32, 1)):
+            return None
+        r = _rope_form(rope)
+    if positions is not None and (r is None or positions.shape != (B, N)):
+        return None
+    if q is not None or q_out is not None:
+        if q is None or q_out is None or q_out.dtype not in _IO:
+            return None
+        shape = (B, N, cfg.num_q_heads, d)
+        hq, hy = _heads_fit(q, t, dev, shape), _heads_fit(q_out, q_out.dtype, dev, shape)
+        if hq is None or hy is None:
+            return None
+    hk, hv = _heads_fit(k_new, t, dev, k_new.shape), _heads_fit(v_new, t, dev, k_new.shape)
+    return None if hk is None or hv is None else (hk, hv, hq, hy, r)
+
+
+def _new(cfg, k_new, v_new, seq_lens, new_lens, rope, positions, q, q_out, new_seq_lens):
+    """The separate checks of an append's arguments: their C views."""
+    if k_new is None or k_new.dim() != 4:
         raise CobsError(f"k_new must have shape [{cfg.batch}, N, {cfg.num_kv_heads}, {cfg.head_dim}]")
     B, N, d = cfg.batch, k_new.shape[1], cfg.head_dim
     hk = _heads("k_new", k_new, None, (B, N, cfg.num_kv_heads, d))
     hv = _heads("v_new", v_new, k_new.dtype, (B, N, cfg.num_kv_heads, d))
-    hq = hy = r = None
+    hq = hy = None
     if (q is None) != (q_out is None):
         raise CobsError("q and q_out go together")
     if q is not None:
         hq = _heads("q", q, k_new.dtype, (B, N, cfg.num_q_heads, d))
         hy = _heads("q_out", q_out, None, (B, N, cfg.num_q_heads, d))
     if rope is not None:
-        r = _rope(rope, positions, B * N)
-        if positions is not None and tuple(positions.shape) != (B, N):
-            raise CobsError(f"positions must have shape [{B}, {N}], got {list(positions.shape)}")
+        _rope(rope, positions, (B, N))
     elif positions is not None:
         raise CobsError("positions needs rope")
-    dev = _gpu(k_new)
-    if not _fits(dev, (seq_lens, torch.int32, B), (new_lens, torch.int32, B), (new_seq_lens, torch.int32, B)) or seq_lens is None:
-        _need("seq_lens", seq_lens, torch.int32, B)
-        _opt("new_lens", new_lens, torch.int32, B)
-        _opt("new_seq_lens", new_seq_lens, torch.int32, B)
-    _same_gpu(k_new=k_new, v_new=v_new, seq_lens=seq_lens, new_lens=new_lens, new_seq_lens=new_seq_lens, q=q, q_out=q_out,
-              positions=positions, inv_freq=None if rope is None else rope.inv_freq, **tensors)
-    _call(fn, k_new, ctypes.byref(c), ctypes.byref(hk), ctypes.byref(hv), _IO[k_new.dtype], N, ctypes.byref(view),
-          seq_lens.data_ptr(), _ptr(new_lens), None if r is None else ctypes.byref(r), _ptr(positions),
-          None if hq is None else ctypes.byref(hq), None if hy is None else ctypes.byref(hy),
-          0 if q_out is None else _IO[q_out.dtype], _ptr(new_seq_lens), _stream(stream, k_new))
+    _need("seq_lens", seq_lens, torch.int32, B)
+    _opt("new_lens", new_lens, torch.int32, B)
+    _opt("new_seq_lens", new_seq_lens, torch.int32, B)
+    return hk, hv, hq, hy, None if rope is None else _rope_form(rope)
+
+
+def _append(fn, c, view, k_new, views, seq_lens, new_lens, positions, q_out, new_seq_lens, stream):
+    hk, hv, hq, hy, r = views
+    _call(fn, k_new, ctypes.byref(c), hk, hv, _IO[k_new.dtype], k_new.shape[1], view, seq_lens.data_ptr(), _ptr(new_lens), r,
+          _ptr(positions), hq, hy, 0 if q_out is None else _IO[q_out.dtype], _ptr(new_seq_lens), _stream(stream, k_new))
 
 
 def cobs_append(cfg, k_new, v_new, k, v, seq_lens, new_lens=None, rope=None, positions=None, q=None, q_out=None,
                 new_seq_lens=None, block_table=None, num_pages=0, stream=None):
     """Tokens k_new, v_new [B, N, Hkv, d] behind the cache's seq_lens [B] tokens (new_lens [B] of the N; None: all), keys rotated;
     their queries q [B, N, Hq, d], rotated, to q_out; new_seq_lens [B]: the lengths after."""
-    c = _struct(cfg)
-    _append(lib().cobs_append, cfg, c, _kv(cfg, k, v, block_table, num_pages), k_new, v_new,
-            dict(k=k, v=v, block_table=block_table), seq_lens, new_lens, rope, positions, q, q_out, new_seq_lens, stream)
+    c, _, kvt = cfg.marshalled()
+    kv = views = None
+    if k_new is not None and v_new is not None and k is not None and v is not None and seq_lens is not None and len(k_new.shape) == 4:
+        dev = _gpu(k_new)
+        views = _new_fit(cfg, dev, k_new, v_new, seq_lens, new_lens, rope, positions, q, q_out, new_seq_lens)
+        if views is not None:
+            kv = _cache_fits(cfg, kvt, dev, k, v, block_table, num_pages)
+    if kv is None:
+        views = _new(cfg, k_new, v_new, seq_lens, new_lens, rope, positions, q, q_out, new_seq_lens)
+        kv = _kv(cfg, k, v, block_table, num_pages)
+        _same_gpu(k_new=k_new, v_new=v_new, seq_lens=seq_lens, new_lens=new_lens, new_seq_lens=new_seq_lens, q=q, q_out=q_out,
+                  positions=positions, inv_freq=None if rope is None else rope.inv_freq, k=k, v=v, block_table=block_table)
+    _append(lib().cobs_append, c, ctypes.byref(kv), k_new, views, seq_lens, new_lens, positions, q_out, new_seq_lens, stream)
+
+
+def _cache8_fits(cfg, dev, cache8, block_table, num_pages):
+    """The C view of an 8-bit cache on GPU `dev`, or None if anything does not fit."""
+    if type(cache8) is not Cache8:
+        return None
+    k, v, ks, vs = cache8
+    if k is None or v is None or ks is None or vs is None:
+        return None
+    shape, stride, t = k.shape, k.stride(), k.dtype
+    if ((t is not E4M3 and t is not torch.uint8) or v.dtype is not t or len(shape) != 4 or v.shape != shape or
+            v.stride() != stride or stride[3] != 1 or k.get_device() != dev or v.get_device() != dev or
+            not _fits(dev, (ks, torch.float32, 0), (vs, torch.float32, 0))):
+        return None
+    H, L, d = cfg.num_kv_heads, cfg.block_size, cfg.head_dim
+    if block_table is None:
+        if (shape[0] < cfg.batch or shape[1] < H or shape[2] < cfg.max_seq_len or shape[3] != d or
+                not ks.shape == vs.shape == (cfg.batch, H, cfg.max_seq_len // L)):
+            return None
+        return _pack_kv8(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), stride[0], stride[1], stride[2], 0, 0)
+    if (shape != (shape[0], H, L, d) or not k.is_contiguous() or type(num_pages) is not int or not 1 <= num_pages <= shape[0] or
+            not ks.shape == vs.shape == (shape[0], H) or not _fits(dev, (block_table, torch.int32, cfg.batch * cfg.num_blocks))):
+        return None
+    return _pack_kv8(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), 0, 0, 0, block_table.data_ptr(), num_pages)
 
 
 def _cache8(cfg, cache8, block_table, num_pages):
@@ -227,9 +282,10 @@ def _cache8(cfg, cache8, block_table, num_pages):
         _need(name, t, torch.float32, math.prod(want))
         if t.dim() != len(want) or tuple(t.shape[1:]) != want[1:]:
             raise CobsError(f"{name} must have shape {list(want)}, got {list(t.shape)}")
+    at = (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
     if block_table is not None:
-        return _KV8(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), 0, 0, 0, block_table.data_ptr(), int(num_pages))
-    return _KV8(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), k.stride(0), k.stride(1), k.stride(2), None, 0)
+        return _pack_kv8(*at, 0, 0, 0, block_table.data_ptr(), int(num_pages))
+    return _pack_kv8(*at, *k.stride()[:3], 0, 0)
 
 
 def _of8(cache8, block_table):
@@ -240,35 +296,48 @@ def cobs_append8(cfg, k_new, v_new, cache8, seq_lens, new_lens=None, rope=None, 
                  new_seq_lens=None, block_table=None, num_pages=0, stream=None):
     """cobs_append into an 8-bit cache; a block whose scale grows has its earlier codes written anew."""
     c = _struct(cfg)
-    view = _cache8(cfg, cache8, block_table, num_pages)
-    _append(lib().cobs_append8, cfg, c, view, k_new, v_new, _of8(cache8, block_table), seq_lens, new_lens, rope, positions,
-            q, q_out, new_seq_lens, stream)
+    view = views = None
+    if k_new is not None and v_new is not None and seq_lens is not None and len(k_new.shape) == 4:
+        dev = _gpu(k_new)
+        views = _new_fit(cfg, dev, k_new, v_new, seq_lens, new_lens, rope, positions, q, q_out, new_seq_lens)
+        if views is not None:
+            view = _cache8_fits(cfg, dev, cache8, block_table, num_pages)
+    if view is None:
+        view = _cache8(cfg, cache8, block_table, num_pages)
+        views = _new(cfg, k_new, v_new, seq_lens, new_lens, rope, positions, q, q_out, new_seq_lens)
+        _same_gpu(k_new=k_new, v_new=v_new, seq_lens=seq_lens, new_lens=new_lens, new_seq_lens=new_seq_lens, q=q, q_out=q_out,
+                  positions=positions, inv_freq=None if rope is None else rope.inv_freq, **_of8(cache8, block_table))
+    _append(lib().cobs_append8, c, view, k_new, views, seq_lens, new_lens, positions, q_out, new_seq_lens, stream)
 
 
 def cobs_decode8(cfg, q, cache8, seq_lens, draft_lens, tree_mask, out, ws, sel=None, lse=None, block_table=None,
                  num_pages=0, stream=None):
     """Attention of the N queries q [B, N, Hq, d] of each row over an 8-bit cache; arguments as for cache.cobs_tree_decode."""
     c = _struct(cfg)
-    n = _queries(cfg, q, seq_lens, draft_lens, tree_mask, sel)
-    _need("out", out, q.dtype, q.numel())
-    _opt("lse", lse, torch.float32, cfg.batch * n * cfg.num_q_heads)
-    view = _cache8(cfg, cache8, block_table, num_pages)
-    nws = _ws(ws)
-    _same_gpu(q=q, seq_lens=seq_lens, draft_lens=draft_lens, tree_mask=tree_mask, sel=sel, out=out, lse=lse, ws=ws,
-              **_of8(cache8, block_table))
-    _call(lib().cobs_decode8, q, ctypes.byref(c), q.data_ptr(), _IO[q.dtype], n, ctypes.byref(view), seq_lens.data_ptr(),
-          _ptr(draft_lens), _ptr(tree_mask), sel is not None, _ptr(sel) or None, out.data_ptr(), _ptr(lse), ws.data_ptr(), nws,
-          _stream(stream, q))
+    view = None
+    if q is not None and out is not None and ws is not None and seq_lens is not None:
+        nq, t = q.numel(), q.dtype
+        if _queries_alone_fit(cfg, q, seq_lens, draft_lens, tree_mask, sel, (out, t, nq), (lse, torch.float32, nq // cfg.head_dim),
+                        (ws, ws.dtype, 0)):
+            view = _cache8_fits(cfg, _gpu(q), cache8, block_table, num_pages)
+    if view is None:
+        n = _queries(cfg, q, seq_lens, draft_lens, tree_mask, sel)
+        _need("out", out, q.dtype, q.numel())
+        _opt("lse", lse, torch.float32, cfg.batch * n * cfg.num_q_heads)
+        view = _cache8(cfg, cache8, block_table, num_pages)
+        _ws(ws)
+        _same_gpu(q=q, seq_lens=seq_lens, draft_lens=draft_lens, tree_mask=tree_mask, sel=sel, out=out, lse=lse, ws=ws,
+                  **_of8(cache8, block_table))
+    _call(lib().cobs_decode8, q, ctypes.byref(c), q.data_ptr(), _IO[q.dtype], q.shape[1], view, seq_lens.data_ptr(),
+          _ptr(draft_lens), _ptr(tree_mask), sel is not None, _ptr(sel) or None, out.data_ptr(), _ptr(lse), ws.data_ptr(),
+          ws.numel() * ws.element_size(), _stream(stream, q))
 
 
 def cobs_unpack8(cfg, cache8, seq_lens, k_out, v_out, first_block=0, num_blocks=None, last=None, block_table=None,
                  num_pages=0, out_block_table=None, out_num_pages=0, stream=None):
     """Blocks of an 8-bit cache as bf16 or fp32 (cfg.kv_dtype) in the same places of the cache k_out, v_out: num_blocks
     from first_block on (None: all), or the `last` blocks of each row."""
-    c = _struct(cfg)
-    view = _cache8(cfg, cache8, block_table, num_pages)
-    dst = _kv(cfg, k_out, v_out, out_block_table, out_num_pages)
-    _need("seq_lens", seq_lens, torch.int32, cfg.batch)
+    c, _, kvt = cfg.marshalled()
     if last is not None:
         if first_block != 0 or num_blocks is not None:
             raise CobsError("last stands for itself, without first_block and num_blocks")
@@ -279,6 +348,16 @@ def cobs_unpack8(cfg, cache8, seq_lens, k_out, v_out, first_block=0, num_blocks=
         raise CobsError("first_block must not be negative")
     elif num_blocks is None:
         num_blocks = cfg.num_blocks - first_block
-    _same_gpu(seq_lens=seq_lens, k_out=k_out, v_out=v_out, out_block_table=out_block_table, **_of8(cache8, block_table))
-    _call(lib().cobs_unpack8, seq_lens, ctypes.byref(c), ctypes.byref(view), seq_lens.data_ptr(), int(first_block),
-          int(num_blocks), ctypes.byref(dst), _stream(stream, seq_lens))
+    dst = view = None
+    if seq_lens is not None and k_out is not None and v_out is not None and _fits(_gpu(seq_lens), (seq_lens, torch.int32, cfg.batch)):
+        dev = _gpu(seq_lens)
+        view = _cache8_fits(cfg, dev, cache8, block_table, num_pages)
+        if view is not None:
+            dst = _cache_fits(cfg, kvt, dev, k_out, v_out, out_block_table, out_num_pages)
+    if dst is None:
+        view = _cache8(cfg, cache8, block_table, num_pages)
+        dst = _kv(cfg, k_out, v_out, out_block_table, out_num_pages)
+        _need("seq_lens", seq_lens, torch.int32, cfg.batch)
+        _same_gpu(seq_lens=seq_lens, k_out=k_out, v_out=v_out, out_block_table=out_block_table, **_of8(cache8, block_table))
+    _call(lib().cobs_unpack8, seq_lens, ctypes.byref(c), view, seq_lens.data_ptr(), int(first_block), int(num_blocks),
+          ctypes.byref(dst), _stream(stream, seq_lens))

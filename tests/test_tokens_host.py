@@ -93,13 +93,13 @@ def _cfg(**over):
 def _heads(**over):
     base = dict(p=FAKE, stride_b=1 << 16, stride_n=1 << 12, stride_h=128)
     base.update(over)
-    return tokens._Heads(*base.values())
+    return tokens._pack_heads(base["p"] or 0, *list(base.values())[1:])
 
 
 def _rope(**over):
     base = dict(inv_freq=FAKE, rotary_dim=128, interleaved=0, scale=1.0)
     base.update(over)
-    return tokens._Rope(*base.values())
+    return tokens._pack_rope(base["inv_freq"] or 0, *list(base.values())[1:])
 
 
 def _kv(**over):
@@ -112,11 +112,11 @@ def _kv8(**over):
     base = dict(k=FAKE, v=FAKE + 4096, k_scale=FAKE + 8192, v_scale=FAKE + 16384, stride_b=1 << 20, stride_h=1 << 19, stride_t=128,
                 block_table=None, num_pages=0)
     base.update(over)
-    return tokens._KV8(*base.values())
+    return tokens._pack_kv8(*(x or 0 for x in base.values()))
 
 
 def _ref(x):
-    return None if x is None else ctypes.byref(x)
+    return x if x is None or isinstance(x, bytes) else ctypes.byref(x)
 
 
 def _rotate(**over):
