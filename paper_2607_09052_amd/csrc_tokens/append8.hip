@@ -14,6 +14,11 @@
 
 namespace cobs {
 
+// Query heads from which on a launch of their own rotates them: the workgroups that encode leave a CU three at a time, too few
+// for a copy (q and all: 446 us for four prompts of 16k tokens, 8 KV and 32 query heads).
+constexpr int64_t kApart = 1 << 15;
+constexpr int kMostItems = 64;         // (head, keys or values) pairs that a workgroup takes in turn
+
 // The smallest power of two s, 2^-100 at least, with top / s <= 448 = 1.75 * 2^8: a mantissa above 1.75 carries
 // into the exponent.
 __device__ __forceinline__ float scale_for(float top) {
@@ -36,12 +41,13 @@ __device__ __forceinline__ void values4(uint32_t w, float* x) {
   x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
 }
 
-template <int D, int LANES, int PASSES>
+template <int D, int LANES, int PASSES, bool F32>
 __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) {
   constexpr int TPR = D / 16, RP = LANES / TPR, UNITS = kHeadThreads / LANES;
-  static_assert(LANES == kHeadThreads || LANES <= 64, "a workgroup, or lanes of a wave");
+  constexpr bool GROUP = LANES == kHeadThreads;
+  static_assert(GROUP || LANES <= 64, "a workgroup, or lanes of a wave");
   __shared__ HeadsShared hs;
-  __shared__ float s_top[2][kHeadThreads / 64], s_held[2];
+  __shared__ float s_top[2][kHeadThreads / 64], s_held[kMostItems];
   if (blockIdx.x == 0) write_lens(p.t);
   if ((int)blockIdx.x < p.q_groups) {
     heads_body<D, false>(p.t, nullptr, false, blockIdx.x, p.per_wg, p.slots, p.slot_groups, hs);
@@ -49,7 +55,7 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
   }
   const int tid = threadIdx.x, H2 = 2 * p.t.hkv;
   // items: (head, K or V), keys first, `items` of them a workgroup (LANES < 256: one a unit)
-  const int per = LANES == kHeadThreads ? p.items : 1, groups = (H2 + per - 1) / per;
+  const int per = GROUP ? p.items : 1, groups = (H2 + per - 1) / per;
   const int64_t unit = (int64_t)((int)blockIdx.x - p.q_groups) * UNITS + tid / LANES;
   const int64_t units = (int64_t)p.t.B * p.blocks * groups;
   if (unit >= units) return;                           // (LANES == 256: the whole workgroup)
@@ -70,6 +76,25 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
 
   const int lane = tid % LANES, row = lane / TPR, piece = lane % TPR;
   const Piece e = piece_of(p.t.rope, piece), straight = {16 * piece, 16 * piece + 8, false};
+  // the new tokens' rows of an item as they come; the next item's are loaded while one is encoded
+  Raw8 raw[PASSES][2];
+  auto load = [&](int it) {
+    const bool key = it < p.t.hkv;
+    const HeadsView& from = key ? p.t.k : p.t.v;
+    const Piece c = key ? e : straight;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+      const int t = t0 + row + k * RP;
+      if (t < t1) {
+        const int64_t at = b * from.sb + (t - r.T) * from.sn + (key ? it : it - p.t.hkv) * from.sh;
+        raw[k][0] = load_raw8(from.p, at + c.e0, F32);
+        raw[k][1] = load_raw8(from.p, at + c.e1, F32);
+      }
+    }
+  };
+  auto scale_of = [&](int it) { return (it < p.t.hkv ? p.k_scale + it * sstep : p.v_scale + (it - p.t.hkv) * sstep) + srow; };
+  load(it0);
+  if (GROUP && earlier > 0 && tid < it1 - it0) s_held[tid] = *scale_of(it0 + tid);
   float2 cs[PASSES][8];
   if (e.turned && it0 < p.t.hkv) {
 #pragma unroll
@@ -85,41 +110,37 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
   for (int it = it0; it < it1; ++it) {
     const bool key = it < p.t.hkv;
     const int h = key ? it : it - p.t.hkv;
-    const HeadsView& from = key ? p.t.k : p.t.v;
     const Piece c = key ? e : straight;
     float x[PASSES][16];
     float top = 0.0f;
 #pragma unroll
     for (int k = 0; k < PASSES; ++k) {
-      const int t = t0 + row + k * RP;
-      if (t < t1) {
-        const int64_t at = b * from.sb + (t - r.T) * from.sn + h * from.sh;
-        const Raw8 r0 = load_raw8(from.p, at + c.e0, from.f32), r1 = load_raw8(from.p, at + c.e1, from.f32);
-        widen8(r0, from.f32, x[k]);
-        widen8(r1, from.f32, x[k] + 8);
+      if (t0 + row + k * RP < t1) {
+        widen8(raw[k][0], F32, x[k]);
+        widen8(raw[k][1], F32, x[k] + 8);
         if (c.turned) turn16(x[k], cs[k], p.t.rope.interleaved);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float a = fabsf(x[k][i]);
+        for (int y = 0; y < 16; ++y) {
+          const float a = fabsf(x[k][y]);
           top = a < INFINITY ? fmaxf(top, a) : top;
         }
       }
     }
-    float* const scale = (key ? p.k_scale : p.v_scale) + srow + h * sstep;
-    float held;
-    if constexpr (LANES == kHeadThreads) {
-      top = wave_max(top);
+    if (it + 1 < it1) load(it + 1);
+    float* const scale = scale_of(it);
+    float held = 0.0f;
+    if constexpr (GROUP) {
+      top = wave_max_rows(top);
       const int buf = (it - it0) & 1;                   // (a barrier lies between a buffer's use and its next writing)
       if ((tid & 63) == 0) s_top[buf][tid >> 6] = top;
-      if (tid == 0) s_held[buf] = *scale;
       __syncthreads();
 #pragma unroll
       for (int w = 0; w < kHeadThreads / 64; ++w) top = fmaxf(top, s_top[buf][w]);
-      held = s_held[buf];
+      if (earlier > 0) held = s_held[it - it0];
     } else {
 #pragma unroll
       for (int o = LANES / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-      held = *scale;
+      if (earlier > 0) held = *scale;
     }
     const float need = scale_for(top);
     const float now = earlier > 0 && held >= need ? held : need, inv = 1.0f / now;
@@ -147,13 +168,20 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
   }
 }
 
-template <int D>
+template <int D, bool F32>
 static hipError_t launch_d(Append8Params p, hipStream_t st) {
   constexpr int TPR = D / 16;
   const int L = 1 << p.kv.lsh;
   p.q_groups = p.per_wg = p.slots = p.slot_groups = 0;
-  if (p.t.hq > 0) {
-    const int64_t tokens = (int64_t)p.t.B * p.t.N;
+  const int64_t tokens = (int64_t)p.t.B * p.t.N;
+  if (p.t.hq > 0 && tokens * p.t.hq >= kApart) {
+    AppendParams q = {};
+    q.t = p.t;
+    q.t.hkv = 0;
+    q.t.new_seq_lens = nullptr;
+    const hipError_t e = launch_append(q, st);
+    if (e != hipSuccess) return e;
+  } else if (p.t.hq > 0) {
     plan_heads(tokens, p.t.hq, D, &p.per_wg, &p.slots, &p.slot_groups);
     const int64_t g = (tokens + p.per_wg - 1) / p.per_wg * p.slot_groups;
     if (g > 0x3fffffff) return hipErrorInvalidValue;
@@ -161,14 +189,14 @@ static hipError_t launch_d(Append8Params p, hipStream_t st) {
   }
   const int most = p.t.N < L ? p.t.N : L;               // new tokens of a block
   p.blocks = (p.t.N + L - 2) / L + 1;
-  // (with 64 lanes a unit: one unit a wave)
   const int lanes = most == 1 ? TPR : (most <= 64 / TPR ? 64 : kHeadThreads);
   p.items = 1;
   if (lanes == kHeadThreads) {
-    // heads of a workgroup: as many as leave four workgroups a CU
+    // heads of a workgroup: as many as leave some eight workgroups a CU
     const int64_t all = (int64_t)p.t.B * p.blocks * 2 * p.t.hkv;
-    p.items = (int)(all / 1024);
-    p.items = p.items < 1 ? 1 : (p.items > 2 * p.t.hkv ? 2 * p.t.hkv : p.items);
+    p.items = (int)(all / 2048);
+    const int top = 2 * p.t.hkv < kMostItems ? 2 * p.t.hkv : kMostItems;
+    p.items = p.items < 1 ? 1 : (p.items > top ? top : p.items);
   }
   const int64_t units = (int64_t)p.t.B * p.blocks * ((2 * p.t.hkv + p.items - 1) / p.items);
   const int per_group = kHeadThreads / lanes;
@@ -176,16 +204,17 @@ static hipError_t launch_d(Append8Params p, hipStream_t st) {
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   const dim3 g((uint32_t)grid), t(kHeadThreads);
   const int rows = kHeadThreads / TPR;                  // tokens of a workgroup's pass
-  if (lanes == TPR) hipLaunchKernelGGL((append8_kernel<D, TPR, 1>), g, t, 0, st, p);
-  else if (lanes == 64) hipLaunchKernelGGL((append8_kernel<D, 64, 1>), g, t, 0, st, p);
-  else if (most <= rows) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 1>), g, t, 0, st, p);
-  else if (most <= 2 * rows) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 2>), g, t, 0, st, p);
-  else if constexpr (D == 128) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 4>), g, t, 0, st, p);
+  if (lanes == TPR) hipLaunchKernelGGL((append8_kernel<D, TPR, 1, F32>), g, t, 0, st, p);
+  else if (lanes == 64) hipLaunchKernelGGL((append8_kernel<D, 64, 1, F32>), g, t, 0, st, p);
+  else if (most <= rows) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 1, F32>), g, t, 0, st, p);
+  else if (most <= 2 * rows) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 2, F32>), g, t, 0, st, p);
+  else if constexpr (D == 128) hipLaunchKernelGGL((append8_kernel<D, kHeadThreads, 4, F32>), g, t, 0, st, p);
   return hipGetLastError();
 }
 
 hipError_t launch_append8(const Append8Params& p, hipStream_t st) {
-  return p.t.d == 64 ? launch_d<64>(p, st) : launch_d<128>(p, st);
+  if (p.t.k.f32) return p.t.d == 64 ? launch_d<64, true>(p, st) : launch_d<128, true>(p, st);
+  return p.t.d == 64 ? launch_d<64, false>(p, st) : launch_d<128, false>(p, st);
 }
 
 }  // namespace cobs

@@ -2,7 +2,7 @@
 #include "decode8_impl.h"
 
 namespace cobs {
-hipError_t launch_decode8_bf16_d128(const Decode8Params& p, int tiles, int grid, hipStream_t st) {
-  return launch_decode8_kernels<128, 1>(p, tiles, grid, st);
+hipError_t launch_decode8_bf16_d128(const Decode8Params& p, int rows, int grid, hipStream_t st) {
+  return launch_decode8_kernels<128, 1>(p, rows, grid, st);
 }
 }  // namespace cobs
