@@ -377,7 +377,7 @@ template <int D, int PARTS, int R>
 __global__ __launch_bounds__(kTreeThreads, (kWorkgroups8<D, PARTS, R>)) void decode8_kernel(Decode8Params p) {
   using T = Tile8<D, R>;
   constexpr int WT = 4, KS = T::KS, NO = T::NO, PP = PARTS == 3 ? 3 : 2;
-  constexpr bool SHARED = D == 128 && R == 32;             // the queries' operands in LDS (the pool's place): in registers they spill
+  constexpr bool SHARED = D == 128 && R == 32 && PARTS == 3;      // the queries' operands in LDS (the pool's place): in registers they spill
   __shared__ Frame8 table[kTable8];
   __shared__ __align__(16) float pool[WT * R * D];
   __shared__ float s_m[WT][R], s_l[WT][R];
@@ -431,36 +431,43 @@ __global__ __launch_bounds__(kTreeThreads, (kWorkgroups8<D, PARTS, R>)) void dec
 
   bool nan = false;                                     // whether a drafted token's value was
   uint32_t ky[D / 8], vy[D / 8];
+  auto scores = [&](float (&s)[T::NI]) {
+#pragma unroll
+    for (int tt = 0; tt < T::TT; ++tt) {
+      typename T::Acc z;
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) z[i] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const sbf16x8_t kk = key_operand(ky, tt * KS + ks);
+#pragma unroll
+        for (int k = PARTS - 1; k >= 0; --k) z = product<R>(kk, SHARED ? q_lds[(ks * PARTS + k) * 64] : qb[SHARED ? 0 : ks][k], z);
+      }
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) s[tt * T::NA + i] = z[i];
+    }
+  };
 
   for (int t0 = f_lo; t0 < f_hi; t0 += kTable8) {
     const int cnt = min(kTable8, f_hi - t0);
     __syncthreads();                                    // the table is free; the queries are there
     if (tid < cnt) table[tid] = describe_frame(p, x, b, h, t0 + tid, c2);
     __syncthreads();
-    ScalarFrame f = table_frame(table, wave, cnt);
+    // A frame's scores are computed while the softmax of the one before runs.  Loads begin where their registers fall free, a frame's
+    // keys before the values of the frame before it.  There is always a next frame (past the end at place 0, the cache's first
+    // rows): were loads left out on some path, or in another order before the loop, the waits in it would be for all loads
+    // under way instead of the older ones.
+    ScalarFrame f = table_frame(table, wave, cnt), next = table_frame(table, wave + WT, cnt);
+    float s[T::NI];
     load_keys<D, R>(kp + f.base, rs, ky);
+    scores(s);
+    load_keys<D, R>(kp + next.base, rs, ky);
+    __builtin_amdgcn_sched_barrier(0);
     load_values<D, R>(vp + f.base, rs, vy);
-    // The next frame's loads begin where this one's registers fall free.  There is always a next one (past the end at place 0, the cache's
-    // first rows): were loads left out on some path, the waits behind would be for all loads under way instead of the older ones.
     int it = wave;
     while (it < cnt) {
       float top;
       while (true) {
-        float s[T::NI];
-#pragma unroll
-        for (int tt = 0; tt < T::TT; ++tt) {
-          typename T::Acc z;
-#pragma unroll
-          for (int i = 0; i < T::NA; ++i) z[i] = 0.0f;
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            const sbf16x8_t kk = key_operand(ky, tt * KS + ks);
-#pragma unroll
-            for (int k = PARTS - 1; k >= 0; --k) z = product<R>(kk, SHARED ? q_lds[(ks * PARTS + k) * 64] : qb[SHARED ? 0 : ks][k], z);
-          }
-#pragma unroll
-          for (int i = 0; i < T::NA; ++i) s[tt * T::NA + i] = z[i];
-        }
         if (!f.whole(x.C)) {
           asm volatile("");                             // (nothing of this is for the other frames)
           const int to_c = x.C - f.a;
@@ -475,11 +482,14 @@ __global__ __launch_bounds__(kTreeThreads, (kWorkgroups8<D, PARTS, R>)) void dec
         for (int j = 1; j < T::NI; ++j) top = fmaxf(top, s[j]);
         top *= f.ks;
         // The maximum is followed with a slack of 2^8 in the probabilities, so that few frames raise it and scale the outputs
-        // anew; such a frame is begun again, so that this loop changes the outputs by products alone (a path that scales
-        // them in it costs copies of them all in each frame).
+        // anew, outside of this loop, which changes the outputs by products alone (a path that scales them in it costs
+        // copies of them all in each frame).
         if (__ballot(top > m + 8.0f)) break;
-        const ScalarFrame next = table_frame(table, it + WT, cnt);
-        load_keys<D, R>(kp + next.base, rs, ky);
+        const ScalarFrame after = table_frame(table, it + 2 * WT, cnt);
+        float z[T::NI];
+        scores(z);
+        load_keys<D, R>(kp + after.base, rs, ky);
+        __builtin_amdgcn_sched_barrier(0x40f);          // (arithmetic may cross: the compiler would move the loads to the loop's end)
         sbf16x8_t pb[T::PS][PP];
         softmax_tile<R, PP>(s, f.ks, f.vs, m, l, pb);
         value_operands<D, R>(vy, [&](int c, int ks, sbf16x8_t v) {
@@ -487,7 +497,10 @@ __global__ __launch_bounds__(kTreeThreads, (kWorkgroups8<D, PARTS, R>)) void dec
           for (int k = PP - 1; k >= 0; --k) o[c] = product<R>(v, pb[ks][k], o[c]);
         });
         load_values<D, R>(vp + next.base, rs, vy);
+#pragma unroll
+        for (int j = 0; j < T::NI; ++j) s[j] = z[j];
         f = next;
+        next = after;
         it += WT;
         if (it >= cnt) break;
       }
