@@ -44,9 +44,13 @@ def lib():
     return _lib
 
 
+# (a tensor on a GPU has initialised torch's side, which torch.cuda.current_device looks after once more each time)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _call(fn, t, *args):
     """The C call on the GPU of tensor `t`, which becomes the current one for it where it is not."""
-    if t.get_device() == torch.cuda.current_device():
+    if t.get_device() == _current_device():
         return _check(fn(*args))
     with torch.cuda.device(t.device):
         return _check(fn(*args))

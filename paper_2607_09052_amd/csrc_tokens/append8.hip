@@ -26,14 +26,11 @@ __device__ __forceinline__ float scale_for(float top) {
   return __uint_as_float((uint32_t)max(e, 27) << 23);
 }
 
-// Four codes of x * inv (at most 448 in magnitude), the lowest byte first.  The hardware rounds to nearest even and
-// keeps denormals; what is not finite becomes NaN.
+// Four codes of x * inv (at most 448 in magnitude, or NaN), the lowest byte first.  The hardware rounds to nearest even and
+// keeps denormals.
 __device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
-  float y[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = fabsf(x[i]) < INFINITY ? x[i] * inv : __uint_as_float(0x7fc00000u);
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, r, true);
 }
 
 __device__ __forceinline__ void values4(uint32_t w, float* x) {
@@ -120,11 +117,19 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
         widen8(raw[k][1], F32, x[k] + 8);
         if (c.turned) turn16(x[k], cs[k], p.t.rope.interleaved);
 #pragma unroll
-        for (int y = 0; y < 16; ++y) {
-          const float a = fabsf(x[k][y]);
-          top = a < INFINITY ? fmaxf(top, a) : top;
-        }
+        for (int y = 0; y < 16; ++y) top = fmaxf(top, fabsf(x[k][y]));      // (NaN leaves it)
       }
+    }
+    if (__ballot(top == INFINITY)) {                    // rare: infinities become NaN and do not count
+      top = 0.0f;
+#pragma unroll
+      for (int k = 0; k < PASSES; ++k)
+#pragma unroll
+        for (int y = 0; y < 16; ++y) {
+          if (t0 + row + k * RP >= t1) continue;
+          x[k][y] = fabsf(x[k][y]) < INFINITY ? x[k][y] : __uint_as_float(0x7fc00000u);
+          top = fmaxf(top, fabsf(x[k][y]));
+        }
     }
     if (it + 1 < it1) load(it + 1);
     float* const scale = scale_of(it);
@@ -192,11 +197,13 @@ static hipError_t launch_d(Append8Params p, hipStream_t st) {
   const int lanes = most == 1 ? TPR : (most <= 64 / TPR ? 64 : kHeadThreads);
   p.items = 1;
   if (lanes == kHeadThreads) {
-    // heads of a workgroup: as many as leave some eight workgroups a CU
+    // Heads of a workgroup, which share their tokens' cosines and sines: as many as leave two workgroups a CU, keys and values apart
+    // (16000 tokens in blocks of 128, 8 heads: 26 us; by 2048 workgroups of one head each 38; 49000 tokens by workgroups of
+    // 8 heads' keys or values 102, of both 130).
     const int64_t all = (int64_t)p.t.B * p.blocks * 2 * p.t.hkv;
-    p.items = (int)(all / 2048);
-    const int top = 2 * p.t.hkv < kMostItems ? 2 * p.t.hkv : kMostItems;
-    p.items = p.items < 1 ? 1 : (p.items > top ? top : p.items);
+    const int top = p.t.hkv < kMostItems ? p.t.hkv : kMostItems;
+    p.items = (int)(all / 512 < top ? all / 512 : top);
+    if (p.items < 1) p.items = 1;
   }
   const int64_t units = (int64_t)p.t.B * p.blocks * ((2 * p.t.hkv + p.items - 1) / p.items);
   const int per_group = kHeadThreads / lanes;
