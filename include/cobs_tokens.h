@@ -113,7 +113,9 @@ cobs_status_t cobs_append8(const cobs_config_t* cfg, const cobs_heads_t* k_new, 
                            const cobs_heads_t* q, const cobs_heads_t* q_out, cobs_dtype_t q_dtype,
                            int32_t* new_seq_lens, void* stream);
 
-/* Workspace bytes of cobs_decode8 (0 if invalid).  It needs no clearing. */
+/* Workspace bytes of cobs_decode8 (0 if invalid).  It has to be zero-filled before its first use;
+ * every call leaves its arrival counters (the first 16 KB) zero again, so that later calls on the
+ * same stream, of other shapes too, may use it.  Calls that share it must not overlap in time. */
 size_t cobs_decode8_workspace_bytes(const cobs_config_t* cfg, int32_t num_queries);
 
 /* Attention of num_queries query tokens a row (1 <= num_queries <= 64) over an 8-bit cache.

@@ -1,5 +1,5 @@
-// cobs_decode8: the plan of a call and its launches.  The attention itself is in decode8_kernel.h, the
-// kernels that join the parts of a split context are cobs_tree_decode's.
+// cobs_decode8: the plan of a call and its launches.  The attention itself is in decode8_kernel.h.  The parts of a
+// split context are joined there by the last workgroup to leave one (few rows), or by cobs_tree_decode's kernels.
 #include "tokens_kernels.h"
 
 namespace cobs {
@@ -22,6 +22,16 @@ static void decode8_plan(const AttendParams& a, int* rows, int* mtiles, int* nsp
   *nsplit = parts_of(passes, (int64_t)a.B * a.hkv * *mtiles, 2.0, 1 << 30, 128, 0, slots);
 }
 
+// Arrival counters at the workspace's start: as many for every shape, so that calls of different shapes may use it in turn.
+constexpr int kCounters = 4096;
+constexpr size_t kCounterBytes = kCounters * sizeof(unsigned);
+
+// Whether the last workgroup of a (row, KV head) joins its parts: few rows, as one workgroup reads them all (32 KB in about a us,
+// where a launch of its own takes 3 to 4).
+static bool joined_by_last(const TreeParams& t) {
+  return t.nsplit > 1 && t.mtiles == 1 && t.units <= kCounters && t.nsplit * t.a.N * t.a.G <= 64;
+}
+
 static size_t ml_bytes(size_t rows) { return (rows * 2 * sizeof(float) + 255) / 256 * 256; }
 
 // Enough for both attended sets and types of q.
@@ -36,7 +46,7 @@ size_t decode8_workspace(const AttendParams& a) {
     nsplit = n > nsplit ? n : nsplit;
   }
   const size_t rows = (size_t)a.B * a.hkv * nsplit * a.N * a.G;
-  return ml_bytes(rows) + (rows * a.d * sizeof(float) + 255) / 256 * 256;
+  return kCounterBytes + ml_bytes(rows) + (rows * a.d * sizeof(float) + 255) / 256 * 256;
 }
 
 hipError_t launch_decode8(const Decode8Params& q, hipStream_t st) {
@@ -47,6 +57,8 @@ hipError_t launch_decode8(const Decode8Params& q, hipStream_t st) {
   t.units = t.a.B * t.a.hkv;
   t.even = parts_by_length(t.a, t.nsplit);
   t.step = kFramesOfPass;
+  p.counters = joined_by_last(t) ? reinterpret_cast<unsigned*>(t.part_ml) : nullptr;
+  t.part_ml += kCounterBytes / sizeof(float);
   t.part_o = t.part_ml + ml_bytes((size_t)t.units * t.nsplit * t.a.N * t.a.G) / sizeof(float);
   // eight XCDs: a multiple of 8 workgroup slots (see decode8_kernel)
   const int64_t groups = ((int64_t)t.units * t.nsplit + 7) / 8 * 8, grid = groups * t.mtiles;
@@ -55,7 +67,7 @@ hipError_t launch_decode8(const Decode8Params& q, hipStream_t st) {
   hipError_t e;
   if (t.a.io_bf16) e = t.a.d == 64 ? launch_decode8_bf16_d64(p, rows, g, st) : launch_decode8_bf16_d128(p, rows, g, st);
   else e = t.a.d == 64 ? launch_decode8_f32_d64(p, rows, g, st) : launch_decode8_f32_d128(p, rows, g, st);
-  if (e != hipSuccess || t.nsplit == 1) return e;
+  if (e != hipSuccess || t.nsplit == 1 || p.counters) return e;
   return launch_tree_merge(t, st);
 }
 

@@ -351,20 +351,66 @@ __device__ __forceinline__ void softmax_tile(float (&x)[R / 2], float ks, float 
   }
 }
 
-// A row's outputs, or its part of them, at element d (a multiple of 4): sums, maximum mm (-inf: no score above that) and total.
+// A row's outputs at element d (a multiple of 4): sums, maximum mm (-inf: no score above that) and total.
 template <int D>
-__device__ __forceinline__ void leave_row(const TreeParams& p, const TreePart& part, int row, int d, float4 sum, float mm, float total) {
+__device__ __forceinline__ void finish_row(const TreeParams& p, const TreePart& part, int row, int d, float4 sum, float mm, float total) {
   const AttendParams& a = p.a;
-  if (p.nsplit == 1) {
-    const int i = row / a.G;
-    const int64_t at = ((int64_t)part.b * a.N + i) * a.hq + part.h * a.G + (row - i * a.G);
-    store_row4(p.out, at * D + d, sum, total, a.io_bf16);
-    if (d == 0 && p.lse)
-      p.lse[at] = total != 0.0f ? (mm == -INFINITY ? 0.0f : mm) * 0.6931471805599453f + logf(total) : -INFINITY;
+  const int i = row / a.G;
+  const int64_t at = ((int64_t)part.b * a.N + i) * a.hq + part.h * a.G + (row - i * a.G);
+  store_row4(p.out, at * D + d, sum, total, a.io_bf16);
+  if (d == 0 && p.lse)
+    p.lse[at] = total != 0.0f ? (mm == -INFINITY ? 0.0f : mm) * 0.6931471805599453f + logf(total) : -INFINITY;
+}
+
+// Its part of them, written through to where any XCD reads it if the last workgroup joins the parts.
+template <int D>
+__device__ __forceinline__ void leave_part(const TreeParams& p, const TreePart& part, bool joined, int row, int d, float4 sum, float mm,
+                                           float total) {
+  const int64_t at = part_row(p, part, row);
+  float* const o = p.part_o + at * D + d;
+  float* const ml = p.part_ml + 2 * at;
+  if (joined) {
+    st_agent(o, sum.x); st_agent(o + 1, sum.y); st_agent(o + 2, sum.z); st_agent(o + 3, sum.w);
+    if (d == 0) { st_agent(ml, mm); st_agent(ml + 1, total); }
   } else {
-    const int64_t at = part_row(p, part, row);
-    *reinterpret_cast<float4*>(p.part_o + at * D + d) = sum;
-    if (d == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(mm, total);
+    *reinterpret_cast<float4*>(o) = sum;
+    if (d == 0) *reinterpret_cast<float2*>(ml) = make_float2(mm, total);
+  }
+}
+
+// The `rows` rows of a (row, KV head) out of its parts, by the workgroup that is the last to leave one: in the parts' order.
+template <int D>
+__device__ __forceinline__ void join_parts(const TreeParams& p, const TreePart& part, int rows) {
+  constexpr int U = 4;                                   // parts whose loads are under way together
+  const int M = p.a.N * p.a.G;
+  const int64_t first = part.first * M;
+  const __amdgpu_buffer_rsrc_t ml = coherent_view(p.part_ml + 2 * first, (uint32_t)(part.n * M * 8));
+  const __amdgpu_buffer_rsrc_t o = coherent_view(p.part_o + first * D, (uint32_t)(part.n * M * D * 4));
+  for (int idx = threadIdx.x; idx < rows * (D / 4); idx += kTreeThreads) {
+    const int row = idx / (D / 4), d4 = idx % (D / 4);
+    float top = -INFINITY, total = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k0 = 0; k0 < part.n; k0 += U) {
+      float2 w[U];
+      float4 y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t at = (uint32_t)(min(k0 + u, part.n - 1) * M + row);
+        w[u] = ld_coherent2(ml, at * 8);
+        y[u] = ld_coherent4(o, at * (D * 4) + d4 * 16);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (k0 + u >= part.n) continue;
+        const float mn = fmaxf(top, w[u].x), ref = mn == -INFINITY ? 0.0f : mn;
+        const float f = __builtin_amdgcn_exp2f(top - ref), g = __builtin_amdgcn_exp2f(w[u].x - ref);
+        top = mn;
+        total = total * f + w[u].y * g;
+        sum.x = sum.x * f + y[u].x * g; sum.y = sum.y * f + y[u].y * g;
+        sum.z = sum.z * f + y[u].z * g; sum.w = sum.w * f + y[u].w * g;
+      }
+    }
+    finish_row<D>(p, part, row, 4 * d4, sum, top, total);
   }
 }
 
@@ -412,7 +458,7 @@ __global__ __launch_bounds__(kTreeThreads, (kWorkgroups8<D, PARTS, R>)) void dec
   }
 
   const Attended x = attended<kTreeThreads>(a, b, h, red);
-  if (tp.nsplit == 1) clear_padding<D>(tp, b, h, mt * R, R, x.nq);
+  if (tp.nsplit == 1 || (p.counters && part.split == 0)) clear_padding<D>(tp, b, h, mt * R, R, x.nq);
   if (mt * R >= x.nq * a.G) return;                       // the tile's rows are all padding
 
   typename T::Acc o[NO];
@@ -574,8 +620,10 @@ __global__ __launch_bounds__(kTreeThreads, (kWorkgroups8<D, PARTS, R>)) void dec
       const float4 y = *reinterpret_cast<const float4*>(pool + (t * R + r) * D + 4 * (d4 ^ (r & 15)));
       sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
     }
-    leave_row<D>(tp, part, row, 4 * d4, sum, mm, ll);
+    if (tp.nsplit == 1) finish_row<D>(tp, part, row, 4 * d4, sum, mm, ll);
+    else leave_part<D>(tp, part, p.counters != nullptr, row, 4 * d4, sum, mm, ll);
   }
+  if (p.counters && arrive_last(p.counters + b * a.hkv + h, part.n, red)) join_parts<D>(tp, part, x.nq * a.G);
 }
 
 }  // namespace cobs

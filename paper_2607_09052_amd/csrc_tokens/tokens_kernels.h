@@ -60,6 +60,7 @@ struct Decode8Params {
   TreeParams t;                 // (kv: places of codes, one byte an element)
   const float* k_scale;
   const float* v_scale;
+  unsigned* counters;           // of each (row, KV head), if the last workgroup joins its parts; else null
 };
 
 hipError_t launch_append(const AppendParams& p, hipStream_t st);

@@ -96,7 +96,8 @@ def decode8_workspace_bytes(cfg, num_queries):
 
 
 def new_decode8_workspace(cfg, num_queries, device):
-    return torch.empty(max(decode8_workspace_bytes(cfg, num_queries), 256), dtype=torch.uint8, device=device)
+    """Zero-filled workspace of cobs_decode8 (the library requires zeros before first use)."""
+    return torch.zeros(max(decode8_workspace_bytes(cfg, num_queries), 256), dtype=torch.uint8, device=device)
 
 
 # As in ``cobs``, a call looks its arguments over in one pass; only when something does
