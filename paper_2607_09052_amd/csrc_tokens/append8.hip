@@ -10,6 +10,10 @@
 //   D / 16 lanes  (one new token a row: a decode step, 8 or 16 units a wave).
 // Scales are powers of two, so a grown scale changes the exponents of the block's earlier codes and nothing else
 // (but for the smallest ones, which are rounded again).
+//
+// Measured (d 128, 8 KV and 32 query heads, bf16): four prompts of 8k to 16k tokens in 284 us with their queries, 1.34 GB, 4.7 TB/s (HBM, the
+// rate of a large copy being 5.0); without queries 102 us, 3.6 TB/s read (a token's heads are apart by the queries') and written, waiting
+// for a block's maximum between.  One token of 64 rows: 5.4 us, a chain of loads (length, page, row, scale).
 #include "append_body.h"
 
 namespace cobs {

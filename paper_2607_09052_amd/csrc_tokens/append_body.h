@@ -6,6 +6,9 @@
 // tokens' cosines and sines to LDS, a pair each, as the fp64 reduction costs as much as the copy of 8
 // elements and all heads of a token share it.  Then a thread takes 16 elements of a head, both
 // sides of 8 pairs, in two 16-byte pieces (bf16).
+//
+// Measured (d 128, bf16): 8190 tokens of 32 heads rotated in 29.8 us, 4.5 TB/s; 32749 tokens of 32 query and 8 KV heads
+// appended in 172 us, 4.7 TB/s (a large copy: 5.0); one token of 64 rows 4.6 us, the chain of loads.
 #pragma once
 
 #include "tokens_device.h"

@@ -12,9 +12,15 @@
 // of this one fall free.  A block's scale of the keys multiplies the scores, that of the values the probabilities, both in fp32.
 //
 // A workgroup's four waves take the same R rows and different frames; the frames of a row's context are split over
-// workgroups as in cobs_tree_decode, whose kernels join the parts.  More rows take more workgroups, next to each other on one
-// XCD, whose L2 gives the frames again.  (Waves that share frames through LDS, converted once, took 115 us where these
-// take 89 for 64 rows over 8 x 16k tokens: a barrier a pass costs more than the conversions.)
+// workgroups as in cobs_tree_decode.  Few rows' parts are joined by the last workgroup to leave one, others by that operator's
+// kernels.  More than R rows take more workgroups, next to each other on one XCD, whose L2 gives the frames again.
+//
+// What bounds it, d 128, bf16 queries: one token of 16 rows of 32k tokens (4 heads a KV head): 1.07 GB in 178 us, 6.0 TB/s, HBM.
+// From 32 rows on the waves' instructions: a frame of 32 rows is some 270 vector instructions (80 of them conversions)
+// and 24 products of 32 cycles, and two waves a SIMD overlap little of the one with the other (16 drafted tokens of 8 heads
+// over 4 contexts of 16k to 32k: 43 GFLOP, 64 with the probabilities' second part, in 98 us; vector pipes busy 55 % of the time, matrix
+// pipes 40 %).  Tried for that: frames shared through LDS and converted once (64 rows over 8 x 16k tokens: 115 us for 89), tiles of 16
+// rows two a wave (89 for 88), both frames' codes in registers (spills), a wave's priority raised in its products (85 for 82).
 //
 // The codes of tokens that take no part are cleared; a NaN in a drafted token's value, which not all queries see,
 // is cleared and then reaches the rows that see it by a product of flags (spread_nan).
@@ -381,7 +387,7 @@ __device__ __forceinline__ void leave_part(const TreeParams& p, const TreePart& 
 // The `rows` rows of a (row, KV head) out of its parts, by the workgroup that is the last to leave one: in the parts' order.
 template <int D>
 __device__ __forceinline__ void join_parts(const TreeParams& p, const TreePart& part, int rows) {
-  constexpr int U = 4;                                   // parts whose loads are under way together
+  constexpr int U = 8;                                   // parts whose loads are under way together
   const int M = p.a.N * p.a.G;
   const int64_t first = part.first * M;
   const __amdgpu_buffer_rsrc_t ml = coherent_view(p.part_ml + 2 * first, (uint32_t)(part.n * M * 8));

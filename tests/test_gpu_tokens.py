@@ -138,6 +138,19 @@ def test_append_without_queries_lengths_or_a_count(eight):
 
 
 @pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("N", [1, 30])
+def test_queries_rotated_in_place_beside_an_append(eight, N):
+    p = Appending(DEV, B=2, N=N, T=(3, 60), eight=eight).fresh().call()
+    keys, values = p.kn.clone(), p.vn.clone()
+    q = Appending(DEV, B=2, N=N, T=(3, 60), eight=eight).fresh()
+    q.q_out = q.qd
+    q.call()
+    sync()
+    assert torch.equal(q.qd, p.q_out) and torch.equal(q.kn, keys) and torch.equal(q.vn, values)
+    (q.check_cache8 if eight else q.check_cache)()
+
+
+@pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("N", [1, 40])
 def test_append_drops_tokens_on_pages_out_of_range(eight, N):
     p = Appending(DEV, B=3, N=N, T=(70, 5, 64), layout="pages", eight=eight, spread=False)
@@ -246,6 +259,29 @@ def test_decode8_matches_fp64(shape, io, layout):
     out, lse = run_decode8(p)
     sync()
     say(f"worst error / tolerance {p.check(out, lse):.3f}")
+
+
+def test_one_workspace_for_calls_of_different_shapes():
+    """Parts joined by the last workgroup and by a launch of their own, larger and smaller calls in turn on one workspace, whose
+    counters are zero again after each."""
+    ps = [Problem8(DEV, io="bf16", seed=i, **shape).upload() for i, shape in enumerate([
+        dict(B=1, Hkv=2, G=4, T=1000, N=1, draft=False), dict(B=2, Hkv=2, G=8, T=(700, 64), N=20), dict(B=3, Hkv=4, G=1, d=64, T=(900, 5, 400), N=2),
+        dict(B=2, Hkv=2, G=4, T=(500, 300), N=3, drafts=(0, 2)), dict(B=5, Hkv=1, G=2, T=(3000, 17, 410, 0, 700), N=1)])]
+    want = [run_decode8(p) for p in ps]
+    ws = max((tokens.new_decode8_workspace(p.cfg, p.N, DEV) for p in ps), key=lambda w: w.numel())
+    for _ in range(2):
+        for p, (o, z) in zip(ps, want):
+            got, lse = run_decode8(p, ws=ws)
+            sync()
+            assert torch.equal(got, o) and torch.equal(lse, z)
+            assert not ws[:16384].any()
+
+
+def test_more_units_than_counters():
+    p = Problem8(DEV, B=600, Hkv=8, G=1, d=64, L=32, T=[(b * 7) % 50 for b in range(600)], N=1, draft=False, extra=128).upload()
+    out, lse = run_decode8(p)
+    sync()
+    p.check(out, lse)
 
 
 def test_decode8_without_a_log_sum_gives_the_same():
