@@ -1,7 +1,7 @@
 // cobs_unpack8: blocks of an 8-bit cache as bf16 or fp32.  A copy, bound by HBM (three times the codes' bytes for bf16).
-// A thread takes 16 codes of a token's head, 16 bytes in, 32 or 64 out; a workgroup a block's keys or values.
-// Measured (d 128, bf16): 4 rows of 32741 tokens of 8 heads, 805 MB, in 154 us, 5.2 TB/s (a large copy: 5.0); the newest block of 32
-// rows 4.5 us.
+// A thread takes 8 codes of a token's head, or 4 for fp32, 16 bytes out; a workgroup a block's keys or values.
+// Measured (d 128, 8 heads): 4 rows of 32741 tokens as bf16, 805 MB, in 140 us, 5.7 TB/s (a large copy: 5.0); as fp32 236 us, 5.7 TB/s;
+// the newest block of 32 rows 4.5 us.
 #include "tokens_device.h"
 
 namespace cobs {
@@ -11,7 +11,8 @@ constexpr int kUnpackThreads = 256;
 // grid: (block and row, KV head, keys or values)
 template <int D, bool F32>
 __global__ __launch_bounds__(kUnpackThreads) void unpack8_kernel(Unpack8Params p) {
-  constexpr int TPR = D / 16;
+  constexpr int E = F32 ? 4 : 8, TPR = D / E, U = 4;      // elements of a thread; its loads under way together
+  using Codes = std::conditional_t<F32, uint32_t, uint2>;
   const int b = blockIdx.x / p.num, which = blockIdx.x % p.num, h = blockIdx.y, value = blockIdx.z;
   const int T = clamp_len(p.seq_lens[b], p.tmax), lsh = p.src.lsh;
   const int blocks = blocks_of(T, lsh);
@@ -25,21 +26,33 @@ __global__ __launch_bounds__(kUnpackThreads) void unpack8_kernel(Unpack8Params p
   void* const out = const_cast<void*>(value ? p.dst.v : p.dst.k);
   const int64_t rs = p.src.table ? D : p.src.st, ws = p.dst.table ? D : p.dst.st;
   const int rows = min(1 << lsh, T - (j << lsh));
-  for (int x = threadIdx.x; x < rows * TPR; x += kUnpackThreads) {
-    const int t = x / TPR, e = 16 * (x % TPR);
-    const uint4 w = *reinterpret_cast<const uint4*>(codes + t * rs + e);
-    const uint32_t c[4] = {w.x, w.y, w.z, w.w};
-    float y[16];
+  // (stores of 16 bytes next to each other: with 16 codes a thread, whose stores lie 32 or 64 bytes apart, 154 and 389 us
+  // for 140 and 236)
+  for (int x0 = threadIdx.x; x0 < rows * TPR; x0 += U * kUnpackThreads) {
+    Codes w[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], true);
-      y[4 * i] = lo[0] * scale;
-      y[4 * i + 1] = lo[1] * scale;
-      y[4 * i + 2] = hi[0] * scale;
-      y[4 * i + 3] = hi[1] * scale;
+    for (int u = 0; u < U; ++u) {
+      const int x = x0 + u * kUnpackThreads;
+      if (x < rows * TPR) w[u] = *reinterpret_cast<const Codes*>(codes + (x / TPR) * rs + E * (x % TPR));
     }
-    store8(out, to + t * ws + e, F32, y);
-    store8(out, to + t * ws + e + 8, F32, y + 8);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = x0 + u * kUnpackThreads;
+      if (x >= rows * TPR) continue;
+      const int64_t at = to + (x / TPR) * ws + E * (x % TPR);
+      float y[E];
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) {
+        const int c = reinterpret_cast<const int*>(&w[u])[i];
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+        y[4 * i] = lo[0] * scale;
+        y[4 * i + 1] = lo[1] * scale;
+        y[4 * i + 2] = hi[0] * scale;
+        y[4 * i + 3] = hi[1] * scale;
+      }
+      if constexpr (F32) *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(y[0], y[1], y[2], y[3]);
+      else store8(out, at, false, y);
+    }
   }
 }
 
