@@ -5,20 +5,20 @@
 // its scale, so a unit holds its tokens in registers between that maximum and their encoding, and memory is
 // read once.  D / 16 lanes take a token's head, 16 elements each.  A unit is taken by
 //   a workgroup   (many new tokens; 256 lanes, PASSES times 16 elements each), which takes several heads in turn, so
-//                 that the cosines and sines of its tokens stay in registers;
+//                 that the cosines and sines of its tokens stay in registers, or in LDS;
 //   a wave        (up to 8 new tokens a row, 16 of 64-element heads);
 //   D / 16 lanes  (one new token a row: a decode step, 8 or 16 units a wave).
 // Scales are powers of two, so a grown scale changes the exponents of the block's earlier codes and nothing else
 // (but for the smallest ones, which are rounded again).
 //
-// Measured (d 128, 8 KV and 32 query heads, bf16): four prompts of 8k to 16k tokens in 284 us with their queries, 1.34 GB, 4.7 TB/s (HBM, the
-// rate of a large copy being 5.0); without queries 102 us, 3.6 TB/s read (a token's heads are apart by the queries') and written, waiting
+// Measured (d 128, 8 KV and 32 query heads, bf16): four prompts of 8k to 16k tokens in 272 us with their queries, 1.34 GB, 4.9 TB/s (HBM, the
+// rate of a large copy being 5.0); without queries 89 us, 4.1 TB/s read (a token's heads are apart by the queries') and written, waiting
 // for a block's maximum between.  One token of 64 rows: 5.4 us, a chain of loads (length, page, row, scale).
 #include "append_body.h"
 
 namespace cobs {
 
-// Query heads from which on a launch of their own rotates them: the workgroups that encode leave a CU three at a time, too few
+// Query heads from which on a launch of their own rotates them: the workgroups that encode leave a CU three or four at a time, too few
 // for a copy (q and all: 446 us for four prompts of 16k tokens, 8 KV and 32 query heads).
 constexpr int64_t kApart = 1 << 15;
 constexpr int kMostItems = 64;         // (head, keys or values) pairs that a workgroup takes in turn
@@ -42,8 +42,13 @@ __device__ __forceinline__ void values4(uint32_t w, float* x) {
   x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
 }
 
+// Whether a workgroup's cosines and sines are in LDS instead of registers, for four workgroups a CU in place of three (four prompts of
+// 8k to 16k tokens 272 us for 285, without queries 89 for 102; fp32, which spills for it, four of 16k without queries 157 for 145).
+template <int LANES, int PASSES, bool F32>
+constexpr bool kTurnsShared = LANES == kHeadThreads && PASSES == 2 && !F32;
+
 template <int D, int LANES, int PASSES, bool F32>
-__global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) {
+__global__ __launch_bounds__(kHeadThreads, (kTurnsShared<LANES, PASSES, F32> ? 4 : 1)) void append8_kernel(Append8Params p) {
   constexpr int TPR = D / 16, RP = LANES / TPR, UNITS = kHeadThreads / LANES;
   constexpr bool GROUP = LANES == kHeadThreads;
   static_assert(GROUP || LANES <= 64, "a workgroup, or lanes of a wave");
@@ -94,9 +99,16 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
     }
   };
   auto scale_of = [&](int it) { return (it < p.t.hkv ? p.k_scale + it * sstep : p.v_scale + (it - p.t.hkv) * sstep) + srow; };
-  load(it0);
-  if (GROUP && earlier > 0 && tid < it1 - it0) s_held[tid] = *scale_of(it0 + tid);
-  float2 cs[PASSES][8];
+  // (workgroups begin with different heads, as those of one head of all tokens may lie in few memory channels: fp32 prompts 145 us for 165)
+  const int items = it1 - it0, shift = GROUP ? bj % items : 0;
+  auto item = [&](int i) { return it0 + (i + shift < items ? i + shift : i + shift - items); };
+  load(item(0));
+  if (GROUP && earlier > 0 && tid < items) s_held[tid] = *scale_of(it0 + tid);
+  // (in LDS by token and pair; twos of pairs change places by the token, so that eight tokens are read from different banks)
+  constexpr bool SHARED = kTurnsShared<LANES, PASSES, F32>;
+  __shared__ __align__(16) float2 turn[SHARED ? PASSES * RP * (D / 2) : 1];
+  auto turn_at = [&](int k, int x) { return &turn[(k * RP + row) * (D / 2) + ((8 * piece + x) ^ (2 * (row & 3)))]; };
+  float2 cs[SHARED ? 1 : PASSES][8];
   if (e.turned && it0 < p.t.hkv) {
 #pragma unroll
     for (int k = 0; k < PASSES; ++k) {
@@ -104,11 +116,16 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
       if (t < t1) {
         const int i = t - r.T, at = p.t.rope.positions ? p.t.rope.positions[(int64_t)b * p.t.N + i] : t;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) cs[k][x] = turn_of(p.t.rope, at, 8 * piece + x);
+        for (int x = 0; x < 8; ++x) {
+          const float2 c = turn_of(p.t.rope, at, 8 * piece + x);
+          if constexpr (SHARED) *turn_at(k, x) = c;        // (read by this lane alone)
+          else cs[k][x] = c;
+        }
       }
     }
   }
-  for (int it = it0; it < it1; ++it) {
+  for (int i = 0; i < items; ++i) {
+    const int it = item(i);
     const bool key = it < p.t.hkv;
     const int h = key ? it : it - p.t.hkv;
     const Piece c = key ? e : straight;
@@ -119,7 +136,17 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
       if (t0 + row + k * RP < t1) {
         widen8(raw[k][0], F32, x[k]);
         widen8(raw[k][1], F32, x[k] + 8);
-        if (c.turned) turn16(x[k], cs[k], p.t.rope.interleaved);
+        if (c.turned) {
+          if constexpr (SHARED) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+              const float4 w = *reinterpret_cast<const float4*>(turn_at(k, i));
+              cs[0][i] = make_float2(w.x, w.y);
+              cs[0][i + 1] = make_float2(w.z, w.w);
+            }
+          }
+          turn16(x[k], cs[SHARED ? 0 : k], p.t.rope.interleaved);
+        }
 #pragma unroll
         for (int y = 0; y < 16; ++y) top = fmaxf(top, fabsf(x[k][y]));      // (NaN leaves it)
       }
@@ -135,12 +162,12 @@ __global__ __launch_bounds__(kHeadThreads) void append8_kernel(Append8Params p) 
           top = fmaxf(top, fabsf(x[k][y]));
         }
     }
-    if (it + 1 < it1) load(it + 1);
+    if (i + 1 < items) load(item(i + 1));
     float* const scale = scale_of(it);
     float held = 0.0f;
     if constexpr (GROUP) {
       top = wave_max_rows(top);
-      const int buf = (it - it0) & 1;                   // (a barrier lies between a buffer's use and its next writing)
+      const int buf = i & 1;                   // (a barrier lies between a buffer's use and its next writing)
       if ((tid & 63) == 0) s_top[buf][tid >> 6] = top;
       __syncthreads();
 #pragma unroll
@@ -203,7 +230,7 @@ static hipError_t launch_d(Append8Params p, hipStream_t st) {
   if (lanes == kHeadThreads) {
     // Heads of a workgroup, which share their tokens' cosines and sines: as many as leave two workgroups a CU, keys and values apart
     // (16000 tokens in blocks of 128, 8 heads: 26 us; by 2048 workgroups of one head each 38; 49000 tokens by workgroups of
-    // 8 heads' keys or values 102, of both 130).
+    // 8 heads' keys or values 89, when those took 102 by workgroups of both 130).
     const int64_t all = (int64_t)p.t.B * p.blocks * 2 * p.t.hkv;
     const int top = p.t.hkv < kMostItems ? p.t.hkv : kMostItems;
     p.items = (int)(all / 512 < top ? all / 512 : top);
