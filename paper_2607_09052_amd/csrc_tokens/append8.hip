@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kHeadThreads, (kTurnsShared<LANES, PASSES, F32> ? 4
   const int64_t sstep = p.kv.table ? 1 : p.kv.nbmax;
 
   const int lane = tid % LANES, row = lane / TPR, piece = lane % TPR;
-  const Piece e = piece_of(p.t.rope, piece), straight = {16 * piece, 16 * piece + 8, false};
+  const Piece e = piece_of<D>(p.t.rope, piece), straight = {16 * piece, 16 * piece + 8, false};
   // the new tokens' rows of an item as they come; the next item's are loaded while one is encoded
   Raw8 raw[PASSES][2];
   auto load = [&](int it) {
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kHeadThreads, (kTurnsShared<LANES, PASSES, F32> ? 4
         const int i = t - r.T, at = p.t.rope.positions ? p.t.rope.positions[(int64_t)b * p.t.N + i] : t;
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
-          const float2 c = turn_of(p.t.rope, at, 8 * piece + x);
+          const float2 c = turn_of(p.t.rope, at, pair_of(p.t.rope, piece, x));
           if constexpr (SHARED) *turn_at(k, x) = c;        // (read by this lane alone)
           else cs[k][x] = c;
         }

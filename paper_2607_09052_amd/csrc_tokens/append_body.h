@@ -7,8 +7,8 @@
 // elements and all heads of a token share it.  Then a thread takes 16 elements of a head, both
 // sides of 8 pairs, in two 16-byte pieces (bf16).
 //
-// Measured (d 128, bf16): 8190 tokens of 32 heads rotated in 29.8 us, 4.5 TB/s; 32749 tokens of 32 query and 8 KV heads
-// appended in 172 us, 4.7 TB/s (a large copy: 5.0); one token of 64 rows 4.6 us, the chain of loads.
+// Measured (d 128, bf16): 8190 tokens of 32 heads rotated in 29.8 us, 4.5 TB/s, one round of workgroups; 32000 in 98 us, 5.3 TB/s;
+// 32749 tokens of 32 query and 8 KV heads appended in 161 us, 5.0 TB/s (a large copy: 5.0); one token of 64 rows 4.6 us, the chain of loads.
 #pragma once
 
 #include "tokens_device.h"
@@ -16,7 +16,7 @@
 namespace cobs {
 
 constexpr int kHeadThreads = 256;
-constexpr int kMostTokens = 4;       // tokens of a workgroup
+constexpr int kMostTokens = 8;       // tokens of a workgroup
 
 struct HeadsShared {
   float2 turn[kMostTokens][64];
@@ -61,7 +61,7 @@ __device__ __forceinline__ void heads_body(const NewTokens& p, const KvView* kv,
   }
   __syncthreads();
   const int piece = tid % TPR;
-  const Piece e = piece_of(p.rope, piece);
+  const Piece e = piece_of<D>(p.rope, piece);
   const int64_t head_step = CACHE ? (kv->table ? ((int64_t)D << kv->lsh) : kv->sh) : 0;
   const int rows = per_wg * (h1 - h0);
   for (int x = tid / TPR; x < rows; x += kHeadThreads / TPR) {
@@ -91,7 +91,7 @@ __device__ __forceinline__ void heads_body(const NewTokens& p, const KvView* kv,
     if (turned) {
       float2 cs[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) cs[j] = s.turn[k][8 * piece + j];
+      for (int j = 0; j < 8; ++j) cs[j] = s.turn[k][pair_of(p.rope, piece, j)];
       turn16(y, cs, p.rope.interleaved);
     }
     store8(out, to + e.e0, f32, y);
@@ -99,11 +99,14 @@ __device__ __forceinline__ void heads_body(const NewTokens& p, const KvView* kv,
   }
 }
 
-// Tokens and heads of a workgroup: with tokens enough to fill the card four tokens and all their heads, else
-// one token and 256 threads' worth of heads.
+// Tokens and heads of a workgroup: with tokens enough to fill the card all heads of as many tokens as are two passes
+// of its threads, else one token and 256 threads' worth of heads.  (By 4 tokens, 6 passes: 32749 tokens of 32 query and 8 KV heads
+// appended in 173 us, by 2 in 164; by 4, half a pass: 64000 tokens of 2 KV heads 48 us for 38.)
 inline void plan_heads(int64_t tokens, int heads, int d, int* per_wg, int* slots, int* groups) {
-  *per_wg = tokens >= 4 * 1024 ? kMostTokens : 1;
-  *slots = *per_wg > 1 ? heads : kHeadThreads / (d / 16);
+  const bool many = tokens >= 4 * 1024;
+  *per_wg = 1;
+  while (many && *per_wg < kMostTokens && *per_wg * heads * (d / 16) < 2 * kHeadThreads) *per_wg *= 2;
+  *slots = many ? heads : kHeadThreads / (d / 16);
   if (*slots > heads) *slots = heads;
   *groups = (heads + *slots - 1) / *slots;
 }
