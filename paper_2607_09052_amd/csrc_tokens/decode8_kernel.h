@@ -18,8 +18,8 @@
 // What bounds it, d 128, bf16 queries: one token of 16 rows of 32k tokens (4 heads a KV head): 1.07 GB in 178 us, 6.0 TB/s, HBM.
 // From 32 rows on the waves' instructions: a frame of 32 rows is some 270 vector instructions (80 of them conversions)
 // and 24 products of 32 cycles, and two waves a SIMD overlap little of the one with the other (16 drafted tokens of 8 heads
-// over 4 contexts of 16k to 32k: 43 GFLOP, 64 with the probabilities' second part, in 98 us; vector pipes busy 55 % of the time, matrix
-// pipes 40 %).  Tried for that: frames shared through LDS and converted once (64 rows over 8 x 16k tokens: 115 us for 89), tiles of 16
+// over 4 contexts of 16k to 32k: 43 GFLOP, 64 with the probabilities' second part, in 98 us; vector pipes busy 63 % of the time, matrix
+// pipes 39 %).  Tried for that: frames shared through LDS and converted once (64 rows over 8 x 16k tokens: 115 us for 89), tiles of 16
 // rows two a wave (89 for 88), both frames' codes in registers (spills), a wave's priority raised in its products (85 for 82).
 //
 // The codes of tokens that take no part are cleared; a NaN in a drafted token's value, which not all queries see,
