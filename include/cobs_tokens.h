@@ -62,7 +62,7 @@ cobs_status_t cobs_rotate(const cobs_heads_t* x, cobs_dtype_t in_dtype, int32_t 
 /* New tokens behind a cache's: token i < n of row b, n = new_lens[b] (clamped to [0, num_new];
  * new_lens NULL: num_new), becomes cached token T + i, T = seq_lens[b] (clamped), its key
  * rotated, its value as it is, rounded once to kv_dtype.
- *   k_new, v_new: in_dtype COBS_F32 or COBS_BF16, [B, num_new, Hkv, d] by their strides.
+ *   k_new, v_new: in_dtype COBS_F32 or COBS_BF16, [B, num_new, Hkv, d] by their strides, apart from what the call writes.
  *   rope:      NULL leaves keys and queries as they are.
  *   positions: optional device int32 [B, num_new]; NULL: T + i (the place in the cache;
  *              after an eviction, or for a draft's tree, the positions are others).
@@ -71,8 +71,8 @@ cobs_status_t cobs_rotate(const cobs_heads_t* x, cobs_dtype_t in_dtype, int32_t 
  *              (same type and strides), or apart from all else.  Queries i >= n are left as they were.
  *   new_seq_lens: optional device int32 [B], written: min(T + n, max_seq_len); not seq_lens itself.
  *   Tokens behind the cache's capacity, or whose page id is out of range, are dropped.
- *   1 <= num_new, batch * num_new <= 2^24.  Rows and heads of the cache share no memory
- *   (strides of 0 are refused; no page is in a table twice).
+ *   1 <= num_new, batch * num_new <= 2^24.  Keys, values, rows and heads of the cache share no memory
+ *   (strides of 0 and one pointer for both are refused; no page is in a table twice).
  * The records of the blocks that got tokens are stale afterwards (cobs_decode_step
  * refreshes the newest; cobs_build_block_stats rebuilds any).                       */
 cobs_status_t cobs_append(const cobs_config_t* cfg, const cobs_heads_t* k_new, const cobs_heads_t* v_new,
@@ -114,8 +114,9 @@ cobs_status_t cobs_append8(const cobs_config_t* cfg, const cobs_heads_t* k_new, 
                            int32_t* new_seq_lens, void* stream);
 
 /* Workspace bytes of cobs_decode8 (0 if invalid).  It has to be zero-filled before its first use;
- * every call leaves its arrival counters (the first 16 KB) zero again, so that later calls on the
- * same stream, of other shapes too, may use it.  Calls that share it must not overlap in time. */
+ * every call leaves its arrival counters (the first 16 KB) zero again, so that later calls of cobs_decode8
+ * on the same stream, of other shapes too, may use it; other operators may not, as they leave
+ * what they like there.  Calls that share it must not overlap in time. */
 size_t cobs_decode8_workspace_bytes(const cobs_config_t* cfg, int32_t num_queries);
 
 /* Attention of num_queries query tokens a row (1 <= num_queries <= 64) over an 8-bit cache.
@@ -138,7 +139,7 @@ cobs_status_t cobs_decode8(const cobs_config_t* cfg, const void* q, cobs_dtype_t
  *   T = seq_lens[b] tokens has; first_block = -1: its last num_blocks blocks.  num_blocks >= 0.
  *   dst: strides or pages of its own, apart from the source.  Tokens from T on, and those whose
  *   page is out of range in the source or in dst (so a table may have pages for the wanted
- *   blocks alone), are left as they were.  Rows and heads of dst share no memory.              */
+ *   blocks alone), are left as they were.  Keys, values, rows and heads of dst share no memory.              */
 cobs_status_t cobs_unpack8(const cobs_config_t* cfg, const cobs_kv8_t* kv, const int32_t* seq_lens,
                            int32_t first_block, int32_t num_blocks, const cobs_kv_t* dst, void* stream);
 

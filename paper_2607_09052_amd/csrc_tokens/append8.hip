@@ -140,9 +140,9 @@ __global__ __launch_bounds__(kHeadThreads, (kTurnsShared<LANES, PASSES, F32> ? 4
           if constexpr (SHARED) {
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-              const float4 w = *reinterpret_cast<const float4*>(turn_at(k, i));
-              cs[0][i] = make_float2(w.x, w.y);
-              cs[0][i + 1] = make_float2(w.z, w.w);
+              const float2* const two = turn_at(k, i);
+              cs[0][i] = two[0];
+              cs[0][i + 1] = two[1];
             }
           }
           turn16(x[k], cs[SHARED ? 0 : k], p.t.rope.interleaved);

@@ -104,9 +104,11 @@ cobs_status_t new_tokens(const cobs_config_t* cfg, const cobs_heads_t* k_new, co
   return COBS_OK;
 }
 
-// A cache that is written: rows and heads that share memory cannot be.
-bool shares_rows(const cobs_config_t* c, bool paged, int64_t stride_b, int64_t stride_h) {
-  return !paged && ((c->batch > 1 && stride_b == 0) || (c->num_kv_heads > 1 && stride_h == 0));
+// A cache that is written: keys, values, rows and heads that share memory cannot be.
+template <typename Kv>
+bool shares_memory(const cobs_config_t* c, const Kv* kv) {
+  if (kv->k == kv->v) return true;
+  return !kv->block_table && ((c->batch > 1 && kv->stride_b == 0) || (c->num_kv_heads > 1 && kv->stride_h == 0));
 }
 
 cobs_status_t check_cache8(const cobs_config_t* c, const cobs_kv8_t* kv) {
@@ -157,7 +159,7 @@ cobs_status_t cobs_append(const cobs_config_t* cfg, const cobs_heads_t* k_new, c
   cobs_status_t s = check_shape(cfg);
   if (s != COBS_OK) return s;
   if ((s = check_cache(cfg, kv)) != COBS_OK) return s;
-  if (shares_rows(cfg, kv->block_table != nullptr, kv->stride_b, kv->stride_h)) return COBS_ERR_INVALID_ARG;
+  if (shares_memory(cfg, kv)) return COBS_ERR_INVALID_ARG;
   s = new_tokens(cfg, k_new, v_new, in_dtype, num_new, seq_lens, new_lens, rope, positions, q, q_out, q_dtype, new_seq_lens,
                  &p.t);
   if (s != COBS_OK) return s;
@@ -175,7 +177,7 @@ cobs_status_t cobs_append8(const cobs_config_t* cfg, const cobs_heads_t* k_new, 
   cobs_status_t s = check_shape(cfg);
   if (s != COBS_OK) return s;
   if ((s = check_cache8(cfg, kv)) != COBS_OK) return s;
-  if (shares_rows(cfg, kv->block_table != nullptr, kv->stride_b, kv->stride_h)) return COBS_ERR_INVALID_ARG;
+  if (shares_memory(cfg, kv) || kv->k_scale == kv->v_scale) return COBS_ERR_INVALID_ARG;
   s = new_tokens(cfg, k_new, v_new, in_dtype, num_new, seq_lens, new_lens, rope, positions, q, q_out, q_dtype, new_seq_lens,
                  &p.t);
   if (s != COBS_OK) return s;
@@ -220,7 +222,7 @@ cobs_status_t cobs_unpack8(const cobs_config_t* cfg, const cobs_kv8_t* kv, const
   if (s != COBS_OK) return s;
   if ((s = check_cache8(cfg, kv)) != COBS_OK) return s;
   if ((s = check_cache(cfg, dst)) != COBS_OK) return s;
-  if (shares_rows(cfg, dst->block_table != nullptr, dst->stride_b, dst->stride_h)) return COBS_ERR_INVALID_ARG;
+  if (shares_memory(cfg, dst)) return COBS_ERR_INVALID_ARG;
   const int32_t nb = cfg->max_seq_len / cfg->block_size;
   if (!seq_lens || first_block < -1 || first_block > nb || num_blocks < 0 || num_blocks > nb - (first_block < 0 ? 0 : first_block))
     return COBS_ERR_INVALID_ARG;

@@ -27,8 +27,10 @@ ROTATIONS = [
     dict(B=3, N=5, H=4, d=64, r=64),
     dict(B=2, N=33, H=3, d=128, r=96, inter=True, scale=1.25),
     dict(B=1, N=257, H=40, d=128, r=64, base=5e5),
-    dict(B=2, N=2500, H=2, d=64, r=32, inter=True),                   # more than 4096 tokens: four to a workgroup
+    dict(B=2, N=2500, H=2, d=64, r=32, inter=True),                   # more than 4096 tokens: several to a workgroup
     dict(B=1, N=4099, H=5, d=128, r=112),
+    dict(B=3, N=1367, H=33, d=128, r=128, inter=True),                # two tokens to a workgroup
+    dict(B=1, N=4101, H=66, d=128, r=80),                             # one, and all its heads
 ]
 
 
@@ -122,6 +124,21 @@ def test_append_matches_fp64(shape, io, kv, out, layout):
 def test_append8_matches_the_definition(shape, io, out, layout):
     say(f"append8 {shape} {io} {out} {layout}")
     p = Appending(DEV, io=io, out=out, layout=layout, eight=True, **shape).fresh().call()
+    sync()
+    p.check_cache8()
+    p.check_queries()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [
+    dict(B=5, Hkv=8, G=1, N=900, T=(0, 70, 3, 64, 127), new=(900, 0, 850, 17, 900), inter=True),      # two heads in turn
+    dict(B=7, Hkv=9, G=1, d=64, L=32, N=600, T=(0, 5, 31, 32, 40, 7, 100), r=32),                     # four
+    dict(B=3, Hkv=8, G=2, N=2000, T=(0, 130, 90), L=128),
+    dict(B=16, Hkv=8, G=2, N=520, T=[11 * b for b in range(16)]),                                     # four, queries by a launch of their own
+], ids=_ids)
+def test_append8_by_workgroups_of_several_heads(shape, io):
+    say(f"append8 {shape} {io}")
+    p = Appending(DEV, io=io, out="bf16", layout="pages", eight=True, **shape).fresh().call()
     sync()
     p.check_cache8()
     p.check_queries()

@@ -165,6 +165,12 @@ def test_append_refuses(eight, edit, code):
     assert _append(eight, **edit) == code
 
 
+def test_caches_whose_keys_are_their_values_are_not_written():
+    assert _append(False, kv=_kv(v=FAKE)) == 1 and _append(False, kv=_kv(v=FAKE, block_table=FAKE, num_pages=4)) == 1
+    assert _append(True, kv=_kv8(v=FAKE)) == 1 and _append(True, kv=_kv8(v_scale=FAKE + 8192)) == 1
+    assert _unpack(dst=_kv(k=OTHER, v=OTHER)) == 1
+
+
 def test_caches_that_share_rows_and_bad_caches_are_refused():
     for over in (dict(stride_b=0), dict(stride_h=0), dict(stride_t=64), dict(stride_t=130), dict(k=None), dict(v=FAKE + 8),
                  dict(block_table=FAKE, num_pages=0)):
