@@ -125,8 +125,9 @@ size_t cobs_decode8_workspace_bytes(const cobs_config_t* cfg, int32_t num_querie
  * behind it.  One query without a draft is a decode step.
  * A token that a query does not attend to has no effect on it, whatever its codes are.
  * Scores, softmax and sums are fp32.  The matrix cores take the codes as bf16, which is exact, an
- * fp32 query and its probabilities as three bf16 parts, which hold all their bits; with io_dtype
- * COBS_BF16 the probabilities enter as two (2^-17) and the outputs are rounded once.            */
+ * fp32 query and the probabilities as three bf16 parts, which hold all their bits; with io_dtype
+ * COBS_BF16 and more than 16 query rows of a KV head (num_queries * num_q_heads / num_kv_heads)
+ * the probabilities enter as two (2^-17).  bf16 outputs are rounded once.                       */
 cobs_status_t cobs_decode8(const cobs_config_t* cfg, const void* q, cobs_dtype_t io_dtype, int32_t num_queries,
                            const cobs_kv8_t* kv, const int32_t* seq_lens, const int32_t* draft_lens,
                            const uint64_t* tree_mask, int32_t sparse, const int32_t* sel, void* out, float* lse,

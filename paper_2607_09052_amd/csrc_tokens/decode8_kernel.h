@@ -420,6 +420,12 @@ __device__ __forceinline__ void join_parts(const TreeParams& p, const TreePart& 
   }
 }
 
+// bf16 parts of a probability: three, which hold all its bits, or two (2^-17) where the query is bf16 and the product's time counts.  Tiles of 16
+// rows wait for memory, and the third part is free (one token of 16 rows of 32k tokens 182.2 us, with two parts 181.8; 1k tokens 10.3 and 10.2);
+// tiles of 32 rows wait for the waves' instructions (16 drafted tokens of 8 heads over 4 contexts of 16k to 32k: 126 us with three, 108 with two).
+template <int PARTS, int R>
+constexpr int kProbabilityParts = PARTS == 3 || R == 16 ? 3 : 2;
+
 // Workgroups that a CU takes: three where they need not spill for it (64 rows over 8 x 16k tokens of 64-element heads: 54 us,
 // by two 61).
 template <int D, int PARTS, int R>
@@ -428,7 +434,7 @@ constexpr int kWorkgroups8 = D == 64 && (PARTS == 1 || R == 16) ? 3 : 2;
 template <int D, int PARTS, int R>
 __global__ __launch_bounds__(kTreeThreads, (kWorkgroups8<D, PARTS, R>)) void decode8_kernel(Decode8Params p) {
   using T = Tile8<D, R>;
-  constexpr int WT = 4, KS = T::KS, NO = T::NO, PP = PARTS == 3 ? 3 : 2;
+  constexpr int WT = 4, KS = T::KS, NO = T::NO, PP = kProbabilityParts<PARTS, R>;
   constexpr bool SHARED = D == 128 && R == 32 && PARTS == 3;      // the queries' operands in LDS (the pool's place): in registers they spill
   __shared__ Frame8 table[kTable8];
   __shared__ __align__(16) float pool[WT * R * D];
