@@ -39,8 +39,9 @@ typedef struct {
  * lo = p, hi = p + r/2 (interleaved = 0) or lo = 2p, hi = 2p + 1 (interleaved = 1).  The
  * elements from r on are left as they are.  The frequencies are the caller's, so that any
  * scaling of them for long contexts is a matter of this table.
- *   inv_freq: device fp32 [r/2], f_p in radians, finite.  t f_p is taken in fp64 before it is
- *             reduced, so far positions lose nothing; the pair's products are fp32.
+ *   inv_freq: device fp32 [r/2], f_p in radians, |t f_p| <= 2^51 (all positions: |f_p| <= 2^20);
+ *             a pair whose angle is past that, or not finite, becomes NaN.  t f_p is exact before
+ *             it is reduced, so far positions lose nothing; the pair's products are fp32.
  *   rotary_dim: a multiple of 16, 16 <= r <= d.  scale: finite.                       */
 typedef struct {
   const float* inv_freq;

@@ -6,13 +6,16 @@
 
 namespace cobs {
 
-// Cosine and sine of `a`, in fp64 up to the reduction to |x| <= pi / 4 (n quarter turns taken off in two
-// parts, after Cody and Waite), then by their power series, whose next terms are below 2^-28.
-__device__ __forceinline__ float2 cos_sin(double a) {
+// Cosine and sine of t f, |t f| <= 2^51 (NaN beyond): the product in two fp64 halves, as it has up to 55 bits, reduced to |x| <= pi / 4
+// (n quarter turns taken off in two parts, after Cody and Waite), then power series, whose next terms are below 2^-28.
+// Past 2^51 n would be no integer that kMagic's sum holds.
+__device__ __forceinline__ float2 cos_sin(double t, double f) {
   constexpr double kMagic = 6755399441055744.0;                 // 1.5 * 2^52: its sum's low bits are the integer
-  const double t = fma(a, 0.6366197723675814, kMagic), n = t - kMagic;
-  const float x = (float)fma(-n, 6.123233995736766e-17, fma(-n, 1.5707963267948966, a));
-  const int quarter = __double2loint(t);
+  const double a = t * f, rest = fma(t, f, -a);
+  const double turns = fma(a, 0.6366197723675814, kMagic), n = turns - kMagic;
+  const double y = fma(-n, 1.5707963267948966, a) + fma(-n, 6.123233995736766e-17, rest);
+  const float x = fabs(a) <= 2251799813685248.0 ? (float)y : __uint_as_float(0x7fc00000u);
+  const int quarter = __double2loint(turns);
   const float z = x * x;
   const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
   const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
@@ -22,7 +25,7 @@ __device__ __forceinline__ float2 cos_sin(double a) {
 
 // Cosine and sine, times the rotation's scale, of pair `pair` at position `t`.
 __device__ __forceinline__ float2 turn_of(const RopeView& r, int t, int pair) {
-  const float2 y = cos_sin((double)t * (double)r.freq[pair]);
+  const float2 y = cos_sin((double)t, (double)r.freq[pair]);
   return make_float2(y.x * r.scale, y.y * r.scale);
 }
 

@@ -1,5 +1,8 @@
 """The token operators at the ends of what their header allows, in small problems whose answers are known by arithmetic."""
 
+import math
+from decimal import Decimal, localcontext
+
 import numpy as np
 import pytest
 import torch
@@ -51,3 +54,56 @@ def test_probabilities_of_up_to_16_rows_enter_with_all_their_bits(d, G, N, io):
     off = np.abs(f64(out) - want) * (p + tail)[:, None, None, None]
     say(f"largest error {off.max() / U32:.1f} half steps")
     assert np.all(off <= 27 * U32 + 2.0 ** -8 * np.abs(want) * (p + tail)[:, None, None, None])
+
+
+# ------------------------------------------------------------------ angles --
+PI = Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798")
+
+
+def exact_turn(t, f):
+    """Cosine and sine of t f, whose exact product is reduced with 100 digits."""
+    with localcontext() as ctx:
+        ctx.prec = 160
+        a = float((Decimal(t) * Decimal(f)) % (2 * PI))
+    return math.cos(a), math.sin(a)
+
+
+FAR_FREQUENCIES = [2.0 ** 20, 2.0 ** 20 - 2.0 ** -4, 543210.9375, 12345.678, 1.0, 0.9999999, 1.0 / 3.0, 1e-6]
+FAR_POSITIONS = [(1 << 31) - 1, -(1 << 31), (1 << 31) - 12345, -(1 << 30) - 1, 1 << 29, 987654321, 4099, -7, 0]
+
+
+def _turned(positions, frequencies):
+    """Cosines and sines [positions, frequencies] that a rotation of (1, 0) gives, 8 pairs at a time."""
+    x = torch.zeros((1, len(positions), 1, 64), device=DEV)
+    x[..., :8] = 1.0
+    y = torch.empty_like(x)
+    at = torch.tensor([positions], dtype=torch.int64).to(torch.int32).to(DEV)
+    freq = torch.zeros(8)
+    freq[:len(frequencies)] = torch.tensor(frequencies, dtype=torch.float64).float()
+    tokens.cobs_rotate(x, tokens.Rope(freq.to(DEV)), at, y)
+    sync()
+    n = len(frequencies)
+    return freq[:n].double().tolist(), f64(y)[0, :, 0, :n], f64(y)[0, :, 0, 8:8 + n]
+
+
+def test_angles_up_to_2_51():
+    """Every position at frequencies of up to 2^20: the product of both has up to 55 bits."""
+    freq, cos, sin = _turned(FAR_POSITIONS, FAR_FREQUENCIES)
+    for i, t in enumerate(FAR_POSITIONS):
+        for j, f in enumerate(freq):
+            c, s = exact_turn(t, f)
+            # (the tolerance of a rotation of (1, 0) in fp32: rotation_tolerance)
+            assert abs(cos[i, j] - c) <= 8 * U32 + U32 * abs(c), (t, f)
+            assert abs(sin[i, j] - s) <= 8 * U32 + U32 * abs(s), (t, f)
+
+
+def test_angles_past_2_51_give_nan():
+    far = [2.0 ** 21, 2.0 ** 22, 2.0 ** 31, 1e12, 1e20, 1e30, 3e38, math.inf]
+    freq, cos, sin = _turned([(1 << 31) - 1, -(1 << 31), 1 << 30, 1, 0], far)
+    for i, t in enumerate(((1 << 31) - 1, -(1 << 31), 1 << 30, 1, 0)):
+        for j, f in enumerate(freq):
+            if abs(t) * f <= 2.0 ** 51:                    # (0 times infinity is not)
+                c, s = exact_turn(t, f)
+                assert abs(cos[i, j] - c) <= 9 * U32 and abs(sin[i, j] - s) <= 9 * U32, (t, f)
+            else:
+                assert np.isnan(cos[i, j]) and np.isnan(sin[i, j]), (t, f)
