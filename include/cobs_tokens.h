@@ -72,8 +72,9 @@ cobs_status_t cobs_rotate(const cobs_heads_t* x, cobs_dtype_t in_dtype, int32_t 
  *              (same type and strides), or apart from all else.  Queries i >= n are left as they were.
  *   new_seq_lens: optional device int32 [B], written: min(T + n, max_seq_len); not seq_lens itself.
  *   Tokens behind the cache's capacity, or whose page id is out of range, are dropped.
- *   1 <= num_new, batch * num_new <= 2^24.  Keys, values, rows and heads of the cache share no memory
- *   (strides of 0 and one pointer for both are refused; no page is in a table twice).
+ *   1 <= num_new, batch * num_new <= 2^24.  Keys and values, and rows, heads and tokens of the cache, share no
+ *   memory (one pointer for both is refused, and strides of which, sorted, one does not span the ones before it, as
+ *   with cobs_heads_t; no page is in a table twice).
  * The records of the blocks that got tokens are stale afterwards (cobs_decode_step
  * refreshes the newest; cobs_build_block_stats rebuilds any).                       */
 cobs_status_t cobs_append(const cobs_config_t* cfg, const cobs_heads_t* k_new, const cobs_heads_t* v_new,
@@ -141,7 +142,8 @@ cobs_status_t cobs_decode8(const cobs_config_t* cfg, const void* q, cobs_dtype_t
  *   T = seq_lens[b] tokens has; first_block = -1: its last num_blocks blocks.  num_blocks >= 0.
  *   dst: strides or pages of its own, apart from the source.  Tokens from T on, and those whose
  *   page is out of range in the source or in dst (so a table may have pages for the wanted
- *   blocks alone), are left as they were.  Keys, values, rows and heads of dst share no memory.              */
+ *   blocks alone), are left as they were.  Keys, values, rows, heads and tokens of dst share no memory
+ *   (refused as for cobs_append).                                                                  */
 cobs_status_t cobs_unpack8(const cobs_config_t* cfg, const cobs_kv8_t* kv, const int32_t* seq_lens,
                            int32_t first_block, int32_t num_blocks, const cobs_kv_t* dst, void* stream);
 

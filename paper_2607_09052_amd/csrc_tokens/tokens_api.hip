@@ -26,11 +26,9 @@ cobs_status_t check_heads(const cobs_heads_t* x, cobs_dtype_t type, const HeadsS
   return COBS_OK;
 }
 
-// Whether no two elements share memory: each stride spans the dimensions of smaller strides.
-bool apart(const cobs_heads_t* x, const HeadsShape& n) {
-  int64_t size[3] = {n.batch, n.tokens, n.heads};
-  const int64_t stride[3] = {x->stride_b, x->stride_n, x->stride_h};
-  int64_t extent = n.d;
+// Whether no two elements share memory: sorted, each stride spans the dimensions of smaller ones and the d elements of a row.
+bool apart(const int64_t (&stride)[3], const int64_t (&shape)[3], int64_t d) {
+  int64_t size[3] = {shape[0], shape[1], shape[2]}, extent = d;
   for (int k = 0; k < 3; ++k) {
     int at = -1;
     for (int i = 0; i < 3; ++i)
@@ -62,7 +60,7 @@ cobs_status_t check_out(const cobs_heads_t* x, cobs_dtype_t in, const cobs_heads
   cobs_status_t s;
   if (!io_type(in) || !io_type(out)) return COBS_ERR_INVALID_ARG;
   if ((s = check_heads(x, in, n)) != COBS_OK || (s = check_heads(y, out, n)) != COBS_OK) return s;
-  if (!apart(y, n)) return COBS_ERR_INVALID_ARG;
+  if (!apart({y->stride_b, y->stride_n, y->stride_h}, {n.batch, n.tokens, n.heads}, n.d)) return COBS_ERR_INVALID_ARG;
   const bool same = (n.batch == 1 || x->stride_b == y->stride_b) && (n.tokens == 1 || x->stride_n == y->stride_n) &&
                     (n.heads == 1 || x->stride_h == y->stride_h) && in == out;
   return x->p == y->p && !same ? COBS_ERR_INVALID_ARG : COBS_OK;
@@ -104,11 +102,11 @@ cobs_status_t new_tokens(const cobs_config_t* cfg, const cobs_heads_t* k_new, co
   return COBS_OK;
 }
 
-// A cache that is written: keys, values, rows and heads that share memory cannot be.
+// A cache that is written: keys and values, or rows, heads and tokens, that share memory cannot be.
 template <typename Kv>
 bool shares_memory(const cobs_config_t* c, const Kv* kv) {
   if (kv->k == kv->v) return true;
-  return !kv->block_table && ((c->batch > 1 && kv->stride_b == 0) || (c->num_kv_heads > 1 && kv->stride_h == 0));
+  return !kv->block_table && !apart({kv->stride_b, kv->stride_h, kv->stride_t}, {c->batch, c->num_kv_heads, c->max_seq_len}, c->head_dim);
 }
 
 cobs_status_t check_cache8(const cobs_config_t* c, const cobs_kv8_t* kv) {

@@ -181,6 +181,29 @@ def test_caches_that_share_rows_and_bad_caches_are_refused():
         assert _append(True, kv=_kv8(**{name: None})) == 1 and _append(True, kv=_kv8(**{name: FAKE + 2})) == 1
 
 
+@pytest.mark.parametrize("over", [
+    dict(stride_b=16), dict(stride_b=(1 << 19) + 128), dict(stride_b=(1 << 20) - 16),           # rows: inside heads, over the last tokens
+    dict(stride_h=64), dict(stride_h=128), dict(stride_h=(1 << 19) - 128),                     # heads: inside a token, on tokens
+    dict(stride_h=128, stride_t=192), dict(stride_h=64, stride_t=128),                         # heads beside each other in too short a token
+    dict(stride_b=256, stride_h=128, stride_t=384),                                            # rows beside each other, too
+    dict(stride_t=1 << 19, stride_h=1 << 20),                                                  # a head's tokens over the next's
+], ids=str)
+def test_caches_whose_rows_or_heads_overlap_are_not_written(over):
+    assert _append(False, kv=_kv(**over)) == 1 and _append(True, kv=_kv8(**over)) == 1
+    assert _unpack(dst=_kv(k=OTHER, v=OTHER + 4096, **over)) == 1
+
+
+@pytest.mark.parametrize("over", [
+    dict(), dict(stride_t=256, stride_h=128), dict(stride_t=512, stride_h=128, stride_b=256), dict(stride_b=128, stride_t=256, stride_h=1 << 20),
+    dict(stride_h=(1 << 19) + 16, stride_b=(1 << 20) + 64),
+], ids=str)
+def test_layouts_without_overlap_are_taken(over):
+    """(as far as the next check: too many tokens, too many blocks)"""
+    assert _append(False, kv=_kv(**over), N=1 << 24, q=None, q_out=None) == 2 and _append(True, kv=_kv8(**over), N=1 << 24, q=None, q_out=None) == 2
+    one = _cfg(batch=1, num_kv_heads=1, num_q_heads=4)               # strides of dimensions of 1 are not used
+    assert _append(False, one, kv=_kv(stride_b=0, stride_h=0), N=(1 << 24) + 1, q=None, q_out=None) == 2
+
+
 @pytest.mark.parametrize("edit,code", [(dict(num_q_heads=6), 2), (dict(head_dim=96), 2), (dict(block_size=48, max_seq_len=4800), 2),
                                        (dict(max_seq_len=100), 1), (dict(batch=0), 1), (dict(num_kv_heads=3), 1)])
 def test_configs_are_refused(edit, code):
