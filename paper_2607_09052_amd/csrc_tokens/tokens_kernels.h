@@ -5,6 +5,9 @@
 
 namespace cobs {
 
+// Workgroups of a launch: HIP takes fewer than 2^32 threads in a dimension, and a workgroup has 256.  A call of more takes several launches.
+constexpr int64_t kLaunchGroups = 1 << 23;
+
 // Heads of tokens by their strides, in elements.
 struct HeadsView {
   void* p;
@@ -36,6 +39,7 @@ struct AppendParams {
   KvView kv;
   int kv_f32;
   int per_wg, slots, slot_groups;    // tokens and heads of a workgroup, groups of heads (set by the launcher)
+  int first_wg;                 // the launch's first workgroup
 };
 
 struct Append8Params {
@@ -54,6 +58,7 @@ struct Unpack8Params {
   const float* v_scale;
   const int32_t* seq_lens;
   int B, hkv, d, tmax, first, num, f32;
+  int first_row;                // the launch's first row (set by the launcher)
 };
 
 struct Decode8Params {

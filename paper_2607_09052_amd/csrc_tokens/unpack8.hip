@@ -13,7 +13,7 @@ template <int D, bool F32>
 __global__ __launch_bounds__(kUnpackThreads) void unpack8_kernel(Unpack8Params p) {
   constexpr int E = F32 ? 4 : 8, TPR = D / E, U = 4;      // elements of a thread; its loads under way together
   using Codes = std::conditional_t<F32, uint32_t, uint2>;
-  const int b = blockIdx.x / p.num, which = blockIdx.x % p.num, h = blockIdx.y, value = blockIdx.z;
+  const int b = p.first_row + blockIdx.x / p.num, which = blockIdx.x % p.num, h = blockIdx.y, value = blockIdx.z;
   const int T = clamp_len(p.seq_lens[b], p.tmax), lsh = p.src.lsh;
   const int blocks = blocks_of(T, lsh);
   const int j = (p.first >= 0 ? p.first : max(0, blocks - p.num)) + which;
@@ -56,19 +56,24 @@ __global__ __launch_bounds__(kUnpackThreads) void unpack8_kernel(Unpack8Params p
   }
 }
 
-hipError_t launch_unpack8(const Unpack8Params& p, hipStream_t st) {
-  if (p.num == 0) return hipSuccess;
-  const int64_t grid = (int64_t)p.B * p.num;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 g((uint32_t)grid, p.hkv, 2), t(kUnpackThreads);
-  if (p.d == 64) {
-    if (p.f32) hipLaunchKernelGGL((unpack8_kernel<64, true>), g, t, 0, st, p);
-    else hipLaunchKernelGGL((unpack8_kernel<64, false>), g, t, 0, st, p);
-  } else {
-    if (p.f32) hipLaunchKernelGGL((unpack8_kernel<128, true>), g, t, 0, st, p);
-    else hipLaunchKernelGGL((unpack8_kernel<128, false>), g, t, 0, st, p);
+hipError_t launch_unpack8(const Unpack8Params& q, hipStream_t st) {
+  if (q.num == 0) return hipSuccess;
+  Unpack8Params p = q;
+  const int rows = (int)(kLaunchGroups / p.num);        // (num <= 2^13: 2^10 at least)
+  for (p.first_row = 0; p.first_row < p.B; p.first_row += rows) {
+    const int n = p.B - p.first_row < rows ? p.B - p.first_row : rows;
+    const dim3 g((uint32_t)n * p.num, p.hkv, 2), t(kUnpackThreads);
+    if (p.d == 64) {
+      if (p.f32) hipLaunchKernelGGL((unpack8_kernel<64, true>), g, t, 0, st, p);
+      else hipLaunchKernelGGL((unpack8_kernel<64, false>), g, t, 0, st, p);
+    } else {
+      if (p.f32) hipLaunchKernelGGL((unpack8_kernel<128, true>), g, t, 0, st, p);
+      else hipLaunchKernelGGL((unpack8_kernel<128, false>), g, t, 0, st, p);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace cobs

@@ -107,3 +107,49 @@ def test_angles_past_2_51_give_nan():
                 assert abs(cos[i, j] - c) <= 9 * U32 and abs(sin[i, j] - s) <= 9 * U32, (t, f)
             else:
                 assert np.isnan(cos[i, j]) and np.isnan(sin[i, j]), (t, f)
+
+
+# --------------------------------------------------------- many workgroups --
+def test_unpack8_of_more_blocks_than_a_launch_takes():
+    """4096 rows of up to 128k tokens in blocks of 32: 2^24 blocks and rows, of which a few hold tokens."""
+    B, T, L, d = 4096, 1 << 17, 32, 64
+    cfg = cobs.Config(batch=B, num_q_heads=1, num_kv_heads=1, head_dim=d, max_seq_len=T, rank=0, budget=0, window=0, block_size=L)
+    pages = 12
+    table = torch.full((B, T // L), -1, dtype=torch.int32)
+    lens = torch.zeros(B, dtype=torch.int32)
+    held = {}
+    for page, (b, j, n) in enumerate(((0, 0, 5), (1, 4095, 32), (2047, 7, 1), (2048, 0, 32), (2049, 4095, 31), (4095, 0, 32), (4095, 4095, 32))):
+        table[b, j] = page + 2
+        lens[b] = max(int(lens[b]), j * L + n)
+        held[page + 2] = n
+    c8 = tokens.new_cache8(cfg, DEV, num_pages=pages)
+    gen = torch.Generator().manual_seed(1)
+    for x in c8[:2]:
+        x.copy_(torch.randn(x.shape, generator=gen).to(E4M3))
+    for x in c8[2:]:
+        x.copy_(2.0 ** torch.randint(-3, 4, x.shape, generator=gen))
+    k, v = (torch.full((pages, 1, L, d), 9.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    table = table.to(DEV)
+    tokens.cobs_unpack8(cfg, c8, lens.to(DEV), k, v, block_table=table, num_pages=pages, out_block_table=table, out_num_pages=pages)
+    sync()
+    for got, codes, scale in ((k, c8.k, c8.k_scale), (v, c8.v, c8.v_scale)):
+        want = torch.full_like(got, 9.0)
+        for page, n in held.items():
+            want[page, :, :n] = (codes[page, :, :n].float() * scale[page].view(1, 1, 1)).bfloat16()
+        assert torch.equal(got, want)
+
+
+def test_rotation_of_more_tokens_than_a_launch_takes():
+    """2^27 tokens of one head and a few more, 8 to a workgroup, in place."""
+    n, d = (1 << 27) + 13, 64
+    assert torch.cuda.mem_get_info()[0] > 4 * n * d
+    rope = tokens.Rope(tokens.rope_frequencies(d).to(DEV))
+    few = torch.ones((1, 5, 1, d), dtype=torch.bfloat16, device=DEV)
+    tokens.cobs_rotate(few, rope, torch.arange(5, dtype=torch.int32, device=DEV).view(1, 5), few)
+    x = torch.ones((1, n, 1, d), dtype=torch.bfloat16, device=DEV)
+    at = (torch.arange(n, dtype=torch.int32, device=DEV) % 5).view(1, n)
+    tokens.cobs_rotate(x, rope, at, x)
+    sync()
+    for i in range(0, n, 1 << 24):
+        piece = slice(i, min(n, i + (1 << 24)))
+        assert torch.equal(x[0, piece], few[0, at[0, piece].long()]), i
