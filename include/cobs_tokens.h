@@ -135,9 +135,9 @@ cobs_status_t cobs_decode8(const cobs_config_t* cfg, const void* q, cobs_dtype_t
                            const uint64_t* tree_mask, int32_t sparse, const int32_t* sel, void* out, float* lse,
                            void* ws, size_t ws_bytes, void* stream);
 
-/* Blocks of an 8-bit cache as bf16 or fp32 (kv_dtype): elements code * scale, rounded once (bf16:
- * exact for scales that are powers of two), token t to token t of another cache of the same configuration,
- * for cobs_build_block_stats and whatever else reads one.
+/* Blocks of an 8-bit cache as bf16 or fp32 (kv_dtype): elements code * scale in fp32, for bf16 rounded from
+ * there (both exact for scales that are powers of two), token t to token t of another cache of the same
+ * configuration, for cobs_build_block_stats and whatever else reads one.
  *   first_block >= 0: the blocks first_block <= j < first_block + num_blocks that a row of
  *   T = seq_lens[b] tokens has; first_block = -1: its last num_blocks blocks.  num_blocks >= 0.
  *   dst: strides or pages of its own, apart from the source.  Tokens from T on, and those whose

@@ -13,7 +13,11 @@
 //
 // Measured (d 128, 8 KV and 32 query heads, bf16): four prompts of 8k to 16k tokens in 272 us with their queries, 1.34 GB, 4.9 TB/s (HBM, the
 // rate of a large copy being 5.0); without queries 89 us, 4.1 TB/s read (a token's heads are apart by the queries') and written, waiting
-// for a block's maximum between.  One token of 64 rows: 5.4 us, a chain of loads (length, page, row, scale).
+// for a block's maximum between; in blocks of 128 tokens 132 us, as a lane's four rows take 232 registers, for two workgroups a CU.  One
+// token of 64 rows: 5.6 us, a chain of loads (length, page, row, scale), if no block's scale grows.  The D / 16 lanes of a unit encode its earlier tokens again
+// one after the other, a memory round trip each: where all 1024 units grow 31 us (blocks of 128: 50), and with scales that come from the tokens
+// that the blocks hold (normal ones) 16 us on average over a block's steps (15).  Eight tokens of 64 rows, by a wave a unit: 7.5 us without, 9.5 with
+// such scales, 11.4 if all grow.
 #include "append_body.h"
 
 namespace cobs {

@@ -7,8 +7,10 @@
 // elements and all heads of a token share it.  Then a thread takes 16 elements of a head, both
 // sides of 8 pairs, in two 16-byte pieces (bf16).
 //
-// Measured (d 128, bf16): 8190 tokens of 32 heads rotated in 29.8 us, 4.5 TB/s, one round of workgroups; 32000 in 98 us, 5.3 TB/s;
-// 32749 tokens of 32 query and 8 KV heads appended in 161 us, 5.0 TB/s (a large copy: 5.0); one token of 64 rows 4.6 us, the chain of loads.
+// Measured (d 128, bf16): 8190 tokens of 32 heads rotated in 29.6 us, 4.5 TB/s, two rounds of workgroups; 32000 in 98 us, 5.3 TB/s;
+// 32749 tokens of 32 query and 8 KV heads appended in 161 us, 5.0 TB/s (a large copy: 5.0); one token of 64 rows 4.6 us.  A thread's loads form a
+// chain: length, page, the argument block's strides, then its pointer and type (chosen by lane: queries, keys or values), the row's two pieces one
+// after the other.  Many workgroups hide it; few tokens and the first round show it (8190 tokens of 64-element heads in pairs side by side: 19.4 us, their bytes 13.3).
 #pragma once
 
 #include "tokens_device.h"

@@ -27,7 +27,9 @@ constexpr int kCounters = 4096;
 constexpr size_t kCounterBytes = kCounters * sizeof(unsigned);
 
 // Whether the last workgroup of a (row, KV head) joins its parts: few of them, as it reads them all alone (16 rows over 1000 tokens,
-// 8 parts: 11.9 us a call, 13.7 with a launch for it; over 4000 tokens, 32 parts: 20.7 and 13.7).
+// 8 parts: 11.9 us a call, 13.7 with a launch for it; over 4000 tokens, 32 parts: 20.7 and 13.7).  It goes by the average: with parts by the rows' lengths a long row
+// among short ones has more (8 rows of 8 KV heads, one of 32k tokens and 7 below 100: 4 query rows 26.6 us and 21.6, 16 query rows 36.0 and 22.4; 64 rows of one
+// KV head 86 and 23; 8 rows alike 96 and 97, 16 from 2k to 32k 111 and 112).
 static bool joined_by_last(const TreeParams& t) {
   return t.nsplit > 1 && t.mtiles == 1 && t.units <= kCounters && t.nsplit * t.a.N * t.a.G <= 128;
 }

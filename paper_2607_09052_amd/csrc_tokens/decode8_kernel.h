@@ -15,7 +15,7 @@
 // workgroups as in cobs_tree_decode.  Few rows' parts are joined by the last workgroup to leave one, others by that operator's
 // kernels.  More than R rows take more workgroups, next to each other on one XCD, whose L2 gives the frames again.
 //
-// What bounds it, d 128, bf16 queries: one token of 16 rows of 32k tokens (4 heads a KV head): 1.07 GB in 178 us, 6.0 TB/s, HBM.
+// What bounds it, d 128, bf16 queries: one token of 16 rows of 32k tokens (4 heads a KV head): 1.07 GB in 179 us, 6.0 TB/s, HBM.
 // From 32 rows on the waves' instructions: a frame of 32 rows is some 270 vector instructions (80 of them conversions)
 // and 24 products of 32 cycles, and two waves a SIMD overlap little of the one with the other (16 drafted tokens of 8 heads
 // over 4 contexts of 16k to 32k: 43 GFLOP, 64 with the probabilities' second part, in 98 us; vector pipes busy 63 % of the time, matrix
@@ -421,7 +421,8 @@ __device__ __forceinline__ void join_parts(const TreeParams& p, const TreePart& 
 }
 
 // bf16 parts of a probability: three, which hold all its bits, or two (2^-17) where the query is bf16 and the product's time counts.  Tiles of 16
-// rows wait for memory, and the third part is free (one token of 16 rows of 32k tokens 182.2 us, with two parts 181.8; 1k tokens 10.3 and 10.2);
+// rows wait for memory, and the third part costs a percent at most (one token of 16 rows of 32k tokens 183.5 us, with two parts 182.7; of 64-element heads 99.3
+// and 98.4; 1 row of 1k tokens 11.4 and 11.4);
 // tiles of 32 rows wait for the waves' instructions (16 drafted tokens of 8 heads over 4 contexts of 16k to 32k: 126 us with three, 108 with two).
 template <int PARTS, int R>
 constexpr int kProbabilityParts = PARTS == 3 || R == 16 ? 3 : 2;
