@@ -198,7 +198,7 @@ def test_caches_whose_rows_or_heads_overlap_are_not_written(over):
     dict(stride_h=(1 << 19) + 16, stride_b=(1 << 20) + 64),
 ], ids=str)
 def test_layouts_without_overlap_are_taken(over):
-    """(as far as the next check: too many tokens, too many blocks)"""
+    """(as far as the next check, which finds too many tokens)"""
     assert _append(False, kv=_kv(**over), N=1 << 24, q=None, q_out=None) == 2 and _append(True, kv=_kv8(**over), N=1 << 24, q=None, q_out=None) == 2
     one = _cfg(batch=1, num_kv_heads=1, num_q_heads=4)               # strides of dimensions of 1 are not used
     assert _append(False, one, kv=_kv(stride_b=0, stride_h=0), N=(1 << 24) + 1, q=None, q_out=None) == 2
